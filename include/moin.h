@@ -10,6 +10,7 @@
  *   moin_lora_linear      y = x W^T + s (x A_e^T) B_e^T with the expert e differing per token
  *   moin_decoder_forward  Llama-architecture decoder whose seven per-block projections are
  *                         that layer
+ *   moin_kv_*             paged key/value cache in 4 bits for generation, and the attention that reads it
  *
  * General conventions
  *   - Every tensor pointer is a DEVICE pointer owned by the caller unless the comment says
@@ -109,7 +110,8 @@ typedef struct {
 enum {
   MOIN_K_ROUTE_SIMPLE = 0, MOIN_K_ROUTE_TC = 1, MOIN_K_ROUTE_FINISH = 2, MOIN_K_PLAN = 3, MOIN_K_GEMM_WARP = 4,
   MOIN_K_GEMM_TC = 5, MOIN_K_SHRINK_STREAM = 6, MOIN_K_EXPAND_STREAM = 7, MOIN_K_SHRINK_TC = 8,
-  MOIN_K_FUSED_TC = 9, MOIN_K_GLUE = 10, MOIN_K_ATTENTION = 11, MOIN_K_ROUTE_CLUSTER = 12, MOIN_K_KMEANS_UPDATE = 13, MOIN_K_COUNT = 14
+  MOIN_K_FUSED_TC = 9, MOIN_K_GLUE = 10, MOIN_K_ATTENTION = 11, MOIN_K_ROUTE_CLUSTER = 12, MOIN_K_KMEANS_UPDATE = 13,
+  MOIN_K_KV_TABLES = 14, MOIN_K_KV_STORE = 15, MOIN_K_KV_ATTENTION = 16, MOIN_K_COUNT = 17
 };
 moin_status moin_profile_enable(int32_t capacity);
 moin_status moin_profile_read(moin_profile_record* out, int32_t capacity, int32_t* n);
@@ -438,6 +440,113 @@ moin_status moin_decoder_forward_per_token(const moin_model* model, const int32_
                                            const int32_t* token_expert, int32_t R, int32_t T, int32_t max_seqlen,
                                            void* logits, int32_t logits_mode, const moin_decoder_taps* taps,
                                            void* workspace, size_t workspace_bytes, moin_stream stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Key/value cache in 4 bits, for generation: a request's earlier tokens stay in GPU memory as quantised keys and
+ * values, in pages that any request may own, and a new token attends to them instead of running the prefix again.
+ * (The paper serves a Llama-architecture model and is silent about caches.)
+ *
+ *   moin_kv_update      wanted request lengths -> pages taken or given back, slot and position of every new token
+ *   moin_kv_append      keys and values of the new tokens -> rotated, quantised, stored by slot
+ *   moin_kv_read        stored rows by slot -> the bf16 values they stand for
+ *   moin_kv_attention   queries over their request's cached tokens: one token a request, several, or a prompt's chunk
+ *
+ * Format.  A row is the 64 channels of one token, kv head and plane (head_dim 64: one plane, 128: two) of a key or value:
+ *   zero = min(x);  scale = bf16(max((max(x) - min(x)) / 15, |zero| 2^-12, 2^-64));  code = rint((x - zero) / scale) in 0..15
+ * in fp32 (ties to even), and stands for zero + scale * code; a row with an element or a span that is not finite stands for
+ * NaN.  72 bytes hold the key and value row of a token: 4.5 bits a value.
+ * A cache is one layer's pool of n_pages pages, each [n_kv_heads][page_tokens / 16 tiles][head_dim / 64 planes][1152 bytes].
+ * The 1152 bytes of a tile of 16 tokens are 512 of key codes, 512 of value codes and 128 of pairs:
+ *   keys    byte (g, t, j, c, s) in mixed radix 8, 4, 4, 2, 2 (g slowest) holds token 8 s + g; channel 16 j + 2 t + c in its
+ *           low half, that plus 8 in its high half
+ *   values  byte (g, t, j, c, s) holds token 8 s + 2 t + c; channel 16 j + g in its low half, that plus 8 in its high half
+ *   pairs   32-bit word (g, kv, s) in mixed radix 8, 2, 2 of token 8 s + g: bf16 scale in the low half, bf16 zero in the high
+ *           half; kv 0 = key, 1 = value
+ * Slot of a token: page * page_tokens + its place in the page.  Page memory needs no initialisation: what no call has
+ * stored is never used.
+ * ------------------------------------------------------------------------------------- */
+typedef struct {
+  void* pages;          /* device, moin_kv_bytes(...) bytes, 16-byte aligned */
+  int32_t n_pages;
+  int32_t page_tokens;  /* 16, 32, 64 or 128 */
+  int32_t n_kv_heads;
+  int32_t head_dim;     /* 64 or 128; n_pages * page_tokens < 2^31 */
+} moin_kv;
+size_t moin_kv_bytes(int32_t n_pages, int32_t page_tokens, int32_t n_kv_heads, int32_t head_dim);
+
+/* Page tables of up to n_rows requests, shared by the caches of all layers (a page id means the same page in each).  All
+ * device memory, the caller's. */
+typedef struct {
+  int32_t* block_table; /* [n_rows, max_pages] page of every 16.. tokens of a row's request; only entries of held pages mean anything */
+  int32_t* free_pages;  /* [n_pages] a stack: entries below *n_free are the free pages, the last one is taken first */
+  int32_t* lens;        /* [n_rows] cached tokens */
+  int32_t* n_free;      /* [1] */
+  int32_t n_rows;       /* 1..65536 */
+  int32_t max_pages;    /* pages a request may hold; max_pages * page_tokens <= 2^30 */
+  int32_t n_pages;
+  int32_t page_tokens;
+} moin_kv_tables;
+/* No request holds anything, every page is free (page 0 is taken first). */
+moin_status moin_kv_tables_reset(const moin_kv_tables* tables, moin_stream stream);
+
+/* What an update says about its batch of R requests; the caller's device memory. */
+typedef struct {
+  int32_t R, T;      /* requests; room for new tokens: slot and pos have T entries */
+  int32_t* cu_q;     /* [R+1] offsets of the requests' new tokens in the packed batch */
+  int32_t* kv_len;   /* [R] cached tokens, the new ones included; 0 for a refused request */
+  int32_t* slot;     /* [T] slot of every new token; -1 for those of a refused request and behind the last one */
+  int32_t* pos;      /* [T] its position in its request; -1 likewise */
+  int32_t* refused;  /* [1] number of requests refused */
+} moin_kv_batch;
+
+/* Sets the length of request i of the batch, which lives in row rows[i] of the tables (rows == NULL: row i), to want[i]
+ * tokens.  A longer request takes pages and has want - len new tokens; a shorter one gives its last pages back (want = 0: all of
+ * them); equal lengths have no new tokens.  Pages given back by any request of the call can be taken by any other.  Both go in
+ * batch order, so the same call on the same tables gives the same pages.
+ * A request is refused when its row is outside [0, n_rows) or named twice in the call, when its old or wanted length is outside
+ * [0, max_pages * page_tokens], when its new tokens do not all lie below T in the packed batch, or when the pages asked for up
+ * to and including it (in batch order, by requests not refused for the other reasons) exceed the free ones.  A refused request
+ * keeps its length and pages; its new tokens keep their places in the packed batch (none, if its row or lengths are the reason),
+ * with slot -1.  Nothing is reported to the host: refused[0] counts.
+ *   lens_out, n_free_out   where the new lengths and number of free pages go (NULL: in place; else the entries of rows that the
+ *                          call does not name stay as they were)
+ * Asynchronous on `stream`, reads nothing back: it can be captured with what follows.  The calls on one set of tables must be
+ * ordered by the caller.  Errors: INVALID_ARG, BAD_SHAPE (R > n_rows, R * max_pages > 2^31 - 1, sizes beyond the struct's). */
+moin_status moin_kv_update(const moin_kv_tables* tables, const int32_t* rows, const int32_t* want, const moin_kv_batch* batch,
+                           int32_t* lens_out, int32_t* n_free_out, moin_stream stream);
+
+/* Stores row t of k and v ([T, n_kv_heads, head_dim] bf16, tokens k_stride / v_stride elements apart: multiples of 8, at least
+ * n_kv_heads * head_dim) in slot[t], for every t with a slot in [0, n_pages * page_tokens); other rows are skipped.  The slots of a call
+ * are distinct.  rope (nullable): [rope_len, head_dim / 2] fp32 (cos, sin), 16-byte aligned, see moin_rope_table: keys are rotated by
+ * their position pos[t] first (pairs (i, i + head_dim / 2), fp32, rounded to bf16); a row whose position is outside
+ * [0, rope_len) is skipped.  Only the bytes of the stored tokens are written.  T == 0 is a no-op. */
+moin_status moin_kv_append(const moin_kv* kv, const int32_t* slot, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                           const int32_t* pos, const float* rope, int32_t rope_len, int32_t T, moin_stream stream);
+
+/* Row t of k and v <- bf16 of what slot[t] holds; zeros where there is no such slot. */
+moin_status moin_kv_read(const moin_kv* kv, const int32_t* slot, void* k, int64_t k_stride, void* v, int64_t v_stride, int32_t T,
+                         moin_stream stream);
+
+/* (cos, sin) of pos * base^(-2 i / head_dim), computed in fp64: table [n_pos, head_dim / 2] pairs of fp32. */
+moin_status moin_rope_table(float* table, int32_t n_pos, int32_t head_dim, float base, moin_stream stream);
+
+/* out[t, h] = sum_j softmax_j(scale <q[t, h], K_j>) V_j over the cached tokens j of the request that token t belongs to, seen from
+ * its position: request i's queries are rows cu_q[i] .. cu_q[i+1] of q and sit at its last cu_q[i+1] - cu_q[i] positions;
+ * position x sees j <= x.  Query head h reads kv head h / (n_heads / n_kv_heads).
+ *   q, out   [T, n_heads, head_dim] bf16, tokens q_stride / out_stride elements apart (multiples of 8); may not overlap
+ *   rope     nullable, as for moin_kv_append, rope_len >= max_kv: queries are rotated by their position (fp32, rounded to bf16)
+ *   rows     [R] rows of the tables, NULL: row i
+ *   max_q, max_kv   host upper bounds of a request's queries and cached tokens (outside 1..T / 1..max_pages * page_tokens: those)
+ * A query that sees nothing (kv_len 0, a position before the first) gets zeros; so do the queries of a request whose row or kv_len is
+ * out of range.  A page id outside [0, n_pages) hides its tokens.  Rows of out behind cu_q[R] stay as they were.  fp32 scores, softmax and
+ * sums; the un-normalised weights times the value's scale enter the second product rounded to fp16, relative to the row's largest.
+ * Scratch: workspace, moin_kv_attention_workspace_bytes(...) bytes, 16-byte aligned, of this call alone while it runs.
+ * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED, WORKSPACE.  R == 0 or T == 0 is a no-op. */
+size_t moin_kv_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables* tables, const int32_t* rows, const int32_t* cu_q,
+                              const int32_t* kv_len, int32_t R, int32_t T, int32_t max_q, int32_t max_kv, const void* q,
+                              int64_t q_stride, int32_t n_heads, float scale, const float* rope, int32_t rope_len, void* out,
+                              int64_t out_stride, void* workspace, size_t workspace_bytes, moin_stream stream);
 
 #ifdef __cplusplus
 }

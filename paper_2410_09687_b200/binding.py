@@ -26,6 +26,8 @@ EXPORTED_SYMBOLS = (
     "moin_kernel_name", "moin_route_static", "moin_lora_linear_group", "moin_lora_linear_group_workspace_bytes",
     "moin_kmeans_update", "moin_route_top2", "moin_route_top2_workspace_bytes", "moin_cache_create", "moin_cache_destroy", "moin_cache_admit", "moin_cache_slot_of",
     "moin_selftest_bounded_wait", "moin_decoder_forward_per_token", "moin_dequant_fp8", "moin_pool_set_adapter",
+    "moin_kv_bytes", "moin_kv_tables_reset", "moin_kv_update", "moin_kv_append", "moin_kv_read", "moin_rope_table",
+    "moin_kv_attention_workspace_bytes", "moin_kv_attention",
 )
 
 
@@ -71,6 +73,22 @@ class _Model(ctypes.Structure):
 class _Taps(ctypes.Structure):
     _fields_ = [("hidden_in", ctypes.c_void_p), ("hidden_out", ctypes.c_void_p), ("layer_begin", ctypes.c_int32),
                 ("layer_end", ctypes.c_int32)]
+
+
+class _Kv(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class _KvTables(ctypes.Structure):
+    _fields_ = [("block_table", ctypes.c_void_p), ("free_pages", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("n_free", ctypes.c_void_p), ("n_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32)]
+
+
+class _KvBatch(ctypes.Structure):
+    _fields_ = [("R", ctypes.c_int32), ("T", ctypes.c_int32), ("cu_q", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("slot", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("refused", ctypes.c_void_p)]
 
 
 class _ProfRec(ctypes.Structure):
@@ -135,6 +153,18 @@ def lib() -> ctypes.CDLL:
         L.moin_decoder_forward_per_token.argtypes = L.moin_decoder_forward.argtypes
         L.moin_dequant_fp8.argtypes = [vp, vp, i32, i32, vp, vp]
         L.moin_pool_set_adapter.argtypes = [ctypes.POINTER(_Pool), i32, i32, vp, vp, vp]
+        i64 = ctypes.c_int64
+        L.moin_kv_bytes.restype = sz
+        L.moin_kv_bytes.argtypes = [i32, i32, i32, i32]
+        L.moin_kv_tables_reset.argtypes = [ctypes.POINTER(_KvTables), vp]
+        L.moin_kv_update.argtypes = [ctypes.POINTER(_KvTables), vp, vp, ctypes.POINTER(_KvBatch), vp, vp, vp]
+        L.moin_kv_append.argtypes = [ctypes.POINTER(_Kv), vp, vp, i64, vp, i64, vp, vp, i32, i32, vp]
+        L.moin_kv_read.argtypes = [ctypes.POINTER(_Kv), vp, vp, i64, vp, i64, i32, vp]
+        L.moin_rope_table.argtypes = [vp, i32, i32, f32, vp]
+        L.moin_kv_attention_workspace_bytes.restype = sz
+        L.moin_kv_attention_workspace_bytes.argtypes = [i32, i32, i32]
+        L.moin_kv_attention.argtypes = [ctypes.POINTER(_Kv), ctypes.POINTER(_KvTables), vp, vp, vp, i32, i32, i32, i32, vp, i64,
+                                        i32, f32, vp, i32, vp, i64, vp, sz, vp]
         L.moin_profile_enable.argtypes = [i32]
         L.moin_profile_read.argtypes = [ctypes.POINTER(_ProfRec), i32, ctypes.POINTER(i32)]
         L.moin_kernel_name.restype = ctypes.c_char_p
@@ -576,3 +606,150 @@ def decoder_forward(model: DecoderModel, tokens: torch.Tensor, cu_seqlens: torch
                                       max_seqlen, _ptr(logits), logits_mode, ctypes.byref(taps), _ptr(ws), ws.numel(),
                                       _stream(stream)), "moin_decoder_forward")
     return logits
+
+
+class KvCache:
+    """moin_kv: one layer's pool of pages of 4-bit keys and values, [n_pages, n_kv_heads, page_tokens / 16, head_dim / 64, 1152]
+    bytes (include/moin.h has the layout)."""
+
+    def __init__(self, pages: torch.Tensor):
+        assert pages.dtype == torch.uint8 and pages.dim() == 5 and pages.shape[4] == 1152
+        self.pages = pages
+        self.n_pages, self.n_kv_heads = pages.shape[0], pages.shape[1]
+        self.page_tokens, self.head_dim = pages.shape[2] * 16, pages.shape[3] * 64
+        self.c = _Kv(_ptr(pages), self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim)
+        self.ref = ctypes.byref(self.c)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, device) -> "KvCache":
+        return cls(torch.empty(n_pages, n_kv_heads, page_tokens // 16, head_dim // 64, 1152, dtype=torch.uint8, device=device))
+
+
+class KvTables:
+    """moin_kv_tables: block table, stack of free pages, lengths.  Without ``lens`` and ``n_free`` the tables start empty
+    (moin_kv_tables_reset, which also fills ``free_pages``)."""
+
+    def __init__(self, block_table: torch.Tensor, free_pages: torch.Tensor, page_tokens: int, lens: Optional[torch.Tensor] = None,
+                 n_free: Optional[torch.Tensor] = None, stream=None):
+        assert block_table.dtype == torch.int32 and block_table.dim() == 2 and free_pages.dtype == torch.int32
+        assert (lens is None) == (n_free is None)
+        reset = lens is None
+        if reset:
+            lens = torch.empty(block_table.shape[0], dtype=torch.int32, device=block_table.device)
+            n_free = torch.empty(1, dtype=torch.int32, device=block_table.device)
+        assert lens.dtype == torch.int32 and lens.shape == (block_table.shape[0],) and n_free.dtype == torch.int32 and n_free.numel() == 1
+        self.block_table, self.free_pages, self.lens, self.n_free = block_table, free_pages, lens, n_free
+        self.n_rows, self.max_pages = block_table.shape
+        self.n_pages, self.page_tokens = free_pages.shape[0], page_tokens
+        self.c = _KvTables(_ptr(block_table), _ptr(free_pages), _ptr(lens), _ptr(n_free), self.n_rows, self.max_pages, self.n_pages,
+                           page_tokens)
+        self.ref = ctypes.byref(self.c)
+        if reset:
+            self.reset(stream)
+
+    @classmethod
+    def empty(cls, n_rows: int, max_pages: int, n_pages: int, page_tokens: int, device, stream=None) -> "KvTables":
+        i32 = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device=device)  # noqa: E731
+        return cls(i32(n_rows, max_pages), i32(n_pages), page_tokens, stream=stream)
+
+    def reset(self, stream=None) -> None:
+        """moin_kv_tables_reset: every request forgotten, every page free."""
+        _check(lib().moin_kv_tables_reset(self.ref, _stream(stream)), "moin_kv_tables_reset")
+
+
+class KvBatch:
+    """moin_kv_batch: what ``kv_update`` says about R requests with up to T new tokens."""
+
+    def __init__(self, R: int, T: int, device):
+        i32 = lambda n: torch.empty(n, dtype=torch.int32, device=device)  # noqa: E731
+        self.R, self.T = R, T
+        self.cu_q, self.kv_len, self.slot, self.pos, self.refused = i32(R + 1), i32(R), i32(T), i32(T), i32(1)
+        self.c = _KvBatch(R, T, *[_ptr(t) for t in (self.cu_q, self.kv_len, self.slot, self.pos, self.refused)])
+        self.ref = ctypes.byref(self.c)
+
+
+def kv_update(tables: KvTables, want: torch.Tensor, batch: KvBatch, rows: Optional[torch.Tensor] = None,
+              lens_out: Optional[torch.Tensor] = None, n_free_out: Optional[torch.Tensor] = None, stream=None) -> KvBatch:
+    """moin_kv_update: request i (row ``rows[i]`` of the tables, or i) becomes ``want[i]`` tokens long.  Returns ``batch``."""
+    assert want.dtype == torch.int32 and want.shape == (batch.R,) and (rows is None or (rows.dtype == torch.int32 and rows.shape == want.shape))
+    assert lens_out is None or (lens_out.dtype == torch.int32 and lens_out.shape == tables.lens.shape)
+    assert n_free_out is None or (n_free_out.dtype == torch.int32 and n_free_out.numel() == 1)
+    _check(lib().moin_kv_update(tables.ref, _ptr(rows), _ptr(want), batch.ref, _ptr(lens_out), _ptr(n_free_out), _stream(stream)),
+           "moin_kv_update")
+    return batch
+
+
+def _tokens_ptr(t: torch.Tensor, heads: int, head_dim: int) -> tuple:
+    """(address, elements between tokens) of [T, heads, head_dim] bf16 (or [T, heads * head_dim]) whose tokens may lie apart."""
+    if not t.is_cuda:
+        raise MoinError("tensor arguments must live on a CUDA device (no CPU path exists)")
+    assert t.dtype == torch.bfloat16 and (t.shape[1:] == (heads, head_dim) or t.shape[1:] == (heads * head_dim,)), t.shape
+    if t.stride(-1) != 1 or (t.dim() == 3 and heads > 1 and t.stride(1) != head_dim):
+        raise MoinError("the heads of a token must lie side by side")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else heads * head_dim)
+
+
+def _rope_arg(rope: Optional[torch.Tensor], head_dim: int) -> tuple:
+    if rope is None:
+        return None, 0
+    assert rope.dtype == torch.float32 and rope.dim() == 3 and rope.shape[1:] == (head_dim // 2, 2)
+    return _ptr(rope), rope.shape[0]
+
+
+def rope_table(n_pos: int, head_dim: int, base: float, device, stream=None) -> torch.Tensor:
+    """moin_rope_table: [n_pos, head_dim / 2, 2] fp32 (cos, sin)."""
+    table = torch.empty(n_pos, head_dim // 2, 2, dtype=torch.float32, device=device)
+    _check(lib().moin_rope_table(_ptr(table), n_pos, head_dim, float(base), _stream(stream)), "moin_rope_table")
+    return table
+
+
+def kv_append(cache: KvCache, slot: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: Optional[torch.Tensor] = None,
+              rope: Optional[torch.Tensor] = None, stream=None) -> None:
+    """moin_kv_append: quantise row t of ``k`` (rotated by ``rope`` at ``pos[t]`` if given) and ``v`` and store them in ``slot[t]``."""
+    T = slot.shape[0]
+    assert slot.dtype == torch.int32 and k.shape[0] == T and v.shape[0] == T
+    assert rope is None or (pos is not None and pos.dtype == torch.int32 and pos.shape == slot.shape)
+    kp, ks = _tokens_ptr(k, cache.n_kv_heads, cache.head_dim)
+    vp, vs = _tokens_ptr(v, cache.n_kv_heads, cache.head_dim)
+    rp, rn = _rope_arg(rope, cache.head_dim)
+    _check(lib().moin_kv_append(cache.ref, _ptr(slot), kp, ks, vp, vs, _ptr(pos), rp, rn, T, _stream(stream)), "moin_kv_append")
+
+
+def kv_read(cache: KvCache, slot: torch.Tensor, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None, stream=None) -> tuple:
+    """moin_kv_read: (k, v), bf16 [T, n_kv_heads, head_dim], of what the slots hold."""
+    T, H, D = slot.shape[0], cache.n_kv_heads, cache.head_dim
+    assert slot.dtype == torch.int32
+    if k is None:
+        k = torch.empty(T, H, D, dtype=torch.bfloat16, device=slot.device)
+    if v is None:
+        v = torch.empty(T, H, D, dtype=torch.bfloat16, device=slot.device)
+    assert k.shape[0] == T and v.shape[0] == T
+    kp, ks = _tokens_ptr(k, H, D)
+    vp, vs = _tokens_ptr(v, H, D)
+    _check(lib().moin_kv_read(cache.ref, _ptr(slot), kp, ks, vp, vs, T, _stream(stream)), "moin_kv_read")
+    return k, v
+
+
+def kv_attention(cache: KvCache, tables: KvTables, q: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor, max_q: int = 0,
+                 max_kv: int = 0, rows: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                 rope: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """moin_kv_attention: q [T, n_heads, head_dim] over the cached tokens of each token's request.  Returns out, like q; rows of a new
+    ``out`` behind the last request are undefined."""
+    T, n_heads, D = q.shape
+    R = kv_len.shape[0]
+    assert cu_q.dtype == torch.int32 and cu_q.shape == (R + 1,) and kv_len.dtype == torch.int32 and D == cache.head_dim
+    assert rows is None or (rows.dtype == torch.int32 and rows.shape == kv_len.shape)
+    if out is None:
+        out = torch.empty(T, n_heads, D, dtype=torch.bfloat16, device=q.device)
+    assert out.shape == q.shape
+    qp, qs = _tokens_ptr(q, n_heads, D)
+    op, os_ = _tokens_ptr(out, n_heads, D)
+    rp, rn = _rope_arg(rope, D)
+    n, s = lib().moin_kv_attention_workspace_bytes(n_heads, cache.n_kv_heads, D), _stream(stream)
+    ws = _scratch_alloc(n, s)
+    try:
+        _check(lib().moin_kv_attention(cache.ref, tables.ref, _ptr(rows), _ptr(cu_q), _ptr(kv_len), R, T, max_q, max_kv, qp, qs, n_heads,
+                                       D ** -0.5 if scale is None else float(scale), rp, rn, op, os_, ws, n, s), "moin_kv_attention")
+    finally:
+        _scratch_free(ws)
+    return out

@@ -186,7 +186,8 @@ moin_status moin_profile_read(moin_profile_record* out, int32_t capacity, int32_
 const char* moin_kernel_name(int32_t k) {
   static const char* names[MOIN_K_COUNT] = {"route_simple", "route_tc", "route_finish", "plan", "gemm_warp", "gemm_tc",
                                             "lora_shrink_stream", "lora_expand_stream", "lora_shrink_tc",
-                                            "lora_fused_tc", "decoder_glue", "attention", "route_cluster", "kmeans_update"};
+                                            "lora_fused_tc", "decoder_glue", "attention", "route_cluster", "kmeans_update",
+                                            "kv_tables", "kv_store", "kv_attention"};
   return (k >= 0 && k < MOIN_K_COUNT) ? names[k] : "unknown";
 }
 
