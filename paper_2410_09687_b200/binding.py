@@ -162,7 +162,7 @@ def lib() -> ctypes.CDLL:
         L.moin_kv_read.argtypes = [ctypes.POINTER(_Kv), vp, vp, i64, vp, i64, i32, vp]
         L.moin_rope_table.argtypes = [vp, i32, i32, f32, vp]
         L.moin_kv_attention_workspace_bytes.restype = sz
-        L.moin_kv_attention_workspace_bytes.argtypes = [i32, i32, i32]
+        L.moin_kv_attention_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.moin_kv_attention.argtypes = [ctypes.POINTER(_Kv), ctypes.POINTER(_KvTables), vp, vp, vp, i32, i32, i32, i32, vp, i64,
                                         i32, f32, vp, i32, vp, i64, vp, sz, vp]
         L.moin_profile_enable.argtypes = [i32]
@@ -745,7 +745,8 @@ def kv_attention(cache: KvCache, tables: KvTables, q: torch.Tensor, cu_q: torch.
     qp, qs = _tokens_ptr(q, n_heads, D)
     op, os_ = _tokens_ptr(out, n_heads, D)
     rp, rn = _rope_arg(rope, D)
-    n, s = lib().moin_kv_attention_workspace_bytes(n_heads, cache.n_kv_heads, D), _stream(stream)
+    max_q = T if max_q < 1 or max_q > T else max_q
+    n, s = lib().moin_kv_attention_workspace_bytes(max_q, n_heads, cache.n_kv_heads, D), _stream(stream)
     ws = _scratch_alloc(n, s)
     try:
         _check(lib().moin_kv_attention(cache.ref, tables.ref, _ptr(rows), _ptr(cu_q), _ptr(kv_len), R, T, max_q, max_kv, qp, qs, n_heads,

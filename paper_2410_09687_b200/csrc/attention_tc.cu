@@ -71,26 +71,6 @@ __device__ __forceinline__ float fast_exp2(float x) {   // x <= kAtLag here: 2^x
   return y;
 }
 
-// Two-lane fp32 arithmetic (one instruction for a pair of scores): the softmax threads are bound by the number of
-// instructions they issue, not by any one pipe.
-__device__ __forceinline__ uint64_t pair_f32(float lo, float hi) {
-  uint64_t d;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
-  return d;
-}
-__device__ __forceinline__ void unpair_f32(uint64_t v, float& lo, float& hi) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 // byte offset of 16-byte chunk c of row r in a swizzled [rows x 128 bytes] tile
 __device__ __forceinline__ uint32_t at_swz(int r, int c) {
   return (uint32_t)((r >> 3) * 1024 + (r & 7) * 128 + ((c ^ (r & 7)) << 4));

@@ -21,10 +21,14 @@
 #include <float.h>
 
 #include "kv.cuh"
+#include "ptx.cuh"
 
 namespace moin {
 
 constexpr int kKvAttWarps = 4;
+constexpr int kKvMaxWorkers = 1024;  // CTAs that share the work, at most
+constexpr int kKvStages = 3;         // steps of a warp in shared memory
+constexpr int kKvItemCost = 8;       // what beginning an item costs, in tiles
 constexpr float kKvTop = 10.f;       // log2 of the largest weight after a rescale
 constexpr float kKvMost = 15.f;      // log2 of the largest weight at all
 
@@ -33,11 +37,16 @@ struct KvAttParams {
   const int *table, *rows, *cu_q, *kv_len;
   int n_rows, max_pages;
   int R, T, max_q, max_kv, G, n_heads;
+  uint32_t inv_g;          // row / G = row inv_g >> 32
   const __nv_bfloat16* q;
   __nv_bfloat16* out;
   long long q_stride, out_stride;
   const float2* rope;      // [rope_len, D / 2] or nullptr
   float scale_log2;
+  int split;               // items are cut: CTAs take equal shares of all tiles (else a CTA takes an item)
+  float* part;             // [worker][2][row][64 P + 4]: sums of items that several workers share
+  int4* desc;              // [worker][2]: what they belong to
+  DeviceStatus* status;
 };
 
 __device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -66,7 +75,9 @@ __device__ __forceinline__ float kv_rescale_sum(float l, float d) {
   return l * f * f;
 }
 
-// What a CTA works on: the rows [row0, row0 + 8 NT) of request `req` and kv head `head`; row = (query token) * G + head of the group.
+__device__ __forceinline__ int kv_div_g(const KvAttParams& p, int row) { return p.G == 1 ? row : (int)__umulhi((uint32_t)row, p.inv_g); }
+
+// What a warp works on: the rows [row0, row0 + 8 NT) of request `req` and kv head `head`; row = (query token) * G + head of the group.
 struct KvItem {
   int req, head, row0;
   int t0, q_len, kv_len;      // first query row of the request in q, its tokens, its cached tokens (0: nothing to see)
@@ -86,16 +97,17 @@ __device__ __forceinline__ KvItem kv_item(const KvAttParams& p, int req, int hea
 }
 
 template <int P, int NT>
-struct KvState {            // a warp's share of an item: 8 NT rows, 64 P channels
-  float o[NT][P][4][4];     // [channel block of 16][(g, row 2 t), (g, row 2 t + 1), (g + 8, ..)]
-  float m[NT][2], l[NT][2], z[P][NT][2];
+struct KvState {            // a warp's share of an item: 8 NT rows, 64 P channels; pairs are rows 2 t, 2 t + 1 of an n-tile
+  uint64_t o[NT][P][4][2];  // [channel block of 16][g, g + 8]
+  uint64_t m[NT], l[NT], z[P][NT];   // m: negated
+  uint32_t fresh;           // bit 2 n + c: the row has seen no key yet (its m is 0 and means nothing)
 };
 
 // Query rows as B fragments: b[n][plane][k-step][half], and per row (2 t, 2 t + 1 of an n-tile) the factor and the sum.
 template <int P, int NT>
 struct KvQuery {
   uint32_t b[NT][P][4][2];
-  float fac[NT][2], sum[P][NT][2];
+  uint64_t fac[NT], sum[P][NT];
   int last[NT][2];          // last key the row sees
   int all;                  // keys below this are seen by every row
 };
@@ -108,7 +120,7 @@ __device__ __forceinline__ void kv_load_query(const KvAttParams& p, const KvItem
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int row = it.row0 + 8 * n + g;
-    const int qi = row / p.G;
+    const int qi = kv_div_g(p, row);
     const bool live = row < n_rows && past + qi >= 0;
     float x[P][16];
 #pragma unroll
@@ -116,7 +128,7 @@ __device__ __forceinline__ void kv_load_query(const KvAttParams& p, const KvItem
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[pl][i] = 0.f;
     if (live) {
-      const __nv_bfloat16* src = p.q + (long long)(it.t0 + qi) * p.q_stride + (it.head * p.G + row % p.G) * 64 * P;
+      const __nv_bfloat16* src = p.q + (long long)(it.t0 + qi) * p.q_stride + (it.head * p.G + row - qi * p.G) * 64 * P;
 #pragma unroll
       for (int pl = 0; pl < P; ++pl)
 #pragma unroll
@@ -164,15 +176,15 @@ __device__ __forceinline__ void kv_load_query(const KvAttParams& p, const KvItem
     }
     // to the lanes that hold these rows' scores: rows 2 t, 2 t + 1 of the n-tile
     const float fac = p.scale_log2 * 0x1p24f / f;
+    q.fac[n] = pair_f32(__shfl_sync(0xffffffffu, fac, 8 * t), __shfl_sync(0xffffffffu, fac, 8 * t + 4));
+#pragma unroll
+    for (int pl = 0; pl < P; ++pl)
+      q.sum[pl][n] = pair_f32(__shfl_sync(0xffffffffu, sum[pl], 8 * t) * p.scale_log2, __shfl_sync(0xffffffffu, sum[pl], 8 * t + 4) * p.scale_log2);
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      const int from = 4 * (2 * t + c);
-      q.fac[n][c] = __shfl_sync(0xffffffffu, fac, from);
-#pragma unroll
-      for (int pl = 0; pl < P; ++pl) q.sum[pl][n][c] = __shfl_sync(0xffffffffu, sum[pl], from) * p.scale_log2;
       const int r = it.row0 + 8 * n + 2 * t + c;
       // rows that are not there compute something that is not stored, and mask nothing
-      q.last[n][c] = r < n_rows ? past + r / p.G : it.kv_len - 1;
+      q.last[n][c] = r < n_rows ? past + kv_div_g(p, r) : it.kv_len - 1;
       q.all = min(q.all, q.last[n][c] + 1);
     }
   }
@@ -180,237 +192,565 @@ __device__ __forceinline__ void kv_load_query(const KvAttParams& p, const KvItem
   q.all = min(q.all, __shfl_xor_sync(0xffffffffu, q.all, 2));
 }
 
-struct KvTileRegs { uint4 k, v, pr; };
+__device__ __forceinline__ uint64_t twice_f32(float v) { return pair_f32(v, v); }
 
-template <int P>
-__device__ __forceinline__ void kv_load_tile(const uint8_t* at, int lane, KvTileRegs (&r)[P]) {
-#pragma unroll
-  for (int pl = 0; pl < P; ++pl) {
-    r[pl].k = ldg_stream(at + pl * kKvTileBytes + 16 * lane);
-    r[pl].v = ldg_stream(at + pl * kKvTileBytes + 512 + 16 * lane);
-    r[pl].pr = ldg_stream(at + pl * kKvTileBytes + kKvPairs + 16 * (lane >> 2));
-  }
-}
-
-// One tile of 16 tokens from `key0` on.
-template <int P, int NT>
-__device__ __forceinline__ void kv_tile(const KvTileRegs (&r)[P], int key0, int kv_len, const KvQuery<P, NT>& q, int lane, KvState<P, NT>& st) {
+// U tiles of 16 tokens from shared memory, the first at key0; bit u of `there`: tile u is part of the warp's work.  `whole`: every
+// row sees every token.
+template <bool whole, int P, int NT, int U>
+__device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, int key0, int kv_len, const KvQuery<P, NT>& q, int lane, KvState<P, NT>& st) {
   constexpr uint32_t kLo = 0x000F000Fu, kHi = 0x00F000F0u;
   const int g = lane >> 2;
-  float s[NT][4];
-  uint32_t pk[P][2], pv[P][2];
-  const bool whole = key0 + kKvTile <= q.all;
+  uint64_t s[U][NT][2];    // [token g, g + 8]: scores in powers of two, less the row's m
+  uint32_t pv[U][P][2];
+  float lg[U][2];
 #pragma unroll
-  for (int pl = 0; pl < P; ++pl) {
-    pk[pl][0] = r[pl].pr.x; pk[pl][1] = r[pl].pr.y; pv[pl][0] = r[pl].pr.z; pv[pl][1] = r[pl].pr.w;
-    if (!whole) {   // what lies behind the last token was never written
-      if (key0 + g >= kv_len) pk[pl][0] = pv[pl][0] = 0;
-      if (key0 + g + 8 >= kv_len) pk[pl][1] = pv[pl][1] = 0;
-    }
-    const uint32_t kw[4] = {r[pl].k.x, r[pl].k.y, r[pl].k.z, r[pl].k.w};
-    float acc[NT][4];
+  for (int u = 0; u < U; ++u) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+    for (int pl = 0; pl < P; ++pl) {
+      const uint8_t* at = tiles + (u * P + pl) * kKvTileBytes;
+      const uint4 k4 = *reinterpret_cast<const uint4*>(at + 16 * lane);
+      const uint4 pr = *reinterpret_cast<const uint4*>(at + kKvPairs + 16 * g);
+      uint32_t pk[2] = {pr.x, pr.y};
+      pv[u][pl][0] = pr.z;
+      pv[u][pl][1] = pr.w;
+      if (!whole) {   // what lies behind the last token, or in a tile that was not fetched, may be anything
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t w = kw[j], w8 = w >> 8;
-#pragma unroll
-      for (int n = 0; n < NT; ++n) mma_f16_16816(acc[n], w & kLo, w8 & kLo, w & kHi, w8 & kHi, q.b[n][pl][j][0], q.b[n][pl][j][1]);
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float zero = pl == 0 ? 0.f : s[n][e];
-        s[n][e] = fmaf(acc[n][e], q.fac[n][e & 1] * kv_scale(pk[pl][e >> 1]), fmaf(q.sum[pl][n][e & 1], kv_zero(pk[pl][e >> 1]), zero));
+        for (int h = 0; h < 2; ++h)
+          if (!(there >> u & 1u) || key0 + u * kKvTile + g + 8 * h >= kv_len) pk[h] = pv[u][pl][h] = 0;
       }
+      const uint32_t kw[4] = {k4.x, k4.y, k4.z, k4.w};
+      float acc[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t w = kw[j], w8 = w >> 8;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma_f16_16816(acc[n], w & kLo, w8 & kLo, w & kHi, w8 & kHi, q.b[n][pl][j][0], q.b[n][pl][j][1]);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint64_t ks = twice_f32(kv_scale(pk[h])), kz = twice_f32(kv_zero(pk[h]));
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          s[u][n][h] = fma2(pair_f32(acc[n][2 * h], acc[n][2 * h + 1]), mul2(q.fac[n], ks), fma2(q.sum[pl][n], kz, pl == 0 ? st.m[n] : s[u][n][h]));
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float sv = kv_scale(pv[u][0][h]);
+      if (P == 2) sv = fmaxf(sv, kv_scale(pv[u][P - 1][h]));
+      lg[u][h] = fmaxf(kv_log2(sv), -64.f);
+    }
+    if (!whole) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int key = key0 + u * kKvTile + g + 8 * h;
+          float a, b;
+          unpair_f32(s[u][n][h], a, b);
+          if (!(there >> u & 1u) || key > q.last[n][0]) a = -INFINITY;
+          if (!(there >> u & 1u) || key > q.last[n][1]) b = -INFINITY;
+          s[u][n][h] = pair_f32(a, b);
+        }
+    }
   }
-  float lg[2];
+  float top[NT][2];
+  bool grow = st.fresh != 0;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float sv = kv_scale(pv[0][h]);
-    if (P == 2) sv = fmaxf(sv, kv_scale(pv[P - 1][h]));
-    lg[h] = fmaxf(kv_log2(sv), -64.f);
+  for (int n = 0; n < NT; ++n) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float a0, b0, a1, b1;
+      unpair_f32(s[u][n][0], a0, b0);
+      unpair_f32(s[u][n][1], a1, b1);
+      a0 += lg[u][0]; b0 += lg[u][0]; a1 += lg[u][1]; b1 += lg[u][1];
+      top[n][0] = u == 0 ? fmaxf(a0, a1) : fmax3(top[n][0], a0, a1);
+      top[n][1] = u == 0 ? fmaxf(b0, b1) : fmax3(top[n][1], b0, b1);
+    }
+    grow = grow || fmaxf(top[n][0], top[n][1]) > kKvMost;
   }
-  if (!whole) {
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (key0 + g + 8 * (e >> 1) > q.last[n][e & 1]) s[n][e] = -INFINITY;
-  }
-  bool grow = false;
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) grow = grow || s[n][e] + lg[e >> 1] > st.m[n][e & 1] + kKvMost;
   if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n) {
+      float up[2], corr[2];   // the new m is so much larger
+      float l[2];
+      unpair_f32(st.l[n], l[0], l[1]);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        float mx = fmaxf(s[n][c] + lg[0], s[n][c + 2] + lg[1]);
+        float mx = top[n][c];
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-        if (mx > st.m[n][c] + kKvMost) {
-          const float m = mx - kKvTop, corr = kv_exp2(st.m[n][c] - m);
-          st.l[n][c] = kv_rescale_sum(st.l[n][c], st.m[n][c] - m);
-          st.m[n][c] = m;
-#pragma unroll
-          for (int pl = 0; pl < P; ++pl) {
-            st.z[pl][n][c] *= corr;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              st.o[n][pl][j][c] *= corr;
-              st.o[n][pl][j][c + 2] *= corr;
-            }
+        const uint32_t bit = 1u << (2 * n + c);
+        const bool fresh = st.fresh & bit;      // (its sums are 0, or NaN for good)
+        up[c] = 0.f;
+        corr[c] = 1.f;
+        if (mx > (fresh ? -INFINITY : kKvMost)) {
+          up[c] = mx - kKvTop;
+          st.fresh &= ~bit;
+          if (!fresh) {
+            corr[c] = kv_exp2(-up[c]);
+            l[c] = kv_rescale_sum(l[c], -up[c]);
           }
         }
       }
-  }
-  uint32_t b[NT][P][2];
+      const uint64_t less = pair_f32(-up[0], -up[1]), f = pair_f32(corr[0], corr[1]);
+      st.m[n] = add2(st.m[n], less);
+      st.l[n] = pair_f32(l[0], l[1]);
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    float pr[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      pr[e] = kv_exp2(s[n][e] - st.m[n][e & 1]);
-      st.l[n][e & 1] += pr[e];
-    }
-#pragma unroll
-    for (int pl = 0; pl < P; ++pl) {
-      float w[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float zv = kv_zero(pv[pl][e >> 1]);
-        w[e] = pr[e] * kv_scale(pv[pl][e >> 1]);
-        if (!whole) {   // a value that a row must not see may be anything
-          const bool out = key0 + g + 8 * (e >> 1) > q.last[n][e & 1];
-          w[e] = out ? 0.f : w[e];
-          st.z[pl][n][e & 1] += out ? 0.f : pr[e] * zv;
-        } else {
-          st.z[pl][n][e & 1] = fmaf(pr[e], zv, st.z[pl][n][e & 1]);
-        }
-      }
-      b[n][pl][0] = movmatrix_trans(pack_f16(w[0], w[1]));
-      b[n][pl][1] = movmatrix_trans(pack_f16(w[2], w[3]));
-    }
-  }
-#pragma unroll
-  for (int pl = 0; pl < P; ++pl) {
-    const uint32_t vw[4] = {r[pl].v.x, r[pl].v.y, r[pl].v.z, r[pl].v.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t w = vw[j], w8 = w >> 8;
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float d[4] = {0.f, 0.f, 0.f, 0.f};
-        mma_f16_16816(d, w & kLo, w & kHi, w8 & kLo, w8 & kHi, b[n][pl][0], b[n][pl][1]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) st.o[n][pl][j][e] += d[e];
-      }
-    }
-  }
-}
-
-// A CTA takes an item; its warps take the item's tiles in turn and meet in shared memory.
-template <int P, int NT>
-__global__ void __launch_bounds__(32 * kKvAttWarps)
-kv_attention_kernel(const KvAttParams p) {
-  constexpr int kRows = 8 * NT, kCh = 64 * P, kPitch = kCh + 4;
-  extern __shared__ float smem[];
-  float* s_o = smem;                                             // [warp][row][channel]
-  float* s_ml = smem + kKvAttWarps * kRows * kPitch;             // [warp][row][m, l, z ..]
-  pdl_begin();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const KvItem it = kv_item(p, blockIdx.z, blockIdx.y, blockIdx.x * kRows);
-  const int n_rows = it.q_len * p.G;
-  if (it.row0 >= n_rows) return;
-  KvQuery<P, NT> q;
-  kv_load_query<P, NT>(p, it, lane, q);
-  KvState<P, NT> st;
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      st.m[n][c] = -FLT_MAX;
-      st.l[n][c] = 0.f;
-#pragma unroll
-      for (int pl = 0; pl < P; ++pl) st.z[pl][n][c] = 0.f;
-    }
-#pragma unroll
-    for (int pl = 0; pl < P; ++pl)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) st.o[n][pl][j][0] = st.o[n][pl][j][1] = st.o[n][pl][j][2] = st.o[n][pl][j][3] = 0.f;
-  }
-  // keys that the last row of the tile sees
-  const int see = max(0, min(it.kv_len, it.kv_len - it.q_len + min(it.row0 + kRows - 1, n_rows - 1) / p.G + 1));
-  const int n_tiles = (see + kKvTile - 1) / kKvTile, tpp = p.kv.page_tokens / kKvTile;
-  for (int i = warp; i < n_tiles; i += kKvAttWarps) {
-    const int page = __ldg(it.table + i / tpp);
-    if (page < 0 || page >= p.kv.n_pages) continue;   // (the same for the whole warp)
-    KvTileRegs r[P];
-    kv_load_tile<P>(p.kv.pages + p.kv.tile_at(page, it.head, i % tpp), lane, r);
-    kv_tile<P, NT>(r, i * kKvTile, it.kv_len, q, lane, st);
-  }
-  // ---- this warp's sums to shared memory
-  float* mine = s_o + warp * kRows * kPitch;
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int row = 8 * n + 2 * t + c;
-#pragma unroll
-      for (int o = 4; o < 32; o <<= 1) {
-        st.l[n][c] += __shfl_xor_sync(0xffffffffu, st.l[n][c], o);
-#pragma unroll
-        for (int pl = 0; pl < P; ++pl) st.z[pl][n][c] += __shfl_xor_sync(0xffffffffu, st.z[pl][n][c], o);
-      }
-      if (g == 0) {
-        float* ml = s_ml + (warp * kRows + row) * 4;
-        ml[0] = st.m[n][c];
-        ml[1] = st.l[n][c];
-#pragma unroll
-        for (int pl = 0; pl < P; ++pl) ml[2 + pl] = st.z[pl][n][c];
+      for (int u = 0; u < U; ++u) {
+        s[u][n][0] = add2(s[u][n][0], less);
+        s[u][n][1] = add2(s[u][n][1], less);
       }
 #pragma unroll
-      for (int pl = 0; pl < P; ++pl)
+      for (int pl = 0; pl < P; ++pl) {
+        st.z[pl][n] = mul2(st.z[pl][n], f);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          mine[row * kPitch + 64 * pl + 16 * j + g] = st.o[n][pl][j][c] * 0x1p24f;
-          mine[row * kPitch + 64 * pl + 16 * j + 8 + g] = st.o[n][pl][j][c + 2] * 0x1p20f;
+          st.o[n][pl][j][0] = mul2(st.o[n][pl][j][0], f);
+          st.o[n][pl][j][1] = mul2(st.o[n][pl][j][1], f);
         }
+      }
     }
-  __syncthreads();
-  // ---- joined: a thread takes two channels of a row
-  for (int i = threadIdx.x; i < kRows * kCh / 2; i += 32 * kKvAttWarps) {
-    const int row = i / (kCh / 2), ch = 2 * (i % (kCh / 2));
-    const int r = it.row0 + row;
-    if (r >= n_rows) continue;
-    float top = -FLT_MAX;
+  }
+  uint32_t b[U][NT][P][2];
 #pragma unroll
-    for (int w = 0; w < kKvAttWarps; ++w) top = fmaxf(top, s_ml[(w * kRows + row) * 4]);
-    float l = 0.f, a = 0.f, b = 0.f;
+  for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int w = 0; w < kKvAttWarps; ++w) {
-      const float* ml = s_ml + (w * kRows + row) * 4;
-      const float f = kv_exp2(ml[0] - top);
-      const float* o = s_o + (w * kRows + row) * kPitch + ch;
-      l += kv_rescale_sum(ml[1], ml[0] - top);
-      a += (o[0] + ml[2 + ch / 64]) * f;
-      b += (o[1] + ml[2 + ch / 64]) * f;
+    for (int h = 0; h < 2; ++h) {
+      uint64_t pr[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float x, y;
+        unpair_f32(s[u][n][h], x, y);
+        pr[n] = pair_f32(kv_exp2(x), kv_exp2(y));
+        st.l[n] = add2(st.l[n], pr[n]);
+      }
+#pragma unroll
+      for (int pl = 0; pl < P; ++pl) {
+        const uint64_t sv = twice_f32(kv_scale(pv[u][pl][h])), zv = twice_f32(kv_zero(pv[u][pl][h]));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float x, y;
+          if (whole) {
+            st.z[pl][n] = fma2(pr[n], zv, st.z[pl][n]);
+            unpair_f32(mul2(pr[n], sv), x, y);
+          } else {   // a value that a row must not see may be NaN
+            const int key = key0 + u * kKvTile + g + 8 * h;
+            const bool out0 = !(there >> u & 1u) || key > q.last[n][0], out1 = !(there >> u & 1u) || key > q.last[n][1];
+            float zx, zy;
+            unpair_f32(mul2(pr[n], zv), zx, zy);
+            unpair_f32(mul2(pr[n], sv), x, y);
+            x = out0 ? 0.f : x;
+            y = out1 ? 0.f : y;
+            st.z[pl][n] = add2(st.z[pl][n], pair_f32(out0 ? 0.f : zx, out1 ? 0.f : zy));
+          }
+          b[u][n][pl][h] = movmatrix_trans(pack_f16(x, y));
+        }
+      }
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;   // nothing to see: zeros
-    *reinterpret_cast<uint32_t*>(p.out + (long long)(it.t0 + r / p.G) * p.out_stride + (it.head * p.G + r % p.G) * kCh + ch) = pack_bf16(a * inv, b * inv);
+#pragma unroll
+  for (int pl = 0; pl < P; ++pl) {
+    uint4 v4[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v4[u] = *reinterpret_cast<const uint4*>(tiles + (u * P + pl) * kKvTileBytes + 512 + 16 * lane);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float d[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) d[n][0] = d[n][1] = d[n][2] = d[n][3] = 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t w = j == 0 ? v4[u].x : j == 1 ? v4[u].y : j == 2 ? v4[u].z : v4[u].w, w8 = w >> 8;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma_f16_16816(d[n], w & kLo, w & kHi, w8 & kLo, w8 & kHi, b[u][n][pl][0], b[u][n][pl][1]);
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        st.o[n][pl][j][0] = add2(st.o[n][pl][j][0], pair_f32(d[n][0], d[n][1]));
+        st.o[n][pl][j][1] = add2(st.o[n][pl][j][1], pair_f32(d[n][2], d[n][3]));
+      }
+    }
   }
 }
 
+// What a request counts for an item: its tiles and the cost of beginning.  Items without tiles are there too: their rows are written.
+__device__ __forceinline__ int kv_count(int kv_len, int max_kv) {
+  return kKvItemCost + (kv_len < 1 || kv_len > max_kv ? 1 : (kv_len + kKvTile - 1) / kKvTile);
+}
+__device__ __forceinline__ long long kv_cost(const KvAttParams& p, int req, int rows) {
+  const int t0 = min(max(p.cu_q[req], 0), p.T), t1 = min(max(p.cu_q[req + 1], t0), p.T);
+  const int blocks = (int)(((long long)(t1 - t0) * p.G + rows - 1) / rows);
+  return (long long)blocks * p.kv.H * kv_count(p.kv_len[req], p.max_kv);
+}
+
+// All items stand in one line (request, row block, head), each as long as it counts, and warp w of W takes from total w / W on.
+// Every CTA finds its warps' places: each thread adds up a run of requests, a scan over the CTA gives the total, and the
+// thread whose run holds a place walks it.
+struct KvShare { long long at, end, base; int req; };   // base: what the requests before `req` count
+template <int NT, int U>
+__device__ __forceinline__ void kv_share(const KvAttParams& p, long long* s_sum, KvShare* s_share) {
+  constexpr int kThreads = 32 * kKvAttWarps;
+  const int tid = threadIdx.x, lane = tid & 31, per = (p.R + kThreads - 1) / kThreads;
+  const int r0 = min(tid * per, p.R), r1 = min(r0 + per, p.R);
+  long long mine = 0;
+  for (int r = r0; r < r1; ++r) mine += kv_cost(p, r, 8 * NT);
+  long long inc = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long a = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += a;
+  }
+  if (lane == 31) s_sum[tid >> 5] = inc;
+  if (tid < kKvAttWarps) s_share[tid] = {0, 0, 0, 0};
+  __syncthreads();
+  long long total = 0, before = inc - mine;
+#pragma unroll
+  for (int w = 0; w < kKvAttWarps; ++w) {
+    if (w < (tid >> 5)) before += s_sum[w];
+    total += s_sum[w];
+  }
+  // as many warps as there are, or fewer, so that a share is worth beginning
+  const long long W = min((long long)gridDim.x * kKvAttWarps, (total + kKvItemCost + 2 * U - 1) / (kKvItemCost + 2 * U));
+  const long long stop = before + mine;
+  int r = r0;
+  for (int i = 0; i < kKvAttWarps; ++i) {
+    const long long w = (long long)blockIdx.x * kKvAttWarps + i;
+    if (w >= W) break;
+    const long long at = total * w / W, end = total * (w + 1) / W;
+    if (at < before || at >= stop) continue;
+    for (;;) {
+      const long long c = kv_cost(p, r, 8 * NT);
+      if (at < before + c) break;
+      before += c;
+      ++r;
+    }
+    s_share[i] = {at, end, before, r};
+  }
+  __syncthreads();
+}
+
+// Sums of some rows taken against different maxima, four channels of one row: joined one by one, always in the order of the tokens.
+struct KvSum {
+  float m, l;
+  float4 v;
+  __device__ __forceinline__ void add(float m2, float l2, const float4& v2) {
+    const float top = fmaxf(m, m2), f1 = kv_exp2(m - top), f2 = kv_exp2(m2 - top);
+    l = kv_rescale_sum(l, m - top) + kv_rescale_sum(l2, m2 - top);
+    v.x = v.x * f1 + v2.x * f2; v.y = v.y * f1 + v2.y * f2; v.z = v.z * f1 + v2.z * f2; v.w = v.w * f1 + v2.w * f2;
+    m = top;
+  }
+  __device__ __forceinline__ uint2 result() const {
+    const float inv = l == 0.f ? 0.f : 1.f / l;   // nothing to see: zeros
+    return make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
+  }
+};
+__device__ __forceinline__ __nv_bfloat16* kv_out(const KvAttParams& p, int t0, int head, int r, int ch, int channels) {
+  const int qi = kv_div_g(p, r);
+  return p.out + (long long)(t0 + qi) * p.out_stride + (head * p.G + r - qi * p.G) * channels + ch;
+}
+
+// A piece of an item as its warp leaves it: rows of kPitch floats, 64 P sums and the row's maximum and sum of weights behind them.
+// In slot 0 the piece that begins inside its item (the first of a warp, or of a CTA), in slot 1 the one that begins an item without
+// ending it (the last); KV_LAST: the piece ends its item.
+enum { KV_PART = 1, KV_LAST = 2 };
+
+// A warp's ring, in which its last piece lies too.
+template <int P, int NT, int U>
+__host__ __device__ constexpr int kv_ring_bytes() {
+  return kKvStages * U * P * kKvTileBytes > 8 * NT * (64 * P + 4) * 4 ? kKvStages * U * P * kKvTileBytes : 8 * NT * (64 * P + 4) * 4;
+}
+
+// A warp takes pieces of items, tile by tile through a ring of kKvStages steps of U tiles in shared memory, filled by bulk copies
+// (a tile is contiguous; its page is looked up when it is fetched).  Whole items are written at once; pieces of items that the CTA's
+// warps share are joined in shared memory, those that several CTAs share by kv_join_kernel.
+template <int P, int NT, int U>
+__global__ void __launch_bounds__(32 * kKvAttWarps, P * NT == 1 ? 5 : P * NT == 2 ? 3 : 2)
+kv_attention_kernel(const KvAttParams p) {
+  constexpr int kRows = 8 * NT, kCh = 64 * P, kPitch = kCh + 4, kStep = U * P * kKvTileBytes;
+  constexpr int kPiece = kRows * kPitch * 4, kRing = kv_ring_bytes<P, NT, U>();
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ __align__(8) uint64_t s_bar[kKvAttWarps * kKvStages];
+  __shared__ long long s_sum[kKvAttWarps];
+  __shared__ KvShare s_share[kKvAttWarps];
+  __shared__ int4 s_desc[kKvAttWarps][2];
+  __shared__ int s_t0[kKvAttWarps][2], s_live[kKvAttWarps][2];
+  __shared__ int s_abort;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const uint32_t bars = smem_u32(s_bar + warp * kKvStages);
+  uint8_t* ring = smem + warp * (kRing + kPiece);
+  volatile int* abort_flag = &s_abort;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kKvAttWarps * kKvStages; ++i) mbar_init(smem_u32(s_bar + i), 1);
+    s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (threadIdx.x < 2 * kKvAttWarps) s_desc[threadIdx.x >> 1][threadIdx.x & 1] = make_int4(0, 0, 0, 0);
+  pdl_begin();
+  __syncthreads();
+  const int tpp = p.kv.page_tokens / kKvTile;
+  KvShare share;
+  if (p.split) {
+    kv_share<NT, U>(p, s_sum, s_share);
+    share = s_share[warp];
+  } else {   // the CTA's item in four
+    const int n = kv_count(p.kv_len[blockIdx.z], p.max_kv) - kKvItemCost;
+    share = {(long long)(n * warp / kKvAttWarps), (long long)(n * (warp + 1) / kKvAttWarps), 0, (int)blockIdx.z};
+  }
+  uint32_t n_filled = 0, n_used = 0;   // steps of this warp's ring, over all pieces
+  while (share.at < share.end) {
+    // ---- the piece: tiles tile0 .. tile1 of an item of n_tiles
+    KvItem it;
+    int tile0, tile1, n_tiles;
+    if (p.split) {
+      long long c = kv_cost(p, share.req, kRows);
+      while (share.at >= share.base + c) {
+        share.base += c;
+        c = kv_cost(p, ++share.req, kRows);
+      }
+      const int count = kv_count(p.kv_len[share.req], p.max_kv);
+      const long long in = share.at - share.base;
+      const int item = (int)(in / count), from = (int)(in - (long long)item * count), to = (int)min((long long)count, from + (share.end - share.at));
+      share.at += to - from;
+      if (to <= kKvItemCost) continue;   // only the beginning: left to the next warp
+      n_tiles = count - kKvItemCost;
+      tile0 = max(0, from - kKvItemCost);
+      tile1 = to - kKvItemCost;
+      const int block = item / p.kv.H;
+      it = kv_item(p, share.req, item - block * p.kv.H, block * kRows);
+    } else {
+      it = kv_item(p, blockIdx.z, blockIdx.y, blockIdx.x * kRows);
+      n_tiles = kv_count(p.kv_len[blockIdx.z], p.max_kv) - kKvItemCost;
+      tile0 = (int)share.at;
+      tile1 = (int)share.end;
+      share.at = share.end;
+    }
+    const int n_rows = it.q_len * p.G;
+    if (it.row0 >= n_rows) break;   // (an item of its own CTA that is not there)
+    KvQuery<P, NT> q;
+    kv_load_query<P, NT>(p, it, lane, q);
+    KvState<P, NT> st;
+    st.fresh = (1u << (2 * NT)) - 1;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      st.m[n] = st.l[n] = 0;
+#pragma unroll
+      for (int pl = 0; pl < P; ++pl) {
+        st.z[pl][n] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) st.o[n][pl][j][0] = st.o[n][pl][j][1] = 0;
+      }
+    }
+    // keys that the last row of the block sees
+    const int see = max(0, min(it.kv_len, it.kv_len - it.q_len + kv_div_g(p, min(it.row0 + kRows - 1, n_rows - 1)) + 1));
+    const int stop = min(tile1, (see + kKvTile - 1) / kKvTile);
+    const int n_steps = stop <= tile0 ? 0 : (stop - tile0 + U - 1) / U;
+    uint32_t have = 0;             // tiles of the steps in flight, eight bits each, the next step's lowest
+    auto fill = [&](int i) {       // step i of the piece into the ring; lane u sees to tile u
+      const int tile = tile0 + U * i + lane;
+      int page = -1;
+      if (lane < U && tile < stop) page = __ldg(it.table + tile / tpp);
+      const bool ok = page >= 0 && page < p.kv.n_pages;
+      const uint32_t there = __ballot_sync(0xffffffffu, ok);
+      const uint32_t stage = n_filled % kKvStages;
+      if (lane == 0) mbar_expect_tx(bars + 8 * stage, (uint32_t)__popc(there) * (P * kKvTileBytes));
+      __syncwarp();
+      if (ok) bulk_load_1d(smem_u32(ring + stage * kStep + lane * P * kKvTileBytes), p.kv.pages + p.kv.tile_at(page, it.head, tile % tpp), P * kKvTileBytes, bars + 8 * stage);
+      have |= there << (8 * (n_filled - n_used));
+      ++n_filled;
+    };
+#pragma unroll 1
+    for (int i = 0; i < kKvStages - 1 && i < n_steps; ++i) fill(i);
+#pragma unroll 1
+    for (int i = 0; i < n_steps; ++i) {
+      __syncwarp();   // (the stage that is filled now was last read a step ago, by this warp)
+      if (i + kKvStages - 1 < n_steps) fill(i + kKvStages - 1);
+      const uint32_t stage = n_used % kKvStages;
+      if (!mbar_wait_warp(bars + 8 * stage, (n_used / kKvStages) & 1u, abort_flag, p.status, 51)) break;
+      const int key0 = (tile0 + U * i) * kKvTile;
+      const uint32_t there = have & 0xFFu;
+      have >>= 8;
+      ++n_used;
+      if (there == (1u << U) - 1 && key0 + U * kKvTile <= q.all) kv_step<true, P, NT, U>(ring + stage * kStep, there, key0, it.kv_len, q, lane, st);
+      else kv_step<false, P, NT, U>(ring + stage * kStep, there, key0, it.kv_len, q, lane, st);
+    }
+    // ---- the rows to shared memory: the ring is idle, a piece to be joined with the warp before has its own place
+    __syncwarp();
+    const bool inside = tile0 > 0, whole = !inside && tile1 == n_tiles;
+    float* rows = reinterpret_cast<float*>(ring + (inside ? kRing : 0));
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float l[2], m[2], z[P][2];
+      unpair_f32(st.l[n], l[0], l[1]);
+      unpair_f32(st.m[n], m[0], m[1]);
+#pragma unroll
+      for (int pl = 0; pl < P; ++pl) unpair_f32(st.z[pl][n], z[pl][0], z[pl][1]);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float* row = rows + (8 * n + 2 * t + c) * kPitch;
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          l[c] += __shfl_xor_sync(0xffffffffu, l[c], o);
+#pragma unroll
+          for (int pl = 0; pl < P; ++pl) z[pl][c] += __shfl_xor_sync(0xffffffffu, z[pl][c], o);
+        }
+        if (g == 0) *reinterpret_cast<float2*>(row + kCh) = make_float2((st.fresh >> (2 * n + c) & 1u) ? -FLT_MAX : -m[c], l[c]);
+#pragma unroll
+        for (int pl = 0; pl < P; ++pl)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float x[2], y[2];
+            unpair_f32(st.o[n][pl][j][0], x[0], x[1]);
+            unpair_f32(st.o[n][pl][j][1], y[0], y[1]);
+            row[64 * pl + 16 * j + g] = fmaf(x[c], 0x1p24f, z[pl][c]);
+            row[64 * pl + 16 * j + 8 + g] = fmaf(y[c], 0x1p20f, z[pl][c]);
+          }
+      }
+    }
+    __syncwarp();
+    if (whole) {
+#pragma unroll 1
+      for (int i = lane; i < kRows * kCh / 4; i += 32) {
+        const int row = i / (kCh / 4), ch = 4 * (i % (kCh / 4)), r = it.row0 + row;
+        if (r >= n_rows) break;
+        KvSum sum = {0.f, rows[row * kPitch + kCh + 1], *reinterpret_cast<const float4*>(rows + row * kPitch + ch)};
+        *reinterpret_cast<uint2*>(kv_out(p, it.t0, it.head, r, ch, kCh)) = sum.result();
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the copies of the next piece come behind these accesses
+      __syncwarp();
+    } else if (lane == 0) {
+      s_desc[warp][inside ? 0 : 1] = make_int4(it.req, it.head, it.row0, KV_PART | (tile1 == n_tiles ? KV_LAST : 0));
+      s_t0[warp][inside ? 0 : 1] = it.t0;
+      s_live[warp][inside ? 0 : 1] = n_rows - it.row0;
+    }
+  }
+  __syncthreads();
+  // ---- pieces of the CTA's warps, in order, a thread for four channels of a row
+  float* part = p.part + (size_t)blockIdx.x * 2 * kRows * kPitch;
+  int4 left[2] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
+#pragma unroll 1
+  for (int i = threadIdx.x; i < kRows * kCh / 4; i += 32 * kKvAttWarps) {
+    const int row = i / (kCh / 4), ch = 4 * (i % (kCh / 4));
+    KvSum sum = {0.f, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    int4 d = make_int4(0, 0, 0, 0);
+    bool open = false, outside = false;   // the item began in a CTA before
+    auto leave = [&](int slot, int flags) {
+      float* dst = part + (slot * kRows + row) * kPitch;
+      *reinterpret_cast<float4*>(dst + ch) = sum.v;
+      if (ch == 0) *reinterpret_cast<float2*>(dst + kCh) = make_float2(sum.m, sum.l);
+      if (slot == 0) left[0] = make_int4(d.x, d.y, d.z, flags);
+      else left[1] = make_int4(d.x, d.y, d.z, flags);
+    };
+#pragma unroll 1
+    for (int k = 0; k < 2 * kKvAttWarps; ++k) {
+      const int4 e = s_desc[k >> 1][k & 1];
+      if (!(e.w & KV_PART)) continue;
+      const float* src = reinterpret_cast<const float*>(smem + (k >> 1) * (kRing + kPiece) + ((k & 1) ? 0 : kRing)) + row * kPitch;
+      const float2 ml = *reinterpret_cast<const float2*>(src + kCh);
+      const float4 v = *reinterpret_cast<const float4*>(src + ch);
+      if (!open) {
+        sum = {ml.x, ml.y, v};
+        outside = (k & 1) == 0;
+        d = e;
+        open = true;
+      } else {
+        sum.add(ml.x, ml.y, v);
+      }
+      if (e.w & KV_LAST) {
+        open = false;
+        if (outside) leave(0, KV_PART | KV_LAST);
+        else if (row < s_live[k >> 1][k & 1])
+          *reinterpret_cast<uint2*>(kv_out(p, s_t0[k >> 1][k & 1], d.y, d.z + row, ch, kCh)) = sum.result();
+      }
+    }
+    if (open) leave(outside ? 0 : 1, KV_PART);
+  }
+  if (p.split && threadIdx.x == 0) {
+    p.desc[blockIdx.x * 2] = left[0];
+    p.desc[blockIdx.x * 2 + 1] = left[1];
+  }
+  if (*abort_flag) {   // copies may be in flight
+    const unsigned long long t0 = global_ns();
+    while (global_ns() - t0 < 2000000ull) __nanosleep(1000);
+  }
+}
+
+// Items that several CTAs share: CTA (w, y) looks at the piece of CTA w that begins an item without ending it, and adds up, for
+// two of its rows, this piece and those of the CTAs behind, which begin with the rest of the item (slot 0).
+constexpr int kKvJoinThreads = 256;
 template <int P, int NT>
-static cudaError_t kv_att_launch(const KvAttParams& p, cudaStream_t s) {
-  const size_t smem = (size_t)kKvAttWarps * 8 * NT * (64 * P + 4 + 4) * sizeof(float);
-  const dim3 grid((unsigned)(((long long)p.max_q * p.G + 8 * NT - 1) / (8 * NT)), (unsigned)p.kv.H, (unsigned)p.R);
-  return launch_pdl(kv_attention_kernel<P, NT>, grid, 32 * kKvAttWarps, smem, s, p);
+__global__ void __launch_bounds__(kKvJoinThreads)
+kv_join_kernel(const KvAttParams p, int workers) {
+  constexpr int kRows = 8 * NT, kCh = 64 * P, kPitch = kCh + 4, kWide = 2 * kCh / 4, kSets = kKvJoinThreads / kWide;
+  __shared__ float4 s_acc[kSets][kWide];
+  __shared__ float2 s_ml[kSets][2];
+  __shared__ int s_last;
+  pdl_begin();
+  const int w0 = blockIdx.x;
+  const int4 d = p.desc[w0 * 2 + 1];
+  if (!(d.w & KV_PART)) return;
+  if (threadIdx.x == 0) s_last = INT_MAX;
+  __syncthreads();
+  for (int w = w0 + 1; w < workers; w += kKvJoinThreads) {   // the CTA that ends the item
+    const int at = w + threadIdx.x;
+    if (at < workers && (p.desc[at * 2].w & KV_LAST)) atomicMin(&s_last, at);
+    __syncthreads();
+    if (s_last != INT_MAX) break;
+  }
+  const KvItem it = kv_item(p, d.x, d.y, d.z);
+  const int set = threadIdx.x / kWide, e = threadIdx.x % kWide;
+  const int row = blockIdx.y * 2 + e / (kCh / 4), ch = 4 * (e % (kCh / 4));
+  const int r = it.row0 + row;
+  const int n = min(s_last, workers - 1) - w0 + 1;   // pieces
+  KvSum sum = {-FLT_MAX, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+  // (each set of threads takes a run of pieces: the order of the sums is that of the tokens)
+  const int i0 = n * set / kSets, i1 = n * (set + 1) / kSets;
+#pragma unroll 4
+  for (int i = i0; i < i1; ++i) {
+    const float* part = p.part + ((size_t)(w0 + i) * 2 + (i == 0 ? 1 : 0)) * kRows * kPitch + row * kPitch;
+    const float2 ml = *reinterpret_cast<const float2*>(part + kCh);
+    sum.add(ml.x, ml.y, *reinterpret_cast<const float4*>(part + ch));
+  }
+  s_acc[set][e] = sum.v;
+  if (ch == 0) s_ml[set][e / (kCh / 4)] = make_float2(sum.m, sum.l);
+  __syncthreads();
+  if (set != 0 || r >= it.q_len * p.G) return;
+  for (int i = 1; i < kSets; ++i) sum.add(s_ml[i][e / (kCh / 4)].x, s_ml[i][e / (kCh / 4)].y, s_acc[i][e]);
+  *reinterpret_cast<uint2*>(kv_out(p, it.t0, it.head, r, ch, kCh)) = sum.result();
+}
+
+template <int P, int NT, int U>
+constexpr size_t kv_att_smem() {
+  return (size_t)kKvAttWarps * (kv_ring_bytes<P, NT, U>() + 8 * NT * (64 * P + 4) * sizeof(float));
+}
+static size_t kv_part_bytes(int planes, int nt) { return (size_t)kKvMaxWorkers * 2 * 8 * nt * (64 * planes + 4) * sizeof(float); }
+
+template <int P, int NT, int U>
+static moin_status kv_att_launch(HostState* hs, int optin, KvAttParams& p, cudaStream_t s) {
+  const size_t smem = kv_att_smem<P, NT, U>();
+  cudaError_t e = ensure_smem_optin(optin, kv_attention_kernel<P, NT, U>, smem);
+  if (e != cudaSuccess) return record_cuda(e);
+  const long long blocks = ((long long)p.max_q * p.G + 8 * NT - 1) / (8 * NT);
+  p.split = p.max_kv > 256;
+  ProfScope prof(MOIN_K_KV_ATTENTION, p.split ? 2 : 1, s);
+  if (!p.split)
+    return record_cuda(launch_pdl(kv_attention_kernel<P, NT, U>, dim3((unsigned)blocks, (unsigned)p.kv.H, (unsigned)p.R), 32 * kKvAttWarps, smem, s, p));
+  static int per_sm = 0;   // (the same on every device this library runs on)
+  if (per_sm == 0) {
+    int n = 0;
+    if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kv_attention_kernel<P, NT, U>, 32 * kKvAttWarps, smem)) != cudaSuccess) return record_cuda(e);
+    per_sm = n < 1 ? 1 : n;
+  }
+  // no more CTAs than there can be shares
+  const long long most = ((p.max_kv + kKvTile - 1) / kKvTile + kKvItemCost) * blocks * p.kv.H * p.R / (kKvAttWarps * (kKvItemCost + 2 * U)) + 1;
+  long long workers = (long long)per_sm * hs->n_sms;
+  if (workers > kKvMaxWorkers) workers = kKvMaxWorkers;
+  if (workers > most) workers = most;
+  e = launch_pdl(kv_attention_kernel<P, NT, U>, (unsigned)workers, 32 * kKvAttWarps, smem, s, p);
+  if (e == cudaSuccess) e = launch_pdl(kv_join_kernel<P, NT>, dim3((unsigned)workers, 4 * NT), kKvJoinThreads, 0, s, p, (int)workers);
+  return record_cuda(e);
 }
 
 __global__ void __launch_bounds__(256)
@@ -441,9 +781,13 @@ extern "C" moin_status moin_rope_table(float* table, int32_t n_pos, int32_t head
   return record_cuda(launch_pdl(kv_rope_kernel, (unsigned)((n + 255) / 256), 256, 0, (cudaStream_t)stream, (float2*)table, n_pos, head_dim / 2, (double)base));
 }
 
-extern "C" size_t moin_kv_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
-  (void)n_heads; (void)n_kv_heads; (void)head_dim;
-  return 256;
+// Row blocks of 8 NT rows: as many as a request has, up to what the registers hold.
+static int kv_nt(long long tall) { return tall <= 8 ? 1 : 2; }
+
+extern "C" size_t moin_kv_attention_workspace_bytes(int32_t max_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
+  if (max_q < 1 || n_kv_heads < 1 || n_heads < n_kv_heads || (head_dim != 64 && head_dim != 128)) return 256;
+  const int planes = head_dim / 64, nt = kv_nt((long long)max_q * (n_heads / n_kv_heads));
+  return kv_part_bytes(planes, nt) + (size_t)kKvMaxWorkers * 2 * sizeof(int4);
 }
 
 extern "C" moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables* tables, const int32_t* rows, const int32_t* cu_q,
@@ -464,8 +808,9 @@ extern "C" moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables
   if (rope && rope_len < max_kv) return MOIN_ERR_BAD_SHAPE;
   if (!kv_stride_ok(q_stride, n_heads, kv->head_dim) || !kv_stride_ok(out_stride, n_heads, kv->head_dim)) return MOIN_ERR_BAD_SHAPE;
   if (!aligned16(q) || !aligned16(out) || (rope && !aligned16(rope))) return MOIN_ERR_MISALIGNED;
-  if (R > 65535 || (long long)max_q * n_heads > 0x7FFFFFFFll) return MOIN_ERR_BAD_SHAPE;
-  if (!workspace || !aligned16(workspace) || workspace_bytes < moin_kv_attention_workspace_bytes(n_heads, kv->n_kv_heads, kv->head_dim))
+  const long long group = n_heads / kv->n_kv_heads;
+  if (R > 65535 || max_q * group * group > 0xFFFFFFFFll) return MOIN_ERR_BAD_SHAPE;
+  if (!workspace || !aligned16(workspace) || workspace_bytes < moin_kv_attention_workspace_bytes(max_q, n_heads, kv->n_kv_heads, kv->head_dim))
     return MOIN_ERR_WORKSPACE;
   HostState* hs;
   if ((st = host_state(&hs))) return st;
@@ -476,10 +821,11 @@ extern "C" moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables
   p.rope = (const float2*)rope;
   p.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t s = (cudaStream_t)stream;
-  const long long tall = (long long)max_q * p.G;
-  ProfScope prof(MOIN_K_KV_ATTENTION, 1, s);
-  cudaError_t e;
-  if (p.kv.planes == 1) e = tall <= 8 ? kv_att_launch<1, 1>(p, s) : tall <= 16 ? kv_att_launch<1, 2>(p, s) : kv_att_launch<1, 4>(p, s);
-  else e = tall <= 8 ? kv_att_launch<2, 1>(p, s) : kv_att_launch<2, 2>(p, s);
-  return record_cuda(e);
+  p.status = hs->status;
+  const int nt = kv_nt((long long)max_q * p.G);
+  p.inv_g = (uint32_t)((0x100000000ull + p.G - 1) / p.G);   // exact while row * G < 2^32
+  p.part = (float*)workspace;
+  p.desc = (int4*)((char*)workspace + kv_part_bytes(p.kv.planes, nt));
+  if (p.kv.planes == 2) return nt == 1 ? kv_att_launch<2, 1, 2>(hs, OPTIN_KV_ATTENTION, p, s) : kv_att_launch<2, 2, 1>(hs, OPTIN_KV_ATTENTION + 1, p, s);
+  return nt == 1 ? kv_att_launch<1, 1, 2>(hs, OPTIN_KV_ATTENTION + 2, p, s) : kv_att_launch<1, 2, 2>(hs, OPTIN_KV_ATTENTION + 3, p, s);
 }
