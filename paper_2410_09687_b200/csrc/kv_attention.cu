@@ -38,6 +38,8 @@ struct KvAttParams {
   int n_rows, max_pages;
   int R, T, max_q, max_kv, G, n_heads;
   uint32_t inv_g;          // row / G = row inv_g >> 32
+  uint32_t page_bytes;     // of all heads
+  int tpp_log2;            // tiles of a page
   const __nv_bfloat16* q;
   __nv_bfloat16* out;
   long long q_stride, out_stride;
@@ -46,7 +48,6 @@ struct KvAttParams {
   int split;               // items are cut: CTAs take equal shares of all tiles (else a CTA takes an item)
   float* part;             // [worker][2][row][64 P + 4]: sums of items that several workers share
   int4* desc;              // [worker][2]: what they belong to
-  DeviceStatus* status;
 };
 
 __device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -192,6 +193,12 @@ __device__ __forceinline__ void kv_load_query(const KvAttParams& p, const KvItem
   q.all = min(q.all, __shfl_xor_sync(0xffffffffu, q.all, 2));
 }
 
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ uint64_t twice_f32(float v) { return pair_f32(v, v); }
 
 // U tiles of 16 tokens from shared memory, the first at key0; bit u of `there`: tile u is part of the warp's work.  `whole`: every
@@ -463,34 +470,26 @@ __host__ __device__ constexpr int kv_ring_bytes() {
   return kKvStages * U * P * kKvTileBytes > 8 * NT * (64 * P + 4) * 4 ? kKvStages * U * P * kKvTileBytes : 8 * NT * (64 * P + 4) * 4;
 }
 
-// A warp takes pieces of items, tile by tile through a ring of kKvStages steps of U tiles in shared memory, filled by bulk copies
-// (a tile is contiguous; its page is looked up when it is fetched).  Whole items are written at once; pieces of items that the CTA's
+// A warp takes pieces of items, tile by tile through a ring of kKvStages steps of U tiles in shared memory, filled by its own
+// asynchronous copies of 16 bytes a lane.  Whole items are written at once; pieces of items that the CTA's
 // warps share are joined in shared memory, those that several CTAs share by kv_join_kernel.
 template <int P, int NT, int U>
-__global__ void __launch_bounds__(32 * kKvAttWarps, P * NT == 1 ? 5 : P * NT == 2 ? 3 : 2)
+__global__ void __launch_bounds__(32 * kKvAttWarps, P * NT == 1 ? 4 : P * NT == 2 ? 3 : 2)
 kv_attention_kernel(const KvAttParams p) {
   constexpr int kRows = 8 * NT, kCh = 64 * P, kPitch = kCh + 4, kStep = U * P * kKvTileBytes;
   constexpr int kPiece = kRows * kPitch * 4, kRing = kv_ring_bytes<P, NT, U>();
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ __align__(8) uint64_t s_bar[kKvAttWarps * kKvStages];
   __shared__ long long s_sum[kKvAttWarps];
   __shared__ KvShare s_share[kKvAttWarps];
   __shared__ int4 s_desc[kKvAttWarps][2];
   __shared__ int s_t0[kKvAttWarps][2], s_live[kKvAttWarps][2];
-  __shared__ int s_abort;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const uint32_t bars = smem_u32(s_bar + warp * kKvStages);
   uint8_t* ring = smem + warp * (kRing + kPiece);
-  volatile int* abort_flag = &s_abort;
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < kKvAttWarps * kKvStages; ++i) mbar_init(smem_u32(s_bar + i), 1);
-    s_abort = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
+  const uint32_t ring_addr = smem_u32(ring);
   if (threadIdx.x < 2 * kKvAttWarps) s_desc[threadIdx.x >> 1][threadIdx.x & 1] = make_int4(0, 0, 0, 0);
   pdl_begin();
   __syncthreads();
-  const int tpp = p.kv.page_tokens / kKvTile;
+  const int tpp = 1 << p.tpp_log2;
   KvShare share;
   if (p.split) {
     kv_share<NT, U>(p, s_sum, s_share);
@@ -499,7 +498,6 @@ kv_attention_kernel(const KvAttParams p) {
     const int n = kv_count(p.kv_len[blockIdx.z], p.max_kv) - kKvItemCost;
     share = {(long long)(n * warp / kKvAttWarps), (long long)(n * (warp + 1) / kKvAttWarps), 0, (int)blockIdx.z};
   }
-  uint32_t n_filled = 0, n_used = 0;   // steps of this warp's ring, over all pieces
   while (share.at < share.end) {
     // ---- the piece: tiles tile0 .. tile1 of an item of n_tiles
     KvItem it;
@@ -547,34 +545,63 @@ kv_attention_kernel(const KvAttParams p) {
     const int see = max(0, min(it.kv_len, it.kv_len - it.q_len + kv_div_g(p, min(it.row0 + kRows - 1, n_rows - 1)) + 1));
     const int stop = min(tile1, (see + kKvTile - 1) / kKvTile);
     const int n_steps = stop <= tile0 ? 0 : (stop - tile0 + U - 1) / U;
-    uint32_t have = 0;             // tiles of the steps in flight, eight bits each, the next step's lowest
-    auto fill = [&](int i) {       // step i of the piece into the ring; lane u sees to tile u
-      const int tile = tile0 + U * i + lane;
-      int page = -1;
-      if (lane < U && tile < stop) page = __ldg(it.table + tile / tpp);
-      const bool ok = page >= 0 && page < p.kv.n_pages;
-      const uint32_t there = __ballot_sync(0xffffffffu, ok);
-      const uint32_t stage = n_filled % kKvStages;
-      if (lane == 0) mbar_expect_tx(bars + 8 * stage, (uint32_t)__popc(there) * (P * kKvTileBytes));
-      __syncwarp();
-      if (ok) bulk_load_1d(smem_u32(ring + stage * kStep + lane * P * kKvTileBytes), p.kv.pages + p.kv.tile_at(page, it.head, tile % tpp), P * kKvTileBytes, bars + 8 * stage);
-      have |= there << (8 * (n_filled - n_used));
-      ++n_filled;
+    // pages of 32 tiles at a time, a lane each, and of the 32 behind them
+    auto pages_of = [&](int w) -> int {
+      const int tile = 32 * w + lane;
+      return tile < stop ? __ldg(it.table + (tile >> p.tpp_log2)) : -1;
+    };
+    int window = tile0 >> 5;
+    int pages = 0, pages_next = 0;
+    if (n_steps > 0) {
+      pages = pages_of(window);
+      pages_next = pages_of(window + 1);
+    }
+    const uint8_t* heads = p.kv.pages + (size_t)it.head * tpp * (P * kKvTileBytes) + 16 * lane;
+    uint32_t have = 0;             // tiles of the steps in flight, four bits each, the next step's lowest
+    uint32_t fill_at = ring_addr + 16 * lane, use_at = 0;
+    auto fill = [&](int i) {       // step i of the piece into the ring
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int tile = tile0 + U * i + u;
+        if ((tile >> 5) != window) {
+          ++window;
+          pages = pages_next;
+          pages_next = pages_of(window + 1);
+        }
+        const int page = __shfl_sync(0xffffffffu, pages, tile & 31);
+        if (page >= 0 && page < p.kv.n_pages) {   // (the same for the whole warp; -1 behind the piece)
+          const uint8_t* src = heads + (size_t)(uint32_t)page * p.page_bytes + (tile & (tpp - 1)) * (P * kKvTileBytes);
+#pragma unroll
+          for (int pl = 0; pl < P; ++pl) {
+            cp_async_16(fill_at + (u * P + pl) * kKvTileBytes, src + pl * kKvTileBytes);
+            cp_async_16(fill_at + (u * P + pl) * kKvTileBytes + 512, src + pl * kKvTileBytes + 512);
+            if (lane < 8) cp_async_16(fill_at + (u * P + pl) * kKvTileBytes + kKvPairs, src + pl * kKvTileBytes + kKvPairs);
+          }
+          have |= 1u << (4 * (kKvStages - 1) + u);
+        }
+      }
+      fill_at += kStep;
+      if (fill_at == ring_addr + 16 * lane + kKvStages * kStep) fill_at = ring_addr + 16 * lane;
     };
 #pragma unroll 1
-    for (int i = 0; i < kKvStages - 1 && i < n_steps; ++i) fill(i);
+    for (int i = 0; i < kKvStages - 1; ++i) {
+      have >>= 4;
+      if (i < n_steps) fill(i);
+      cp_async_commit();
+    }
 #pragma unroll 1
     for (int i = 0; i < n_steps; ++i) {
-      __syncwarp();   // (the stage that is filled now was last read a step ago, by this warp)
+      have >>= 4;
+      cp_async_wait<kKvStages - 2>();
+      __syncwarp();   // this step's tiles are there for every lane; the stage filled now was read a step ago
       if (i + kKvStages - 1 < n_steps) fill(i + kKvStages - 1);
-      const uint32_t stage = n_used % kKvStages;
-      if (!mbar_wait_warp(bars + 8 * stage, (n_used / kKvStages) & 1u, abort_flag, p.status, 51)) break;
+      cp_async_commit();
       const int key0 = (tile0 + U * i) * kKvTile;
-      const uint32_t there = have & 0xFFu;
-      have >>= 8;
-      ++n_used;
-      if (there == (1u << U) - 1 && key0 + U * kKvTile <= q.all) kv_step<true, P, NT, U>(ring + stage * kStep, there, key0, it.kv_len, q, lane, st);
-      else kv_step<false, P, NT, U>(ring + stage * kStep, there, key0, it.kv_len, q, lane, st);
+      const uint32_t there = have & ((1u << U) - 1);
+      if (there == (1u << U) - 1 && key0 + U * kKvTile <= q.all) kv_step<true, P, NT, U>(ring + use_at, there, key0, it.kv_len, q, lane, st);
+      else kv_step<false, P, NT, U>(ring + use_at, there, key0, it.kv_len, q, lane, st);
+      use_at += kStep;
+      if (use_at == kKvStages * kStep) use_at = 0;
     }
     // ---- the rows to shared memory: the ring is idle, a piece to be joined with the warp before has its own place
     __syncwarp();
@@ -618,8 +645,7 @@ kv_attention_kernel(const KvAttParams p) {
         KvSum sum = {0.f, rows[row * kPitch + kCh + 1], *reinterpret_cast<const float4*>(rows + row * kPitch + ch)};
         *reinterpret_cast<uint2*>(kv_out(p, it.t0, it.head, r, ch, kCh)) = sum.result();
       }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the copies of the next piece come behind these accesses
-      __syncwarp();
+      __syncwarp();   // (the ring is filled again)
     } else if (lane == 0) {
       s_desc[warp][inside ? 0 : 1] = make_int4(it.req, it.head, it.row0, KV_PART | (tile1 == n_tiles ? KV_LAST : 0));
       s_t0[warp][inside ? 0 : 1] = it.t0;
@@ -670,10 +696,6 @@ kv_attention_kernel(const KvAttParams p) {
   if (p.split && threadIdx.x == 0) {
     p.desc[blockIdx.x * 2] = left[0];
     p.desc[blockIdx.x * 2 + 1] = left[1];
-  }
-  if (*abort_flag) {   // copies may be in flight
-    const unsigned long long t0 = global_ns();
-    while (global_ns() - t0 < 2000000ull) __nanosleep(1000);
   }
 }
 
@@ -821,7 +843,8 @@ extern "C" moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables
   p.rope = (const float2*)rope;
   p.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t s = (cudaStream_t)stream;
-  p.status = hs->status;
+  p.page_bytes = (uint32_t)p.kv.tile_at(1, 0, 0);
+  p.tpp_log2 = kv->page_tokens == 16 ? 0 : kv->page_tokens == 32 ? 1 : kv->page_tokens == 64 ? 2 : 3;
   const int nt = kv_nt((long long)max_q * p.G);
   p.inv_g = (uint32_t)((0x100000000ull + p.G - 1) / p.G);   // exact while row * G < 2^32
   p.part = (float*)workspace;
