@@ -48,7 +48,7 @@ inline moin_status kv_view(const moin_kv* kv, KvView* out) {
   if (!kv || !kv->pages || kv->n_pages < 1 || kv->n_kv_heads < 1) return MOIN_ERR_INVALID_ARG;
   if (kv->head_dim != 64 && kv->head_dim != 128) return MOIN_ERR_BAD_SHAPE;
   if (kv->page_tokens != 16 && kv->page_tokens != 32 && kv->page_tokens != 64 && kv->page_tokens != 128) return MOIN_ERR_BAD_SHAPE;
-  if (kv->n_kv_heads > 65535 || (long long)kv->n_pages * kv->page_tokens > 0x7FFFFFFFll) return MOIN_ERR_BAD_SHAPE;   // slots are 32-bit
+  if (kv->n_kv_heads > 16384 || (long long)kv->n_pages * kv->page_tokens > 0x7FFFFFFFll) return MOIN_ERR_BAD_SHAPE;   // slots are 32-bit
   if (!aligned16(kv->pages)) return MOIN_ERR_MISALIGNED;
   *out = {reinterpret_cast<uint8_t*>(kv->pages), kv->n_pages, kv->page_tokens, kv->n_kv_heads, kv->head_dim / 64};
   return MOIN_OK;

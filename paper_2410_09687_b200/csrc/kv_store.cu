@@ -1,5 +1,6 @@
 // The 4-bit key/value cache: rows stored by slot (rotated, quantised) and read back.  Layout: kv.cuh.
 #include "kv.cuh"
+#include "ptx.cuh"
 
 namespace moin {
 
@@ -38,191 +39,219 @@ __device__ __forceinline__ KvGroup kv_group(const KvStoreParams& p, int t0, int 
   return g;
 }
 
-// 64 channels of a row, 16 to a lane: x[4 j + 2 half + c] = channel 16 j + 8 half + 2 t + c.
-__device__ __forceinline__ void kv_load_row(const __nv_bfloat16* row, int t, float (&x)[16]) {
+// 64 channels of a row, 16 to a lane, two to a word: x[2 j + h] = channels 16 j + 8 h + 2 t, + 1.
+__device__ __forceinline__ void kv_load_row(const __nv_bfloat16* row, int t, uint32_t (&x)[8]) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(row + 16 * j + 8 * h + 2 * t));
-      x[4 * j + 2 * h] = bf16_lo(w);
-      x[4 * j + 2 * h + 1] = bf16_hi(w);
-    }
+  for (int i = 0; i < 8; ++i) x[i] = __ldg(reinterpret_cast<const uint32_t*>(row + 8 * i + 2 * t));
+}
+__device__ __forceinline__ uint32_t min2_nan(uint32_t a, uint32_t b) {   // NaN if either is
+  uint32_t d;
+  asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
 }
 
-// Codes of a row, 16 to a lane: word j holds those of x[4 j ..] in nibbles 0, 1 (low half c = 0, high half c = 1).
-//   scale = bf16(max((max - min) / 15, |min| 2^-12, 2^-64)), zero = min, code = rint((x - zero) / scale) in 0 .. 15
+// Codes of the lane's channels of a row, added into w[j] at bit 8 s: nibbles 0, 1 are x[2 j], x[2 j + 1]; low half first channel.
+//   scale = bf16(max((max - min) / 15, |min| 2^-12, 2^-64)), zero = min, code = rint((x - zero) / scale)
 // Inputs are bf16, so the zero is exact, and rows that are not constant have a step above |min| 2^-12: the second term
 // gives constant rows a step that is not 0 and not out of proportion (attention divides by steps).  2^-64 bounds what
 // underflows: values that far below it are stored as their row's minimum.  A row with an element or a span that is not
 // finite is stored as NaN.
-__device__ __forceinline__ uint32_t kv_quantise(const float (&x)[16], uint32_t (&w)[4]) {
-  float lo = x[0], hi = x[0], bad = 0.f;
+// The quotient is rounded as a division rounds it, by Markstein's correction of a product with the correctly rounded reciprocal:
+// halves of a step are common among bf16 values, and go to the even code.  It is below 15.5 (the scale is at most 2^-8 of itself
+// too small), so nothing is clamped.  Adding 1.5 2^23 leaves the integer in the low bits; the rest of those words' bits
+// adds up to a constant.
+constexpr float kKvMagic = 12582912.f;
+__device__ __forceinline__ uint32_t kv_quantise(uint32_t (&x)[8], int s, uint32_t (&w)[4]) {
+  uint32_t mn = x[0], mx = x[0];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    lo = fminf(lo, x[i]);
-    hi = fmaxf(hi, x[i]);
-    bad = fmaf(x[i], 0.f, bad);   // NaN once an element is not finite
+  for (int i = 1; i < 8; ++i) {
+    mn = min2_nan(mn, x[i]);
+    mx = max2_nan(mx, x[i]);
   }
 #pragma unroll
   for (int o = 1; o < 4; o <<= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    bad += __shfl_xor_sync(0xffffffffu, bad, o);
+    mn = min2_nan(mn, __shfl_xor_sync(0xffffffffu, mn, o));
+    mx = max2_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
   }
-  const float span = hi - lo;
-  bad = fmaf(span, 0.f, bad);
-  const float scale = round_bf16(fmaxf(fmaxf(__fdiv_rn(span, 15.f), fabsf(lo) * 0x1p-12f), 0x1p-64f));
-  const bool ok = bad == 0.f;
+  mn = min2_nan(mn, __byte_perm(mn, mn, 0x1032));
+  mx = max2_nan(mx, __byte_perm(mx, mx, 0x1032));
+  float lo = bf16_lo(mn);
+  const float span = bf16_lo(mx) - lo;
+  const bool bad = !(span < INFINITY);
+  if (bad) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    w[j] = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int c = ok ? min(__float2int_rn(__fdiv_rn(x[4 * j + e] - lo, scale)), 15) : 0;
-      w[j] |= (uint32_t)c << (4 * (e >> 1) + 16 * (e & 1));
-    }
+    for (int i = 0; i < 8; ++i) x[i] = 0u;
+    lo = 0.f;
   }
-  return ok ? (__float_as_uint(scale) >> 16) | (__float_as_uint(lo) & 0xFFFF0000u) : 0x7FC07FC0u;
+  const float scale = bad ? 1.f : round_bf16(fmaxf(fmaxf(span / 15.f, fabsf(lo) * 0x1p-12f), 0x1p-64f));
+  const float inv = __frcp_rn(scale);
+  const uint64_t nlo2 = pair_f32(-lo, -lo), inv2 = pair_f32(inv, inv), nsc2 = pair_f32(-scale, -scale), magic2 = pair_f32(kKvMagic, kKvMagic);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint64_t d = add2(pair_f32(bf16_lo(x[i]), bf16_hi(x[i])), nlo2);
+    uint64_t q = mul2(d, inv2);
+    q = fma2(fma2(q, nsc2, d), inv2, q);
+    float a, b;
+    unpair_f32(add2(q, magic2), a, b);
+    const int sh = 8 * s + 4 * (i & 1);
+    w[i >> 1] += (__float_as_uint(a) << sh) + (__float_as_uint(b) << (sh + 16));
+  }
+  return bad ? 0x7FC07FC0u : (__float_as_uint(scale) >> 16) | (__float_as_uint(lo) & 0xFFFF0000u);
+}
+__host__ __device__ constexpr uint32_t kv_magic_sum() {
+  uint32_t sum = 0;
+  for (int sh = 0; sh < 32; sh += 4) sum += 0x4B400000u << sh;
+  return sum;
 }
 
-// A warp stores a group of one head and plane: its lanes load two token rows (g and g + 8 of the tile, 16 channels each),
-// quantise them and hold the tile's words.  Whole tiles are written by 16-byte stores, others byte by byte, a token's own
-// bytes only.
+__device__ __forceinline__ void kv_rotate_words(uint32_t& a, uint32_t& b, const float4& cs) {   // (cos, sin) of two channels
+  const float2 c0 = make_float2(cs.x, cs.y), c1 = make_float2(cs.z, cs.w);
+  const float a0 = bf16_lo(a), a1 = bf16_hi(a), b0 = bf16_lo(b), b1 = bf16_hi(b);
+  a = pack_bf16(kv_rot_lo(a0, b0, c0), kv_rot_lo(a1, b1, c1));
+  b = pack_bf16(kv_rot_hi(a0, b0, c0), kv_rot_hi(a1, b1, c1));
+}
+
+// A warp stores the keys or the values of a group, of one head and plane: its lanes load two token rows (g and g + 8 of the tile,
+// 16 channels each), quantise them and hold the tile's words.  Whole tiles are written by 16-byte stores, others byte by byte,
+// a token's own bytes only.
 template <int D>
 __global__ void __launch_bounds__(32 * kKvStoreWarps)
 kv_append_kernel(const KvStoreParams p) {
   pdl_begin();
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int hp = blockIdx.y * kKvStoreWarps + (threadIdx.x >> 5);
-  if (hp >= p.kv.H * (D / 64)) return;
-  const int head = hp / (D / 64), plane = hp % (D / 64);
+  const int unit = blockIdx.y * kKvStoreWarps + (threadIdx.x >> 5);
+  if (unit >= 2 * p.kv.H * (D / 64)) return;
+  const bool value = unit & 1;
+  const int hp = unit >> 1, head = hp / (D / 64), plane = hp % (D / 64);
+  const __nv_bfloat16* base = (value ? p.v : p.k) + head * D;
+  const long long stride = value ? p.v_stride : p.k_stride;
   const int first = blockIdx.x * p.window;
   uint32_t starts = __ballot_sync(0xffffffffu, lane < p.window && first + lane < p.T && kv_group_start(p, first + lane));
   while (starts) {
     const KvGroup gr = kv_group(p, first + __ffs(starts) - 1, lane);
     starts &= starts - 1;
-    uint32_t word[2][2][4], pair[2][2];   // [key, value][token g, g + 8]
+    uint32_t x[2][8], w[4] = {0u, 0u, 0u, 0u}, pair[2];
     bool live[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const int row = gr.t0 + g + 8 * s - gr.i0;
       live[s] = g + 8 * s >= gr.i0 && g + 8 * s < gr.i0 + gr.n;
-      float xk[16], xv[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) xk[i] = xv[i] = 0.f;
-      if (live[s]) {
-        const __nv_bfloat16* kr = p.k + (long long)row * p.k_stride + head * D;
-        kv_load_row(kr + 64 * plane, t, xk);
-        kv_load_row(p.v + (long long)row * p.v_stride + head * D + 64 * plane, t, xv);
-        if (p.rope != nullptr) {
-          const int at = p.pos[row];
-          live[s] = at >= 0 && at < p.rope_len;
-          const float2* cs = p.rope + (size_t)(live[s] ? at : 0) * (D / 2);
-          if (D == 64) {
+      for (int i = 0; i < 8; ++i) x[s][i] = 0u;
+      if (live[s]) kv_load_row(base + (gr.t0 + g + 8 * s - gr.i0) * stride + 64 * plane, t, x[s]);
+    }
+    if (p.rope != nullptr) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float2 c = __ldg(cs + 16 * (i >> 2) + 8 * ((i >> 1) & 1) + 2 * t + (i & 1));
-              const float a = xk[i], b = xk[i + 8];
-              xk[i] = round_bf16(kv_rot_lo(a, b, c));
-              xk[i + 8] = round_bf16(kv_rot_hi(a, b, c));
-            }
-          } else {
-            float other[16];
-            kv_load_row(kr + 64 * (1 - plane), t, other);
+      for (int s = 0; s < 2; ++s) {
+        if (!live[s]) continue;
+        const int row = gr.t0 + g + 8 * s - gr.i0, at = p.pos[row];
+        live[s] = at >= 0 && at < p.rope_len;   // (a value is not stored without its key)
+        if (value) continue;
+        const float* cs = reinterpret_cast<const float*>(p.rope + (size_t)(live[s] ? at : 0) * (D / 2) + 2 * t);
+        if (D == 64) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float2 c = __ldg(cs + 16 * (i >> 2) + 8 * ((i >> 1) & 1) + 2 * t + (i & 1));
-              xk[i] = round_bf16(plane == 0 ? kv_rot_lo(xk[i], other[i], c) : kv_rot_hi(other[i], xk[i], c));
-            }
+          for (int i = 0; i < 4; ++i) kv_rotate_words(x[s][i], x[s][i + 4], __ldg(reinterpret_cast<const float4*>(cs + 16 * i)));
+        } else {
+          uint32_t other[8];
+          kv_load_row(base + row * stride + 64 * (1 - plane), t, other);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float4 c = __ldg(reinterpret_cast<const float4*>(cs + 16 * i));
+            if (plane == 0) kv_rotate_words(x[s][i], other[i], c);
+            else kv_rotate_words(other[i], x[s][i], c);
           }
         }
       }
-      pair[0][s] = kv_quantise(xk, word[0][s]);
-      pair[1][s] = kv_quantise(xv, word[1][s]);
     }
-    uint32_t kw[4], vw[4];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) pair[s] = kv_quantise(x[s], s, w);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      kw[j] = word[0][0][j] | word[0][1][j] << 8;
-      vw[j] = movmatrix_trans(word[1][0][j] | word[1][1][j] << 8);
+      w[j] -= kv_magic_sum();
+      if (value) w[j] = movmatrix_trans(w[j]);
     }
     uint8_t* tile = p.kv.pages + p.kv.tile_at(gr.page, head, gr.tile) + plane * kKvTileBytes;
+    uint8_t* words = tile + (value ? 512 : 0) + 16 * lane;
+    uint32_t* pairs = reinterpret_cast<uint32_t*>(tile + kKvPairs) + 4 * g + (value ? 2 : 0);
     const uint32_t rows = __ballot_sync(0xffffffffu, live[0]), rows8 = __ballot_sync(0xffffffffu, live[1]);   // bit 4 g: token g
     if ((rows & rows8) == 0xffffffffu) {
-      reinterpret_cast<uint4*>(tile)[lane] = make_uint4(kw[0], kw[1], kw[2], kw[3]);
-      reinterpret_cast<uint4*>(tile + 512)[lane] = make_uint4(vw[0], vw[1], vw[2], vw[3]);
-      if (t == 0) reinterpret_cast<uint4*>(tile + kKvPairs)[g] = make_uint4(pair[0][0], pair[0][1], pair[1][0], pair[1][1]);
+      *reinterpret_cast<uint4*>(words) = make_uint4(w[0], w[1], w[2], w[3]);
+      if (t == 0) *reinterpret_cast<uint2*>(pairs) = make_uint2(pair[0], pair[1]);
       continue;
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      if (live[s]) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          tile[16 * lane + 4 * j + s] = (uint8_t)(kw[j] >> (8 * s));
-          tile[16 * lane + 4 * j + 2 + s] = (uint8_t)(kw[j] >> (16 + 8 * s));
-        }
-        if (t == 0) {
-          uint32_t* pr = reinterpret_cast<uint32_t*>(tile + kKvPairs) + 4 * g + s;
-          pr[0] = pair[0][s];
-          pr[2] = pair[1][s];
-        }
-      }
+      if (live[s] && t == 0) pairs[s] = pair[s];
       const uint32_t r = s == 0 ? rows : rows8;
 #pragma unroll
-      for (int c = 0; c < 2; ++c)      // value bytes: this lane's tokens 2 t + c (+ 8)
-        if (r >> (4 * (2 * t + c)) & 1u) {
+      for (int c = 0; c < 2; ++c)   // byte 2 c + s of a word: of keys token g + 8 s, of values token 2 t + c + 8 s
+        if (r >> (4 * (value ? 2 * t + c : g)) & 1u) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) tile[512 + 16 * lane + 4 * j + 2 * c + s] = (uint8_t)(vw[j] >> (16 * c + 8 * s));
+          for (int j = 0; j < 4; ++j) words[4 * j + 2 * c + s] = (uint8_t)(w[j] >> (16 * c + 8 * s));
         }
     }
   }
 }
 
-// The rows of a group back as bf16(zero + scale code); rows without a slot are zeros.
+// The rows of a group back as bf16(zero + scale code); rows without a slot are zeros.  A code becomes a bf16 by two operations on a
+// pair (128 + code by its bits, less 128), its value by one fused multiply-add.  A lane's words go through shared memory, so that
+// rows are written 16 bytes a lane (pitch 36 words: neither side meets a bank twice).
+constexpr int kKvReadPitch = 36;
 template <int D>
 __global__ void __launch_bounds__(32 * kKvStoreWarps)
 kv_read_kernel(const KvStoreParams p) {
+  __shared__ __align__(16) uint32_t s_rows[kKvStoreWarps][kKvTile * kKvReadPitch];
   pdl_begin();
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int hp = blockIdx.y * kKvStoreWarps + (threadIdx.x >> 5);
-  if (hp >= p.kv.H * (D / 64)) return;
-  const int head = hp / (D / 64), plane = hp % (D / 64);
+  const int unit = blockIdx.y * kKvStoreWarps + (threadIdx.x >> 5);
+  if (unit >= 2 * p.kv.H * (D / 64)) return;
+  const bool value = unit & 1;
+  const int hp = unit >> 1, head = hp / (D / 64), plane = hp % (D / 64);
+  __nv_bfloat16* base = (value ? p.v_out : p.k_out) + head * D + 64 * plane;
+  const long long stride = value ? p.v_stride : p.k_stride;
+  uint32_t* stage = s_rows[threadIdx.x >> 5];
   const int first = blockIdx.x * p.window;
   const bool mine = lane < p.window && first + lane < p.T;
   uint32_t none = __ballot_sync(0xffffffffu, mine && !kv_slot_ok(p, p.slot[mine ? first + lane : 0]));
-  for (; none; none &= none - 1) {
-    const int row = first + __ffs(none) - 1;
-    reinterpret_cast<uint32_t*>(p.k_out + (long long)row * p.k_stride + head * D + 64 * plane)[lane] = 0u;
-    reinterpret_cast<uint32_t*>(p.v_out + (long long)row * p.v_stride + head * D + 64 * plane)[lane] = 0u;
-  }
+  for (; none; none &= none - 1) reinterpret_cast<uint32_t*>(base + (first + __ffs(none) - 1) * stride)[lane] = 0u;
   uint32_t starts = __ballot_sync(0xffffffffu, mine && kv_group_start(p, mine ? first + lane : 0));
   while (starts) {
     const KvGroup gr = kv_group(p, first + __ffs(starts) - 1, lane);
     starts &= starts - 1;
     const uint8_t* tile = p.kv.pages + p.kv.tile_at(gr.page, head, gr.tile) + plane * kKvTileBytes;
-    const uint4 k4 = reinterpret_cast<const uint4*>(tile)[lane], v4 = reinterpret_cast<const uint4*>(tile + 512)[lane];
-    const uint4 pr = reinterpret_cast<const uint4*>(tile + kKvPairs)[g];
-    const uint32_t kw[4] = {k4.x, k4.y, k4.z, k4.w};
-    const uint32_t vw[4] = {movmatrix_trans(v4.x), movmatrix_trans(v4.y), movmatrix_trans(v4.z), movmatrix_trans(v4.w)};
-    const uint32_t pk[2] = {pr.x, pr.y}, pv[2] = {pr.z, pr.w};
+    const uint4 c4 = *reinterpret_cast<const uint4*>(tile + (value ? 512 : 0) + 16 * lane);
+    const uint2 pr = *reinterpret_cast<const uint2*>(tile + kKvPairs + 16 * g + (value ? 8 : 0));
+    uint32_t w[4] = {c4.x, c4.y, c4.z, c4.w};
+    if (value) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = movmatrix_trans(w[j]);
+    }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      if (g + 8 * s < gr.i0 || g + 8 * s >= gr.i0 + gr.n) continue;
-      const long long row = gr.t0 + g + 8 * s - gr.i0;
-      uint32_t* ko = reinterpret_cast<uint32_t*>(p.k_out + row * p.k_stride + head * D + 64 * plane) + t;
-      uint32_t* vo = reinterpret_cast<uint32_t*>(p.v_out + row * p.v_stride + head * D + 64 * plane) + t;
-      const float ks = kv_scale(pk[s]), kz = kv_zero(pk[s]), vs = kv_scale(pv[s]), vz = kv_zero(pv[s]);
+      const uint32_t pair = s == 0 ? pr.x : pr.y;
+      const uint32_t scale2 = __byte_perm(pair, pair, 0x1010), zero2 = __byte_perm(pair, pair, 0x3232);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int sh = 8 * s + 4 * h;
-          ko[8 * j + 4 * h] = pack_bf16(fmaf((float)(kw[j] >> sh & 15u), ks, kz), fmaf((float)(kw[j] >> (sh + 16) & 15u), ks, kz));
-          vo[8 * j + 4 * h] = pack_bf16(fmaf((float)(vw[j] >> sh & 15u), vs, vz), fmaf((float)(vw[j] >> (sh + 16) & 15u), vs, vz));
-        }
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t bits = (w[i >> 1] >> (8 * s + 4 * (i & 1)) & 0x000F000Fu) | 0x43004300u;
+        uint32_t c, v;
+        asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(c) : "r"(bits), "r"(0x43004300u));
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v) : "r"(c), "r"(scale2), "r"(zero2));
+        stage[(g + 8 * s) * kKvReadPitch + 4 * i + t] = v;
+      }
     }
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int row = 4 * k + (lane >> 3);
+      if (row >= gr.i0 && row < gr.i0 + gr.n)
+        *reinterpret_cast<uint4*>(base + (gr.t0 + row - gr.i0) * stride + 8 * (lane & 7)) =
+            *reinterpret_cast<const uint4*>(stage + row * kKvReadPitch + 4 * (lane & 7));
+    }
+    __syncwarp();
   }
 }
 
@@ -233,7 +262,7 @@ static int kv_window(int T) { return T <= 2048 ? 1 : 16; }
 template <class Fn>
 static moin_status kv_store_launch(Fn* fn64, Fn* fn128, KvStoreParams& p, int head_dim, cudaStream_t s) {
   p.window = kv_window(p.T);
-  const dim3 grid((unsigned)((p.T + p.window - 1) / p.window), (unsigned)((p.kv.H * p.kv.planes + kKvStoreWarps - 1) / kKvStoreWarps));
+  const dim3 grid((unsigned)((p.T + p.window - 1) / p.window), (unsigned)((2 * p.kv.H * p.kv.planes + kKvStoreWarps - 1) / kKvStoreWarps));
   ProfScope prof(MOIN_K_KV_STORE, 1, s);
   return record_cuda(launch_pdl(head_dim == 64 ? fn64 : fn128, grid, 32 * kKvStoreWarps, 0, s, p));
 }
