@@ -116,18 +116,22 @@ __device__ __forceinline__ void kv_rotate_words(uint32_t& a, uint32_t& b, const 
   b = pack_bf16(kv_rot_hi(a0, b0, c0), kv_rot_hi(a1, b1, c1));
 }
 
-// A warp stores the keys or the values of a group, of one head and plane: its lanes load two token rows (g and g + 8 of the tile,
-// 16 channels each), quantise them and hold the tile's words.  Whole tiles are written by 16-byte stores, others byte by byte,
-// a token's own bytes only.
-template <int D>
+// A warp stores the keys or the values of a group, of one head and NP planes of it: its lanes load two token rows (g and g + 8 of
+// the tile, 16 channels a plane each), quantise them and hold the tile's words.  Whole tiles are written by 16-byte stores, others
+// byte by byte, a token's own bytes only.
+// Bound by the instructions of rotation and quantisation (about 480 a warp and tile) for prompts, by the chain slot, position,
+// (cos, sin), row, store for single tokens: 21 thousand tokens of 8 heads of 128 take 71 us with a warp per plane (a key's
+// partner plane is loaded and rotated twice then) and TODO with both planes in a warp; one token is 0.9 us faster the other way.
+template <int D, int NP>
 __global__ void __launch_bounds__(32 * kKvStoreWarps)
 kv_append_kernel(const KvStoreParams p) {
+  constexpr int kPer = D / 64 / NP;   // warps of a head's keys
   pdl_begin();
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int unit = blockIdx.y * kKvStoreWarps + (threadIdx.x >> 5);
-  if (unit >= 2 * p.kv.H * (D / 64)) return;
+  if (unit >= 2 * p.kv.H * kPer) return;
   const bool value = unit & 1;
-  const int hp = unit >> 1, head = hp / (D / 64), plane = hp % (D / 64);
+  const int hp = unit >> 1, head = hp / kPer, plane0 = hp % kPer;
   const __nv_bfloat16* base = (value ? p.v : p.k) + head * D;
   const long long stride = value ? p.v_stride : p.k_stride;
   const int first = blockIdx.x * p.window;
@@ -135,14 +139,17 @@ kv_append_kernel(const KvStoreParams p) {
   while (starts) {
     const KvGroup gr = kv_group(p, first + __ffs(starts) - 1, lane);
     starts &= starts - 1;
-    uint32_t x[2][8], w[4] = {0u, 0u, 0u, 0u}, pair[2];
+    uint32_t x[NP][2][8];
     bool live[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       live[s] = g + 8 * s >= gr.i0 && g + 8 * s < gr.i0 + gr.n;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[s][i] = 0u;
-      if (live[s]) kv_load_row(base + (gr.t0 + g + 8 * s - gr.i0) * stride + 64 * plane, t, x[s]);
+      for (int pl = 0; pl < NP; ++pl) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[pl][s][i] = 0u;
+        if (live[s]) kv_load_row(base + (gr.t0 + g + 8 * s - gr.i0) * stride + 64 * (plane0 + pl), t, x[pl][s]);
+      }
     }
     if (p.rope != nullptr) {
 #pragma unroll
@@ -154,45 +161,52 @@ kv_append_kernel(const KvStoreParams p) {
         const float* cs = reinterpret_cast<const float*>(p.rope + (size_t)(live[s] ? at : 0) * (D / 2) + 2 * t);
         if (D == 64) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) kv_rotate_words(x[s][i], x[s][i + 4], __ldg(reinterpret_cast<const float4*>(cs + 16 * i)));
+          for (int i = 0; i < 4; ++i) kv_rotate_words(x[0][s][i], x[0][s][i + 4], __ldg(reinterpret_cast<const float4*>(cs + 16 * i)));
+        } else if (NP == 2) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) kv_rotate_words(x[0][s][i], x[NP - 1][s][i], __ldg(reinterpret_cast<const float4*>(cs + 16 * i)));
         } else {
           uint32_t other[8];
-          kv_load_row(base + row * stride + 64 * (1 - plane), t, other);
+          kv_load_row(base + row * stride + 64 * (1 - plane0), t, other);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const float4 c = __ldg(reinterpret_cast<const float4*>(cs + 16 * i));
-            if (plane == 0) kv_rotate_words(x[s][i], other[i], c);
-            else kv_rotate_words(other[i], x[s][i], c);
+            if (plane0 == 0) kv_rotate_words(x[0][s][i], other[i], c);
+            else kv_rotate_words(other[i], x[0][s][i], c);
           }
         }
       }
     }
-#pragma unroll
-    for (int s = 0; s < 2; ++s) pair[s] = kv_quantise(x[s], s, w);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      w[j] -= kv_magic_sum();
-      if (value) w[j] = movmatrix_trans(w[j]);
-    }
-    uint8_t* tile = p.kv.pages + p.kv.tile_at(gr.page, head, gr.tile) + plane * kKvTileBytes;
-    uint8_t* words = tile + (value ? 512 : 0) + 16 * lane;
-    uint32_t* pairs = reinterpret_cast<uint32_t*>(tile + kKvPairs) + 4 * g + (value ? 2 : 0);
     const uint32_t rows = __ballot_sync(0xffffffffu, live[0]), rows8 = __ballot_sync(0xffffffffu, live[1]);   // bit 4 g: token g
-    if ((rows & rows8) == 0xffffffffu) {
-      *reinterpret_cast<uint4*>(words) = make_uint4(w[0], w[1], w[2], w[3]);
-      if (t == 0) *reinterpret_cast<uint2*>(pairs) = make_uint2(pair[0], pair[1]);
-      continue;
-    }
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      if (live[s] && t == 0) pairs[s] = pair[s];
-      const uint32_t r = s == 0 ? rows : rows8;
+    for (int pl = 0; pl < NP; ++pl) {
+      uint32_t w[4] = {0u, 0u, 0u, 0u}, pair[2];
 #pragma unroll
-      for (int c = 0; c < 2; ++c)   // byte 2 c + s of a word: of keys token g + 8 s, of values token 2 t + c + 8 s
-        if (r >> (4 * (value ? 2 * t + c : g)) & 1u) {
+      for (int s = 0; s < 2; ++s) pair[s] = kv_quantise(x[pl][s], s, w);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) words[4 * j + 2 * c + s] = (uint8_t)(w[j] >> (16 * c + 8 * s));
-        }
+      for (int j = 0; j < 4; ++j) {
+        w[j] -= kv_magic_sum();
+        if (value) w[j] = movmatrix_trans(w[j]);
+      }
+      uint8_t* tile = p.kv.pages + p.kv.tile_at(gr.page, head, gr.tile) + (plane0 + pl) * kKvTileBytes;
+      uint8_t* words = tile + (value ? 512 : 0) + 16 * lane;
+      uint32_t* pairs = reinterpret_cast<uint32_t*>(tile + kKvPairs) + 4 * g + (value ? 2 : 0);
+      if ((rows & rows8) == 0xffffffffu) {
+        *reinterpret_cast<uint4*>(words) = make_uint4(w[0], w[1], w[2], w[3]);
+        if (t == 0) *reinterpret_cast<uint2*>(pairs) = make_uint2(pair[0], pair[1]);
+        continue;
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (live[s] && t == 0) pairs[s] = pair[s];
+        const uint32_t r = s == 0 ? rows : rows8;
+#pragma unroll
+        for (int c = 0; c < 2; ++c)   // byte 2 c + s of a word: of keys token g + 8 s, of values token 2 t + c + 8 s
+          if (r >> (4 * (value ? 2 * t + c : g)) & 1u) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) words[4 * j + 2 * c + s] = (uint8_t)(w[j] >> (16 * c + 8 * s));
+          }
+      }
     }
   }
 }
@@ -257,14 +271,14 @@ kv_read_kernel(const KvStoreParams p) {
 
 // Rows a CTA looks for groups in: one while warps are few, so that every token has its own; sixteen beyond, where groups are whole
 // tiles and most of the warps of single rows would find nothing.
-static int kv_window(int T) { return T <= 2048 ? 1 : 16; }
+static bool kv_many(int T) { return T > 2048; }
 
 template <class Fn>
-static moin_status kv_store_launch(Fn* fn64, Fn* fn128, KvStoreParams& p, int head_dim, cudaStream_t s) {
-  p.window = kv_window(p.T);
-  const dim3 grid((unsigned)((p.T + p.window - 1) / p.window), (unsigned)((2 * p.kv.H * p.kv.planes + kKvStoreWarps - 1) / kKvStoreWarps));
+static moin_status kv_store_launch(Fn* fn, KvStoreParams& p, int per_head, cudaStream_t s) {
+  p.window = kv_many(p.T) ? 16 : 1;
+  const dim3 grid((unsigned)((p.T + p.window - 1) / p.window), (unsigned)((2 * p.kv.H * per_head + kKvStoreWarps - 1) / kKvStoreWarps));
   ProfScope prof(MOIN_K_KV_STORE, 1, s);
-  return record_cuda(launch_pdl(head_dim == 64 ? fn64 : fn128, grid, 32 * kKvStoreWarps, 0, s, p));
+  return record_cuda(launch_pdl(fn, grid, 32 * kKvStoreWarps, 0, s, p));
 }
 
 }  // namespace moin
@@ -292,7 +306,9 @@ extern "C" moin_status moin_kv_append(const moin_kv* kv, const int32_t* slot, co
   p.slot = slot; p.k = (const __nv_bfloat16*)k; p.v = (const __nv_bfloat16*)v;
   p.k_stride = k_stride; p.v_stride = v_stride;
   p.pos = pos; p.rope = (const float2*)rope; p.rope_len = rope_len; p.T = T;
-  return kv_store_launch(kv_append_kernel<64>, kv_append_kernel<128>, p, kv->head_dim, (cudaStream_t)stream);
+  if (kv->head_dim == 64) return kv_store_launch(kv_append_kernel<64, 1>, p, 1, (cudaStream_t)stream);
+  if (kv_many(T)) return kv_store_launch(kv_append_kernel<128, 2>, p, 1, (cudaStream_t)stream);
+  return kv_store_launch(kv_append_kernel<128, 1>, p, 2, (cudaStream_t)stream);
 }
 
 extern "C" moin_status moin_kv_read(const moin_kv* kv, const int32_t* slot, void* k, int64_t k_stride, void* v, int64_t v_stride,
@@ -309,5 +325,6 @@ extern "C" moin_status moin_kv_read(const moin_kv* kv, const int32_t* slot, void
   if ((st = host_state(&hs))) return st;
   p.slot = slot; p.k_out = (__nv_bfloat16*)k; p.v_out = (__nv_bfloat16*)v;
   p.k_stride = k_stride; p.v_stride = v_stride; p.T = T;
-  return kv_store_launch(kv_read_kernel<64>, kv_read_kernel<128>, p, kv->head_dim, (cudaStream_t)stream);
+  return kv->head_dim == 64 ? kv_store_launch(kv_read_kernel<64>, p, 1, (cudaStream_t)stream)
+                            : kv_store_launch(kv_read_kernel<128>, p, 2, (cudaStream_t)stream);
 }
