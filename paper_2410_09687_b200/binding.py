@@ -619,6 +619,7 @@ class KvCache:
         self.page_tokens, self.head_dim = pages.shape[2] * 16, pages.shape[3] * 64
         self.c = _Kv(_ptr(pages), self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim)
         self.ref = ctypes.byref(self.c)
+        self.ws_bytes: dict = {}   # (queries of a request, heads) -> bytes of scratch (asking the library costs half a microsecond)
 
     @classmethod
     def empty(cls, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, device) -> "KvCache":
@@ -668,32 +669,50 @@ class KvBatch:
         self.ref = ctypes.byref(self.c)
 
 
+# These checks stand before every step of a generation loop: few attribute reads, each costs a tenth of a microsecond.
+_bf16, _int32, _fp32 = torch.bfloat16, torch.int32, torch.float32
+
+
+def _i32(t: torch.Tensor, n: int) -> int:
+    """Address of an int32 vector of n entries."""
+    if t.dtype is not _int32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise MoinError(f"expected {n} contiguous int32 values on a CUDA device, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
 def kv_update(tables: KvTables, want: torch.Tensor, batch: KvBatch, rows: Optional[torch.Tensor] = None,
               lens_out: Optional[torch.Tensor] = None, n_free_out: Optional[torch.Tensor] = None, stream=None) -> KvBatch:
     """moin_kv_update: request i (row ``rows[i]`` of the tables, or i) becomes ``want[i]`` tokens long.  Returns ``batch``."""
-    assert want.dtype == torch.int32 and want.shape == (batch.R,) and (rows is None or (rows.dtype == torch.int32 and rows.shape == want.shape))
-    assert lens_out is None or (lens_out.dtype == torch.int32 and lens_out.shape == tables.lens.shape)
-    assert n_free_out is None or (n_free_out.dtype == torch.int32 and n_free_out.numel() == 1)
-    _check(lib().moin_kv_update(tables.ref, _ptr(rows), _ptr(want), batch.ref, _ptr(lens_out), _ptr(n_free_out), _stream(stream)),
-           "moin_kv_update")
+    R = batch.R
+    st = lib().moin_kv_update(tables.ref, None if rows is None else _i32(rows, R), _i32(want, R), batch.ref,
+                              None if lens_out is None else _i32(lens_out, tables.n_rows),
+                              None if n_free_out is None else _i32(n_free_out, 1), _stream(stream))
+    if st:
+        _check(st, "moin_kv_update")
     return batch
 
 
-def _tokens_ptr(t: torch.Tensor, heads: int, head_dim: int) -> tuple:
+def _tokens_ptr(t: torch.Tensor, T: int, heads: int, head_dim: int) -> tuple:
     """(address, elements between tokens) of [T, heads, head_dim] bf16 (or [T, heads * head_dim]) whose tokens may lie apart."""
-    if not t.is_cuda:
-        raise MoinError("tensor arguments must live on a CUDA device (no CPU path exists)")
-    assert t.dtype == torch.bfloat16 and (t.shape[1:] == (heads, head_dim) or t.shape[1:] == (heads * head_dim,)), t.shape
-    if t.stride(-1) != 1 or (t.dim() == 3 and heads > 1 and t.stride(1) != head_dim):
+    if t.dtype is not _bf16 or t.numel() != T * heads * head_dim or not t.is_cuda or t.shape[0] != T:
+        raise MoinError(f"expected bf16 [{T}, {heads}, {head_dim}] on a CUDA device, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    if t.is_contiguous():
+        return t.data_ptr(), heads * head_dim
+    if t.dim() == 3:
+        if t.shape[1] != heads or t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
+            raise MoinError("the heads of a token must lie side by side")
+    elif t.dim() != 2 or t.stride(1) != 1:
         raise MoinError("the heads of a token must lie side by side")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else heads * head_dim)
+    return t.data_ptr(), (t.stride(0) if T > 1 else heads * head_dim)
 
 
 def _rope_arg(rope: Optional[torch.Tensor], head_dim: int) -> tuple:
     if rope is None:
         return None, 0
-    assert rope.dtype == torch.float32 and rope.dim() == 3 and rope.shape[1:] == (head_dim // 2, 2)
-    return _ptr(rope), rope.shape[0]
+    n, more = divmod(rope.numel(), head_dim)
+    if rope.dtype is not _fp32 or more or not rope.is_contiguous() or not rope.is_cuda:
+        raise MoinError(f"expected a float32 table [positions, {head_dim // 2}, 2] on a CUDA device, got {tuple(rope.shape)} of {rope.dtype}")
+    return rope.data_ptr(), n
 
 
 def rope_table(n_pos: int, head_dim: int, base: float, device, stream=None) -> torch.Tensor:
@@ -707,26 +726,26 @@ def kv_append(cache: KvCache, slot: torch.Tensor, k: torch.Tensor, v: torch.Tens
               rope: Optional[torch.Tensor] = None, stream=None) -> None:
     """moin_kv_append: quantise row t of ``k`` (rotated by ``rope`` at ``pos[t]`` if given) and ``v`` and store them in ``slot[t]``."""
     T = slot.shape[0]
-    assert slot.dtype == torch.int32 and k.shape[0] == T and v.shape[0] == T
-    assert rope is None or (pos is not None and pos.dtype == torch.int32 and pos.shape == slot.shape)
-    kp, ks = _tokens_ptr(k, cache.n_kv_heads, cache.head_dim)
-    vp, vs = _tokens_ptr(v, cache.n_kv_heads, cache.head_dim)
+    kp, ks = _tokens_ptr(k, T, cache.n_kv_heads, cache.head_dim)
+    vp, vs = _tokens_ptr(v, T, cache.n_kv_heads, cache.head_dim)
     rp, rn = _rope_arg(rope, cache.head_dim)
-    _check(lib().moin_kv_append(cache.ref, _ptr(slot), kp, ks, vp, vs, _ptr(pos), rp, rn, T, _stream(stream)), "moin_kv_append")
+    st = lib().moin_kv_append(cache.ref, _i32(slot, T), kp, ks, vp, vs, None if pos is None else _i32(pos, T), rp, rn, T, _stream(stream))
+    if st:
+        _check(st, "moin_kv_append")
 
 
 def kv_read(cache: KvCache, slot: torch.Tensor, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None, stream=None) -> tuple:
     """moin_kv_read: (k, v), bf16 [T, n_kv_heads, head_dim], of what the slots hold."""
     T, H, D = slot.shape[0], cache.n_kv_heads, cache.head_dim
-    assert slot.dtype == torch.int32
     if k is None:
         k = torch.empty(T, H, D, dtype=torch.bfloat16, device=slot.device)
     if v is None:
-        v = torch.empty(T, H, D, dtype=torch.bfloat16, device=slot.device)
-    assert k.shape[0] == T and v.shape[0] == T
-    kp, ks = _tokens_ptr(k, H, D)
-    vp, vs = _tokens_ptr(v, H, D)
-    _check(lib().moin_kv_read(cache.ref, _ptr(slot), kp, ks, vp, vs, T, _stream(stream)), "moin_kv_read")
+        v = torch.empty_like(k) if k.is_contiguous() else torch.empty(T, H, D, dtype=torch.bfloat16, device=slot.device)
+    kp, ks = _tokens_ptr(k, T, H, D)
+    vp, vs = _tokens_ptr(v, T, H, D)
+    st = lib().moin_kv_read(cache.ref, _i32(slot, T), kp, ks, vp, vs, T, _stream(stream))
+    if st:
+        _check(st, "moin_kv_read")
     return k, v
 
 
@@ -737,20 +756,26 @@ def kv_attention(cache: KvCache, tables: KvTables, q: torch.Tensor, cu_q: torch.
     ``out`` behind the last request are undefined."""
     T, n_heads, D = q.shape
     R = kv_len.shape[0]
-    assert cu_q.dtype == torch.int32 and cu_q.shape == (R + 1,) and kv_len.dtype == torch.int32 and D == cache.head_dim
-    assert rows is None or (rows.dtype == torch.int32 and rows.shape == kv_len.shape)
+    qp, qs = _tokens_ptr(q, T, n_heads, cache.head_dim)
     if out is None:
         out = torch.empty(T, n_heads, D, dtype=torch.bfloat16, device=q.device)
-    assert out.shape == q.shape
-    qp, qs = _tokens_ptr(q, n_heads, D)
-    op, os_ = _tokens_ptr(out, n_heads, D)
+        op, os_ = out.data_ptr(), n_heads * D
+    else:
+        op, os_ = _tokens_ptr(out, T, n_heads, D)
     rp, rn = _rope_arg(rope, D)
     max_q = T if max_q < 1 or max_q > T else max_q
-    n, s = lib().moin_kv_attention_workspace_bytes(max_q, n_heads, cache.n_kv_heads, D), _stream(stream)
+    L, s = lib(), _stream(stream)
+    n = cache.ws_bytes.get((max_q, n_heads))
+    if n is None:
+        if len(cache.ws_bytes) >= 1024:
+            cache.ws_bytes.clear()
+        n = cache.ws_bytes[max_q, n_heads] = L.moin_kv_attention_workspace_bytes(max_q, n_heads, cache.n_kv_heads, D)
     ws = _scratch_alloc(n, s)
     try:
-        _check(lib().moin_kv_attention(cache.ref, tables.ref, _ptr(rows), _ptr(cu_q), _ptr(kv_len), R, T, max_q, max_kv, qp, qs, n_heads,
-                                       D ** -0.5 if scale is None else float(scale), rp, rn, op, os_, ws, n, s), "moin_kv_attention")
+        st = L.moin_kv_attention(cache.ref, tables.ref, None if rows is None else _i32(rows, R), _i32(cu_q, R + 1), _i32(kv_len, R), R, T, max_q,
+                                 max_kv, qp, qs, n_heads, D ** -0.5 if scale is None else scale, rp, rn, op, os_, ws, n, s)
     finally:
         _scratch_free(ws)
+    if st:
+        _check(st, "moin_kv_attention")
     return out
