@@ -450,6 +450,7 @@ moin_status moin_decoder_forward_per_token(const moin_model* model, const int32_
  *   moin_kv_append      keys and values of the new tokens -> rotated, quantised, stored by slot
  *   moin_kv_read        stored rows by slot -> the bf16 values they stand for
  *   moin_kv_attention   queries over their request's cached tokens: one token a request, several, or a prompt's chunk
+ *   moin_decoder_forward_cached (below)   the decoder's blocks on top of them
  *
  * Format.  A row is the 64 channels of one token, kv head and plane (head_dim 64: one plane, 128: two) of a key or value:
  *   zero = min(x);  scale = bf16(max((max(x) - min(x)) / 15, |zero| 2^-12, 2^-64));  code = rint((x - zero) / scale) in 0..15
@@ -547,6 +548,26 @@ moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables* tables, c
                               const int32_t* kv_len, int32_t R, int32_t T, int32_t max_q, int32_t max_kv, const void* q,
                               int64_t q_stride, int32_t n_heads, float scale, const float* rope, int32_t rope_len, void* out,
                               int64_t out_stride, void* workspace, size_t workspace_bytes, moin_stream stream);
+
+/* The decoder forward on top of a cache: the batch's new tokens (one a request, a prompt, or a chunk of one, as moin_kv_update laid
+ * them out) run through the blocks, their keys and values are stored in the layers' caches, and they attend to everything
+ * cached of their request, themselves included.  The tokens of a request that runs through in one call or in many see the same
+ * stored keys and values.  Everything else is moin_decoder_forward (adapters by req_expert, conventions, storage, taps).
+ *   tokens     [batch->T] int32; rows of the batch behind cu_q[R] run as tokens of the base model and are stored nowhere
+ *   caches     HOST array [n_layers], each of n_kv_heads heads of head_dim (64) in pages of tables->page_tokens
+ *   batch      as filled by moin_kv_update for these tables and rows; refused requests get the logits of attention outputs of zero
+ *   rope       table of moin_rope_table(rope_len, head_dim, model->rope_base), rope_len >= max_kv
+ *   max_q, max_kv   host upper bounds as for moin_kv_attention
+ *   logits     [batch->T, vocab] or [R, vocab], as logits_mode says (MOIN_LOGITS_LAST: zeros for a request without new tokens)
+ * Reads nothing back; can be captured together with moin_kv_update.  workspace: 256-byte aligned,
+ * moin_decoder_cached_workspace_bytes(...) bytes.  Errors: as for moin_decoder_forward and moin_kv_attention, before anything
+ * is launched. */
+size_t moin_decoder_cached_workspace_bytes(const moin_model* model, int32_t R, int32_t T, int32_t max_q);
+moin_status moin_decoder_forward_cached(const moin_model* model, const int32_t* tokens, const moin_kv* caches,
+                                        const moin_kv_tables* tables, const int32_t* rows, const moin_kv_batch* batch,
+                                        const int32_t* req_expert, int32_t max_q, int32_t max_kv, const float* rope,
+                                        int32_t rope_len, void* logits, int32_t logits_mode, const moin_decoder_taps* taps,
+                                        void* workspace, size_t workspace_bytes, moin_stream stream);
 
 #ifdef __cplusplus
 }

@@ -27,7 +27,7 @@ EXPORTED_SYMBOLS = (
     "moin_kmeans_update", "moin_route_top2", "moin_route_top2_workspace_bytes", "moin_cache_create", "moin_cache_destroy", "moin_cache_admit", "moin_cache_slot_of",
     "moin_selftest_bounded_wait", "moin_decoder_forward_per_token", "moin_dequant_fp8", "moin_pool_set_adapter",
     "moin_kv_bytes", "moin_kv_tables_reset", "moin_kv_update", "moin_kv_append", "moin_kv_read", "moin_rope_table",
-    "moin_kv_attention_workspace_bytes", "moin_kv_attention",
+    "moin_kv_attention_workspace_bytes", "moin_kv_attention", "moin_decoder_cached_workspace_bytes", "moin_decoder_forward_cached",
 )
 
 
@@ -165,6 +165,10 @@ def lib() -> ctypes.CDLL:
         L.moin_kv_attention_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.moin_kv_attention.argtypes = [ctypes.POINTER(_Kv), ctypes.POINTER(_KvTables), vp, vp, vp, i32, i32, i32, i32, vp, i64,
                                         i32, f32, vp, i32, vp, i64, vp, sz, vp]
+        L.moin_decoder_cached_workspace_bytes.restype = sz
+        L.moin_decoder_cached_workspace_bytes.argtypes = [ctypes.POINTER(_Model), i32, i32, i32]
+        L.moin_decoder_forward_cached.argtypes = [ctypes.POINTER(_Model), vp, ctypes.POINTER(_Kv), ctypes.POINTER(_KvTables), vp,
+                                                  ctypes.POINTER(_KvBatch), vp, i32, i32, vp, i32, vp, i32, ctypes.POINTER(_Taps), vp, sz, vp]
         L.moin_profile_enable.argtypes = [i32]
         L.moin_profile_read.argtypes = [ctypes.POINTER(_ProfRec), i32, ctypes.POINTER(i32)]
         L.moin_kernel_name.restype = ctypes.c_char_p
@@ -779,3 +783,46 @@ def kv_attention(cache: KvCache, tables: KvTables, q: torch.Tensor, cu_q: torch.
     if st:
         _check(st, "moin_kv_attention")
     return out
+
+
+class KvLayers:
+    """The caches of a decoder's layers, as moin_decoder_forward_cached takes them."""
+
+    def __init__(self, caches: Sequence[KvCache]):
+        self.caches = list(caches)
+        self.c = (_Kv * len(self.caches))(*[x.c for x in self.caches])
+
+
+def decoder_forward_cached(model: DecoderModel, tokens: torch.Tensor, layers: KvLayers, tables: KvTables, batch: KvBatch,
+                           req_expert: Optional[torch.Tensor], rope: torch.Tensor, max_q: int = 0, max_kv: int = 0,
+                           rows: Optional[torch.Tensor] = None, logits_mode: int = LOGITS_LAST, logits: Optional[torch.Tensor] = None,
+                           hidden_in: Optional[torch.Tensor] = None, hidden_out: Optional[torch.Tensor] = None, layer_begin: int = 0,
+                           layer_end: Optional[int] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """moin_decoder_forward_cached: the batch that ``kv_update`` laid out, on top of the layers' caches.  Returns logits (bf16) or None
+    for LOGITS_NONE.  Without ``workspace`` a call's scratch comes from the caching allocator and belongs to it alone."""
+    cfg, R, T = model.cfg, batch.R, batch.T
+    if len(layers.caches) != cfg.n_layers:
+        raise MoinError(f"{len(layers.caches)} caches for {cfg.n_layers} layers")
+    for t, shape in ((hidden_in, (T, cfg.hidden)), (hidden_out, (T, cfg.hidden))):
+        if t is not None and (t.dtype is not _fp32 or t.shape != shape):
+            raise MoinError(f"expected float32 {shape}, got {tuple(t.shape)} of {t.dtype}")
+    if logits_mode != LOGITS_NONE:
+        shape = (T if logits_mode == LOGITS_ALL else R, cfg.vocab)
+        if logits is None:
+            logits = torch.empty(*shape, dtype=torch.bfloat16, device=tokens.device)
+        elif logits.dtype is not _bf16 or logits.shape != shape:
+            raise MoinError(f"expected bf16 {shape}, got {tuple(logits.shape)} of {logits.dtype}")
+    taps = _Taps(_ptr(hidden_in), _ptr(hidden_out), layer_begin, cfg.n_layers if layer_end is None else layer_end)
+    rp, rn = _rope_arg(rope, cfg.head_dim)
+    s = _stream(stream)
+    n = lib().moin_decoder_cached_workspace_bytes(ctypes.byref(model.c), R, T, max_q)
+    ws = workspace.data_ptr() if workspace is not None else _scratch_alloc(n, s)
+    try:
+        st = lib().moin_decoder_forward_cached(ctypes.byref(model.c), _i32(tokens, T), layers.c, tables.ref, None if rows is None else _i32(rows, R),
+                                               batch.ref, None if req_expert is None else _i32(req_expert, R), max_q, max_kv, rp, rn, _ptr(logits),
+                                               logits_mode, ctypes.byref(taps), ws, n if workspace is None else workspace.numel(), s)
+    finally:
+        if workspace is None:
+            _scratch_free(ws)
+    _check(st, "moin_decoder_forward_cached")
+    return logits

@@ -1,6 +1,7 @@
 // Decoder forward: glue kernels (embedding, RMSNorm, rotary embedding, causal GQA attention,
 // SwiGLU) around the routed LoRA projections, and the host-side sequencing.
 #include "common.cuh"
+#include "kv.cuh"
 #include "tc_gemm.cuh"
 
 namespace moin {
@@ -9,12 +10,15 @@ namespace moin {
 // request).  One CTA per request.
 __global__ void __launch_bounds__(256)
 token_meta_kernel(const int* __restrict__ cu, const int* __restrict__ req_expert,
-                  const int* __restrict__ token_expert_in, int R, int* __restrict__ pos,
+                  const int* __restrict__ token_expert_in, int R, int T, int* __restrict__ pos,
                   int* __restrict__ token_expert, int* __restrict__ last_row) {
   pdl_begin();
   const int r = blockIdx.x;
-  if (r >= R) return;
-  const int t0 = cu[r], t1 = cu[r + 1];
+  if (r == R) {   // (only where the batch has room behind its last request: rows of no request, base model)
+    for (int t = min(max(cu[R], 0), T) + threadIdx.x; t < T; t += blockDim.x) token_expert[t] = -1;
+    return;
+  }
+  const int t0 = min(max(cu[r], 0), T), t1 = min(max(cu[r + 1], t0), T);
   const int e = req_expert ? req_expert[r] : -1;
   for (int t = t0 + threadIdx.x; t < t1; t += blockDim.x) {
     pos[t] = t - t0;
@@ -452,8 +456,19 @@ extern "C" size_t moin_decoder_workspace_bytes(const moin_model* model, int32_t 
   return carve(model, R, T, T, nullptr).total + 256;
 }
 
+// Forward on top of a cache: new tokens are stored and attend to what is cached of their requests (nullptr: whole prompts).
+struct CachedForward {
+  const moin_kv* caches;      // one per layer
+  const moin_kv_tables* tables;
+  const int32_t* rows;
+  const moin_kv_batch* batch;
+  int32_t max_q, max_kv;
+  const float* rope;
+  int32_t rope_len;
+};
+
 static moin_status decoder_forward_impl(const moin_model* m, const int32_t* tokens, const int32_t* cu_seqlens,
-                                        const int32_t* req_expert, const int32_t* token_expert_in, int32_t R,
+                                        const int32_t* req_expert, const int32_t* token_expert_in, const CachedForward* kv, int32_t R,
                                         int32_t T, int32_t max_seqlen, void* logits, int32_t logits_mode,
                                         const moin_decoder_taps* taps, void* workspace, size_t workspace_bytes,
                                         moin_stream stream) {
@@ -471,7 +486,8 @@ static moin_status decoder_forward_impl(const moin_model* m, const int32_t* toke
   if (!from_hidden && (!tokens || !m->embed)) return MOIN_ERR_INVALID_ARG;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return MOIN_ERR_WORKSPACE;
   DecoderWorkspace w = carve(m, R, T, T, workspace);
-  if (workspace_bytes < w.total) return MOIN_ERR_WORKSPACE;
+  const size_t att_bytes = kv ? moin_kv_attention_workspace_bytes(kv->max_q, m->n_heads, m->n_kv_heads, m->head_dim) : 0;
+  if (workspace_bytes < w.total + att_bytes) return MOIN_ERR_WORKSPACE;
   HostState* hs;
   moin_status st = host_state(&hs);
   if (st) return st;
@@ -479,9 +495,9 @@ static moin_status decoder_forward_impl(const moin_model* m, const int32_t* toke
   const int H = m->hidden, nh = m->n_heads, nkv = m->n_kv_heads, F = m->ffn;
   const int qd = nh * 64, kvd = nkv * 64;
 
-  { ProfScope prof(MOIN_K_GLUE, 2, s);
-  launch_pdl(token_meta_kernel, R, 256, 0, s, cu_seqlens, req_expert, token_expert_in, R, w.pos, w.token_expert, w.last_row);
-  launch_pdl(rope_table_kernel, (max_seqlen * 32 + 255) / 256, 256, 0, s, w.rope, max_seqlen, 32, (double)m->rope_base); }
+  { ProfScope prof(MOIN_K_GLUE, kv ? 1 : 2, s);
+  launch_pdl(token_meta_kernel, kv ? R + 1 : R, 256, 0, s, cu_seqlens, req_expert, token_expert_in, R, T, w.pos, w.token_expert, w.last_row);
+  if (!kv) launch_pdl(rope_table_kernel, (max_seqlen * 32 + 255) / 256, 256, 0, s, w.rope, max_seqlen, 32, (double)m->rope_base); }
   moin_plan plan;
   memset(&plan, 0, sizeof(plan));
   const bool lora = m->pools != nullptr && (req_expert != nullptr || token_expert_in != nullptr);
@@ -570,6 +586,12 @@ static moin_status decoder_forward_impl(const moin_model* m, const int32_t* toke
       void* const outs[3] = {w.q, w.k, w.v};
       if ((st = proj_group(l, 0, 3, w.xn, H, dout, outs))) return st;
     }
+    if (kv) {   // stored rotated and quantised, read back by the attention: what later tokens see is what these see
+      if ((st = moin_kv_append(&kv->caches[l], kv->batch->slot, w.k, kvd, w.v, kvd, kv->batch->pos, kv->rope, kv->rope_len, T, stream))) return st;
+      if ((st = moin_kv_attention(&kv->caches[l], kv->tables, kv->rows, cu_seqlens, kv->batch->kv_len, R, T, kv->max_q, kv->max_kv, w.q, qd, nh,
+                                  0.125f, kv->rope, kv->rope_len, w.att, qd, (char*)workspace + w.total, att_bytes, stream)))
+        return st;
+    } else {
     // rotary embedding: the keys are rotated in place once (every query head and every later query reads them);
     // the queries are rotated inside the attention kernel as it loads them
     { ProfScope prof(MOIN_K_GLUE, 1, s);
@@ -583,6 +605,7 @@ static moin_status decoder_forward_impl(const moin_model* m, const int32_t* toke
       ProfScope prof(MOIN_K_ATTENTION, 1, s);
       attention_kernel<<<dim3((max_seqlen + 63) / 64, nh, R), 128, 0, s>>>(w.q, w.k, w.v, cu_seqlens, w.att, nh, nkv, scale_log2,
                                                                          w.rope);
+    }
     }
     void* const o_out[1] = {w.o};   // (also the down projection's)
     if ((st = proj_group(l, 3, 1, w.att, qd, &H, o_out))) return st;
@@ -631,7 +654,7 @@ extern "C" moin_status moin_decoder_forward(const moin_model* m, const int32_t* 
                                             const int32_t* req_expert, int32_t R, int32_t T, int32_t max_seqlen,
                                             void* logits, int32_t logits_mode, const moin_decoder_taps* taps,
                                             void* workspace, size_t workspace_bytes, moin_stream stream) {
-  return decoder_forward_impl(m, tokens, cu_seqlens, req_expert, nullptr, R, T, max_seqlen, logits, logits_mode, taps,
+  return decoder_forward_impl(m, tokens, cu_seqlens, req_expert, nullptr, nullptr, R, T, max_seqlen, logits, logits_mode, taps,
                               workspace, workspace_bytes, stream);
 }
 
@@ -641,7 +664,7 @@ extern "C" moin_status moin_decoder_forward_per_token(const moin_model* m, const
                                                       const moin_decoder_taps* taps, void* workspace,
                                                       size_t workspace_bytes, moin_stream stream) {
   if (!token_expert) return MOIN_ERR_INVALID_ARG;
-  return decoder_forward_impl(m, tokens, cu_seqlens, nullptr, token_expert, R, T, max_seqlen, logits, logits_mode, taps,
+  return decoder_forward_impl(m, tokens, cu_seqlens, nullptr, token_expert, nullptr, R, T, max_seqlen, logits, logits_mode, taps,
                               workspace, workspace_bytes, stream);
 }
 
@@ -658,4 +681,41 @@ extern "C" moin_status moin_dequant_fp8(const void* codes, const float* scale, i
   jobs.n = 1;
   jobs.codes[0] = (const uint2*)codes; jobs.scale[0] = scale; jobs.out[0] = (uint4*)W; jobs.row_end[0] = d_out;
   return launch_dequant(jobs, d_in, (cudaStream_t)stream);
+}
+
+extern "C" size_t moin_decoder_cached_workspace_bytes(const moin_model* model, int32_t R, int32_t T, int32_t max_q) {
+  if (!model || R < 0 || T < 0) return 0;
+  if (max_q < 1 || max_q > T) max_q = T;
+  return carve(model, R, T, T, nullptr).total + moin_kv_attention_workspace_bytes(max_q, model->n_heads, model->n_kv_heads, model->head_dim) + 256;
+}
+
+extern "C" moin_status moin_decoder_forward_cached(const moin_model* m, const int32_t* tokens, const moin_kv* caches,
+                                                   const moin_kv_tables* tables, const int32_t* rows, const moin_kv_batch* batch,
+                                                   const int32_t* req_expert, int32_t max_q, int32_t max_kv, const float* rope,
+                                                   int32_t rope_len, void* logits, int32_t logits_mode, const moin_decoder_taps* taps,
+                                                   void* workspace, size_t workspace_bytes, moin_stream stream) {
+  if (!m || !caches || !tables || !batch) return MOIN_ERR_INVALID_ARG;
+  if (batch->R < 0 || batch->T < 0) return MOIN_ERR_INVALID_ARG;
+  if (batch->R == 0 || batch->T == 0) return MOIN_OK;
+  if (!batch->cu_q || !batch->kv_len || !batch->slot || !batch->pos || !rope) return MOIN_ERR_INVALID_ARG;
+  if (max_q < 1 || max_q > batch->T) max_q = batch->T;
+  // everything the attention of a layer would refuse is refused before the first launch
+  const long long row = (long long)tables->max_pages * tables->page_tokens;
+  if (!tables->block_table || tables->n_rows < 1 || tables->max_pages < 1) return MOIN_ERR_INVALID_ARG;
+  if (row > (1 << 30) || (!rows && batch->R > tables->n_rows) || batch->R > 65535) return MOIN_ERR_BAD_SHAPE;
+  if (max_kv < 1 || max_kv > row) max_kv = (int32_t)row;
+  if (rope_len < max_kv) return MOIN_ERR_BAD_SHAPE;
+  if (!aligned16(rope)) return MOIN_ERR_MISALIGNED;
+  if (m->n_kv_heads < 1 || m->n_heads < m->n_kv_heads) return MOIN_ERR_BAD_SHAPE;
+  const long long group = m->n_heads / m->n_kv_heads;
+  if (max_q * group * group > 0xFFFFFFFFll) return MOIN_ERR_BAD_SHAPE;
+  for (int l = 0; l < m->n_layers; ++l) {
+    KvView v;
+    const moin_status st = kv_view(&caches[l], &v);
+    if (st) return st;
+    if (caches[l].n_kv_heads != m->n_kv_heads || caches[l].head_dim != m->head_dim || caches[l].page_tokens != tables->page_tokens) return MOIN_ERR_BAD_SHAPE;
+  }
+  const CachedForward kv = {caches, tables, rows, batch, max_q, max_kv, rope, rope_len};
+  return decoder_forward_impl(m, tokens, batch->cu_q, req_expert, nullptr, &kv, batch->R, batch->T, max_q, logits, logits_mode, taps, workspace,
+                              workspace_bytes, stream);
 }

@@ -89,6 +89,27 @@ def test_tables_and_cache_must_agree(lib):
         assert L.moin_kv_attention(_kv(lib), _tables(lib, **t), None, A, A, 1, 1, 1, 1, A, 256, 4, 1.0, None, 0, A, 256, A, 1 << 30, None) < 0
 
 
+@pytest.mark.parametrize("args,status", [
+    ({"caches": None}, INVALID), ({"tables": None}, INVALID), ({"batch": None}, INVALID), ({"rope": None}, INVALID), ({"rope_len": 99}, SHAPE),
+    ({"rope": A + 4}, MISALIGNED), ({"t": {"table": None}}, INVALID), ({"t": {"page_tokens": 32}}, SHAPE), ({"k": {"dim": 128}}, SHAPE),
+    ({"k": {"heads": 3}}, SHAPE), ({"k": {"pages": None}}, INVALID), ({"b": {"slot": None}}, INVALID), ({"b": {"R": 5}}, SHAPE),
+    ({"ws": A + 16}, WORKSPACE), ({"n_ws": 4096}, WORKSPACE), ({"b": {"T": 0}}, 0), ({}, NO_DEVICE)])
+def test_cached_forward_refused(lib, args, status):
+    m = lib._Model()
+    m.n_layers, m.hidden, m.n_heads, m.n_kv_heads, m.head_dim, m.ffn, m.vocab, m.rms_eps, m.rope_base = 2, 128, 4, 2, 64, 128, 64, 1e-5, 1e4
+    m.embed = m.lm_head = m.final_norm = A
+    ptrs = (ctypes.c_void_p * 14)(*[A] * 14)
+    m.attn_norm = m.mlp_norm = m.W = ctypes.cast(ptrs, ctypes.POINTER(ctypes.c_void_p))
+    a = {"rope": A, "rope_len": 100, "ws": A, "n_ws": 1 << 30} | args
+    one = {"pages": A, "n_pages": 8, "page_tokens": 16, "heads": 2, "dim": 64} | args.get("k", {})
+    caches = (lib._Kv * 2)(*[lib._Kv(A, 8, 16, 2, 64), lib._Kv(*one.values())])
+    got = lib.lib().moin_decoder_forward_cached(ctypes.byref(m), A, None if "caches" in args else caches,
+                                                None if "tables" in args else _tables(lib, **args.get("t", {})), None,
+                                                None if "batch" in args else _batch(lib, **args.get("b", {})), None, 2, 100, a["rope"], a["rope_len"],
+                                                A, 1, None, a["ws"], a["n_ws"], None)
+    assert got == status
+
+
 def test_rope_table_refused(lib):
     L = lib.lib()
     for args, status in (((A, -1, 64, 1e4), INVALID), ((A, 4, 64, 0.0), INVALID), ((A, 4, 64, float("nan")), INVALID), ((A, 4, 48, 1e4), SHAPE),
