@@ -47,7 +47,7 @@ struct KvAttParams {
   float scale_log2;
   int split;               // items are cut: CTAs take equal shares of all tiles (else a CTA takes an item)
   float* part;             // [worker][2][row][64 P + 4]: sums of items that several workers share
-  int4* desc;              // [worker][2]: what they belong to
+  int4* desc;              // [CTA][2]: the item that it begins without ending it (head, first row, first token, CTAs behind), its rows
 };
 
 __device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -393,12 +393,15 @@ __device__ __forceinline__ long long kv_cost(const KvAttParams& p, int req, int 
   return (long long)blocks * p.kv.H * kv_count(p.kv_len[req], p.max_kv);
 }
 
-// All items stand in one line (request, row block, head), each as long as it counts, and warp w of W takes from total w / W on.
+// All items stand in one line (request, row block, head), each as long as it counts, and every warp takes an equal run of it.
 // Every CTA finds its warps' places: each thread adds up a run of requests, a scan over the CTA gives the total, and the
 // thread whose run holds a place walks it.
 struct KvShare { long long at, end, base; int req; };   // base: what the requests before `req` count
+__device__ __forceinline__ long long kv_div(long long a, long long b) {   // both positive; 32 bits where they do
+  return ((a | b) >> 32) ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+}
 template <int NT, int U>
-__device__ __forceinline__ void kv_share(const KvAttParams& p, long long* s_sum, KvShare* s_share) {
+__device__ __forceinline__ long long kv_share(const KvAttParams& p, long long* s_sum, KvShare* s_share) {
   constexpr int kThreads = 32 * kKvAttWarps;
   const int tid = threadIdx.x, lane = tid & 31, per = (p.R + kThreads - 1) / kThreads;
   const int r0 = min(tid * per, p.R), r1 = min(r0 + per, p.R);
@@ -419,14 +422,12 @@ __device__ __forceinline__ void kv_share(const KvAttParams& p, long long* s_sum,
     if (w < (tid >> 5)) before += s_sum[w];
     total += s_sum[w];
   }
-  // as many warps as there are, or fewer, so that a share is worth beginning
-  const long long W = min((long long)gridDim.x * kKvAttWarps, (total + kKvItemCost + 2 * U - 1) / (kKvItemCost + 2 * U));
+  const long long warps = (long long)gridDim.x * kKvAttWarps;
+  const long long run = max(kv_div(total + warps - 1, warps), (long long)(kKvItemCost + 2 * U));   // (not less than is worth beginning)
   const long long stop = before + mine;
   int r = r0;
   for (int i = 0; i < kKvAttWarps; ++i) {
-    const long long w = (long long)blockIdx.x * kKvAttWarps + i;
-    if (w >= W) break;
-    const long long at = total * w / W, end = total * (w + 1) / W;
+    const long long at = ((long long)blockIdx.x * kKvAttWarps + i) * run;
     if (at < before || at >= stop) continue;
     for (;;) {
       const long long c = kv_cost(p, r, 8 * NT);
@@ -434,9 +435,10 @@ __device__ __forceinline__ void kv_share(const KvAttParams& p, long long* s_sum,
       before += c;
       ++r;
     }
-    s_share[i] = {at, end, before, r};
+    s_share[i] = {at, min(at + run, total), before, r};
   }
   __syncthreads();
+  return run;
 }
 
 // Sums of some rows taken against different maxima, four channels of one row: joined one by one, always in the order of the tokens.
@@ -461,8 +463,8 @@ __device__ __forceinline__ __nv_bfloat16* kv_out(const KvAttParams& p, int t0, i
 
 // A piece of an item as its warp leaves it: rows of kPitch floats, 64 P sums and the row's maximum and sum of weights behind them.
 // In slot 0 the piece that begins inside its item (the first of a warp, or of a CTA), in slot 1 the one that begins an item without
-// ending it (the last); KV_LAST: the piece ends its item.
-enum { KV_PART = 1, KV_LAST = 2 };
+// ending it (the last).
+struct KvPiece { int head, row0, t0, n_rows, left; };   // t0, n_rows of its request; what its item counts behind it; -1: no piece
 
 // A warp's ring, in which its last piece lies too.
 template <int P, int NT, int U>
@@ -481,18 +483,18 @@ kv_attention_kernel(const KvAttParams p) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ long long s_sum[kKvAttWarps];
   __shared__ KvShare s_share[kKvAttWarps];
-  __shared__ int4 s_desc[kKvAttWarps][2];
-  __shared__ int s_t0[kKvAttWarps][2], s_live[kKvAttWarps][2];
+  __shared__ KvPiece s_piece[kKvAttWarps][2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   uint8_t* ring = smem + warp * (kRing + kPiece);
   const uint32_t ring_addr = smem_u32(ring);
-  if (threadIdx.x < 2 * kKvAttWarps) s_desc[threadIdx.x >> 1][threadIdx.x & 1] = make_int4(0, 0, 0, 0);
+  if (threadIdx.x < 2 * kKvAttWarps) s_piece[threadIdx.x >> 1][threadIdx.x & 1].left = -1;
   pdl_begin();
   __syncthreads();
   const int tpp = 1 << p.tpp_log2;
   KvShare share;
+  long long run = 1;
   if (p.split) {
-    kv_share<NT, U>(p, s_sum, s_share);
+    run = kv_share<NT, U>(p, s_sum, s_share);
     share = s_share[warp];
   } else {   // the CTA's item in four
     const int n = kv_count(p.kv_len[blockIdx.z], p.max_kv) - kKvItemCost;
@@ -501,7 +503,7 @@ kv_attention_kernel(const KvAttParams p) {
   while (share.at < share.end) {
     // ---- the piece: tiles tile0 .. tile1 of an item of n_tiles
     KvItem it;
-    int tile0, tile1, n_tiles;
+    int tile0, tile1, left;
     if (p.split) {
       long long c = kv_cost(p, share.req, kRows);
       while (share.at >= share.base + c) {
@@ -510,37 +512,23 @@ kv_attention_kernel(const KvAttParams p) {
       }
       const int count = kv_count(p.kv_len[share.req], p.max_kv);
       const long long in = share.at - share.base;
-      const int item = (int)(in / count), from = (int)(in - (long long)item * count), to = (int)min((long long)count, from + (share.end - share.at));
+      const int item = (int)kv_div(in, count), from = (int)(in - (long long)item * count), to = (int)min((long long)count, from + (share.end - share.at));
       share.at += to - from;
       if (to <= kKvItemCost) continue;   // only the beginning: left to the next warp
-      n_tiles = count - kKvItemCost;
+      left = count - to;
       tile0 = max(0, from - kKvItemCost);
       tile1 = to - kKvItemCost;
       const int block = item / p.kv.H;
       it = kv_item(p, share.req, item - block * p.kv.H, block * kRows);
     } else {
       it = kv_item(p, blockIdx.z, blockIdx.y, blockIdx.x * kRows);
-      n_tiles = kv_count(p.kv_len[blockIdx.z], p.max_kv) - kKvItemCost;
       tile0 = (int)share.at;
       tile1 = (int)share.end;
+      left = kv_count(p.kv_len[blockIdx.z], p.max_kv) - kKvItemCost - tile1;
       share.at = share.end;
     }
     const int n_rows = it.q_len * p.G;
     if (it.row0 >= n_rows) break;   // (an item of its own CTA that is not there)
-    KvQuery<P, NT> q;
-    kv_load_query<P, NT>(p, it, lane, q);
-    KvState<P, NT> st;
-    st.fresh = (1u << (2 * NT)) - 1;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      st.m[n] = st.l[n] = 0;
-#pragma unroll
-      for (int pl = 0; pl < P; ++pl) {
-        st.z[pl][n] = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) st.o[n][pl][j][0] = st.o[n][pl][j][1] = 0;
-      }
-    }
     // keys that the last row of the block sees
     const int see = max(0, min(it.kv_len, it.kv_len - it.q_len + kv_div_g(p, min(it.row0 + kRows - 1, n_rows - 1)) + 1));
     const int stop = min(tile1, (see + kKvTile - 1) / kKvTile);
@@ -589,6 +577,21 @@ kv_attention_kernel(const KvAttParams p) {
       if (i < n_steps) fill(i);
       cp_async_commit();
     }
+    // (under the first copies)
+    KvQuery<P, NT> q;
+    kv_load_query<P, NT>(p, it, lane, q);
+    KvState<P, NT> st;
+    st.fresh = (1u << (2 * NT)) - 1;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      st.m[n] = st.l[n] = 0;
+#pragma unroll
+      for (int pl = 0; pl < P; ++pl) {
+        st.z[pl][n] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) st.o[n][pl][j][0] = st.o[n][pl][j][1] = 0;
+      }
+    }
 #pragma unroll 1
     for (int i = 0; i < n_steps; ++i) {
       have >>= 4;
@@ -605,7 +608,7 @@ kv_attention_kernel(const KvAttParams p) {
     }
     // ---- the rows to shared memory: the ring is idle, a piece to be joined with the warp before has its own place
     __syncwarp();
-    const bool inside = tile0 > 0, whole = !inside && tile1 == n_tiles;
+    const bool inside = tile0 > 0, whole = !inside && left == 0;
     float* rows = reinterpret_cast<float*>(ring + (inside ? kRing : 0));
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -647,100 +650,105 @@ kv_attention_kernel(const KvAttParams p) {
       }
       __syncwarp();   // (the ring is filled again)
     } else if (lane == 0) {
-      s_desc[warp][inside ? 0 : 1] = make_int4(it.req, it.head, it.row0, KV_PART | (tile1 == n_tiles ? KV_LAST : 0));
-      s_t0[warp][inside ? 0 : 1] = it.t0;
-      s_live[warp][inside ? 0 : 1] = n_rows - it.row0;
+      s_piece[warp][inside ? 0 : 1] = {it.head, it.row0, it.t0, n_rows, left};
     }
   }
   __syncthreads();
   // ---- pieces of the CTA's warps, in order, a thread for four channels of a row
   float* part = p.part + (size_t)blockIdx.x * 2 * kRows * kPitch;
-  int4 left[2] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
+  int4 open_item = make_int4(0, 0, 0, 0);   // of an item that this CTA begins and does not end: head, first row, t0 | rows, CTAs behind
+  int open_rows = 0;
 #pragma unroll 1
   for (int i = threadIdx.x; i < kRows * kCh / 4; i += 32 * kKvAttWarps) {
     const int row = i / (kCh / 4), ch = 4 * (i % (kCh / 4));
     KvSum sum = {0.f, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-    int4 d = make_int4(0, 0, 0, 0);
+    KvPiece d = {0, 0, 0, 0, -1};
     bool open = false, outside = false;   // the item began in a CTA before
-    auto leave = [&](int slot, int flags) {
+    auto leave = [&](int slot) {
       float* dst = part + (slot * kRows + row) * kPitch;
       *reinterpret_cast<float4*>(dst + ch) = sum.v;
       if (ch == 0) *reinterpret_cast<float2*>(dst + kCh) = make_float2(sum.m, sum.l);
-      if (slot == 0) left[0] = make_int4(d.x, d.y, d.z, flags);
-      else left[1] = make_int4(d.x, d.y, d.z, flags);
     };
 #pragma unroll 1
     for (int k = 0; k < 2 * kKvAttWarps; ++k) {
-      const int4 e = s_desc[k >> 1][k & 1];
-      if (!(e.w & KV_PART)) continue;
+      const KvPiece e = s_piece[k >> 1][k & 1];
+      if (e.left < 0) continue;
       const float* src = reinterpret_cast<const float*>(smem + (k >> 1) * (kRing + kPiece) + ((k & 1) ? 0 : kRing)) + row * kPitch;
       const float2 ml = *reinterpret_cast<const float2*>(src + kCh);
       const float4 v = *reinterpret_cast<const float4*>(src + ch);
       if (!open) {
         sum = {ml.x, ml.y, v};
         outside = (k & 1) == 0;
-        d = e;
         open = true;
       } else {
         sum.add(ml.x, ml.y, v);
       }
-      if (e.w & KV_LAST) {
+      d = e;
+      if (e.left == 0) {
         open = false;
-        if (outside) leave(0, KV_PART | KV_LAST);
-        else if (row < s_live[k >> 1][k & 1])
-          *reinterpret_cast<uint2*>(kv_out(p, s_t0[k >> 1][k & 1], d.y, d.z + row, ch, kCh)) = sum.result();
+        if (outside) leave(0);
+        else if (d.row0 + row < d.n_rows) *reinterpret_cast<uint2*>(kv_out(p, d.t0, d.head, d.row0 + row, ch, kCh)) = sum.result();
       }
     }
-    if (open) leave(outside ? 0 : 1, KV_PART);
+    if (open) {
+      leave(outside ? 0 : 1);
+      if (!outside) {
+        open_item = make_int4(d.head, d.row0, d.t0, (int)kv_div(d.left + kKvAttWarps * run - 1, kKvAttWarps * run));
+        open_rows = d.n_rows;
+      }
+    }
   }
   if (p.split && threadIdx.x == 0) {
-    p.desc[blockIdx.x * 2] = left[0];
-    p.desc[blockIdx.x * 2 + 1] = left[1];
+    p.desc[blockIdx.x * 2] = open_item;
+    p.desc[blockIdx.x * 2 + 1].x = open_rows;
   }
 }
 
-// Items that several CTAs share: CTA (w, y) looks at the piece of CTA w that begins an item without ending it, and adds up, for
-// two of its rows, this piece and those of the CTAs behind, which begin with the rest of the item (slot 0).
-constexpr int kKvJoinThreads = 256;
-template <int P, int NT>
-__global__ void __launch_bounds__(kKvJoinThreads)
-kv_join_kernel(const KvAttParams p, int workers) {
-  constexpr int kRows = 8 * NT, kCh = 64 * P, kPitch = kCh + 4, kWide = 2 * kCh / 4, kSets = kKvJoinThreads / kWide;
-  __shared__ float4 s_acc[kSets][kWide];
-  __shared__ float2 s_ml[kSets][2];
-  __shared__ int s_last;
+// Items that several CTAs share: CTA (w, y) looks at the item that CTA w begins without ending it, and adds up, for some of its
+// rows, that piece (slot 1) and those of the CTAs behind (slot 0).  Bound by latency: the chain item, pieces, result.
+// SETS = 1: a thread for four channels of every row walks the pieces (most items have two: a step of 256 requests spends 3 us
+// less here than with sets).  Few long items of many pieces: CTAs of two rows, whose sets of threads take a run of pieces each.
+template <int P, int NT, int SETS>
+__global__ void __launch_bounds__(SETS == 1 ? 128 * P * NT : 256)
+kv_join_kernel(const KvAttParams p) {
+  constexpr int kRows = 8 * NT, kCh = 64 * P, kPitch = kCh + 4, kThreads = SETS == 1 ? kRows * kCh / 4 : 2 * kCh / 4, kAhead = SETS == 1 ? 2 : 6;
+  __shared__ float4 s_acc[SETS][SETS == 1 ? 1 : kThreads];
+  __shared__ float2 s_ml[SETS][2];
   pdl_begin();
   const int w0 = blockIdx.x;
-  const int4 d = p.desc[w0 * 2 + 1];
-  if (!(d.w & KV_PART)) return;
-  if (threadIdx.x == 0) s_last = INT_MAX;
-  __syncthreads();
-  for (int w = w0 + 1; w < workers; w += kKvJoinThreads) {   // the CTA that ends the item
-    const int at = w + threadIdx.x;
-    if (at < workers && (p.desc[at * 2].w & KV_LAST)) atomicMin(&s_last, at);
-    __syncthreads();
-    if (s_last != INT_MAX) break;
-  }
-  const KvItem it = kv_item(p, d.x, d.y, d.z);
-  const int set = threadIdx.x / kWide, e = threadIdx.x % kWide;
-  const int row = blockIdx.y * 2 + e / (kCh / 4), ch = 4 * (e % (kCh / 4));
-  const int r = it.row0 + row;
-  const int n = min(s_last, workers - 1) - w0 + 1;   // pieces
-  KvSum sum = {-FLT_MAX, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+  const int4 d = p.desc[w0 * 2];
+  const int n_rows = p.desc[w0 * 2 + 1].x;
+  const int set = SETS == 1 ? 0 : threadIdx.x / kThreads, e = threadIdx.x % kThreads;
+  const int row = blockIdx.y * 2 + e / (kCh / 4), ch = 4 * (e % (kCh / 4)), r = d.y + row;
+  if (d.w == 0 || d.y + (int)blockIdx.y * 2 >= n_rows) return;
+  const int n = d.w + 1;   // pieces
   // (each set of threads takes a run of pieces: the order of the sums is that of the tokens)
-  const int i0 = n * set / kSets, i1 = n * (set + 1) / kSets;
-#pragma unroll 4
-  for (int i = i0; i < i1; ++i) {
-    const float* part = p.part + ((size_t)(w0 + i) * 2 + (i == 0 ? 1 : 0)) * kRows * kPitch + row * kPitch;
-    const float2 ml = *reinterpret_cast<const float2*>(part + kCh);
-    sum.add(ml.x, ml.y, *reinterpret_cast<const float4*>(part + ch));
+  const int sets = min(n, SETS), i0 = set < sets ? n * set / sets : 0, i1 = set < sets ? n * (set + 1) / sets : 0;
+  KvSum sum = {-FLT_MAX, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+  for (int i = i0; i < i1; i += kAhead) {
+    float2 ml[kAhead];
+    float4 v[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (i + k < i1) {
+        const float* part = p.part + ((size_t)(w0 + i + k) * 2 + (i + k == 0 ? 1 : 0)) * kRows * kPitch + row * kPitch;
+        ml[k] = *reinterpret_cast<const float2*>(part + kCh);
+        v[k] = *reinterpret_cast<const float4*>(part + ch);
+      }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (i + k < i1) sum.add(ml[k].x, ml[k].y, v[k]);
   }
-  s_acc[set][e] = sum.v;
-  if (ch == 0) s_ml[set][e / (kCh / 4)] = make_float2(sum.m, sum.l);
-  __syncthreads();
-  if (set != 0 || r >= it.q_len * p.G) return;
-  for (int i = 1; i < kSets; ++i) sum.add(s_ml[i][e / (kCh / 4)].x, s_ml[i][e / (kCh / 4)].y, s_acc[i][e]);
-  *reinterpret_cast<uint2*>(kv_out(p, it.t0, it.head, r, ch, kCh)) = sum.result();
+  if (SETS > 1) {
+    if (set > 0 && set < sets) {
+      s_acc[set][e] = sum.v;
+      if (ch == 0) s_ml[set][e / (kCh / 4)] = make_float2(sum.m, sum.l);
+    }
+    __syncthreads();
+    if (set != 0) return;
+    for (int i = 1; i < sets; ++i) sum.add(s_ml[i][e / (kCh / 4)].x, s_ml[i][e / (kCh / 4)].y, s_acc[i][e]);
+  }
+  if (r < n_rows) *reinterpret_cast<uint2*>(kv_out(p, d.z, d.x, r, ch, kCh)) = sum.result();
 }
 
 template <int P, int NT, int U>
@@ -771,7 +779,9 @@ static moin_status kv_att_launch(HostState* hs, int optin, KvAttParams& p, cudaS
   if (workers > kKvMaxWorkers) workers = kKvMaxWorkers;
   if (workers > most) workers = most;
   e = launch_pdl(kv_attention_kernel<P, NT, U>, (unsigned)workers, 32 * kKvAttWarps, smem, s, p);
-  if (e == cudaSuccess) e = launch_pdl(kv_join_kernel<P, NT>, dim3((unsigned)workers, 4 * NT), kKvJoinThreads, 0, s, p, (int)workers);
+  if (e != cudaSuccess) return record_cuda(e);
+  if (workers > 8 * blocks * p.kv.H * p.R) e = launch_pdl(kv_join_kernel<P, NT, 8 / P>, dim3((unsigned)workers, 4 * NT), 256, 0, s, p);
+  else e = launch_pdl(kv_join_kernel<P, NT, 1>, (unsigned)workers, 128 * P * NT, 0, s, p);
   return record_cuda(e);
 }
 
