@@ -181,6 +181,26 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
+_STEPS_PATH = os.path.join(_HERE, "_steps.so")
+_steps = None
+
+
+def _load_steps():
+    """The Python extension that marshals the cache calls of a generation loop (csrc/steps.cpp), over this library's functions."""
+    global _steps
+    if not os.path.exists(_STEPS_PATH):
+        raise MoinError(f"{_STEPS_PATH} not found: build it with `python -m paper_2410_09687_b200.build` (there is no fallback path)")
+    import importlib.util
+    spec = importlib.util.spec_from_file_location("paper_2410_09687_b200._steps", _STEPS_PATH)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    L = lib()
+    mod.init(MoinError, *[ctypes.cast(f, ctypes.c_void_p).value for f in (L.moin_kv_update, L.moin_kv_append, L.moin_kv_read,
+                                                                       L.moin_kv_attention_workspace_bytes, L.moin_kv_attention)])
+    _steps = mod
+    return mod
+
+
 def _check(st: int, what: str) -> None:
     if st != 0:
         L = lib()
@@ -622,8 +642,7 @@ class KvCache:
         self.n_pages, self.n_kv_heads = pages.shape[0], pages.shape[1]
         self.page_tokens, self.head_dim = pages.shape[2] * 16, pages.shape[3] * 64
         self.c = _Kv(_ptr(pages), self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim)
-        self.ref = ctypes.byref(self.c)
-        self.ws_bytes: dict = {}   # (queries of a request, heads) -> bytes of scratch (asking the library costs half a microsecond)
+        self.addr = ctypes.addressof(self.c)
 
     @classmethod
     def empty(cls, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, device) -> "KvCache":
@@ -648,7 +667,7 @@ class KvTables:
         self.n_pages, self.page_tokens = free_pages.shape[0], page_tokens
         self.c = _KvTables(_ptr(block_table), _ptr(free_pages), _ptr(lens), _ptr(n_free), self.n_rows, self.max_pages, self.n_pages,
                            page_tokens)
-        self.ref = ctypes.byref(self.c)
+        self.addr = ctypes.addressof(self.c)
         if reset:
             self.reset(stream)
 
@@ -659,7 +678,7 @@ class KvTables:
 
     def reset(self, stream=None) -> None:
         """moin_kv_tables_reset: every request forgotten, every page free."""
-        _check(lib().moin_kv_tables_reset(self.ref, _stream(stream)), "moin_kv_tables_reset")
+        _check(lib().moin_kv_tables_reset(ctypes.byref(self.c), _stream(stream)), "moin_kv_tables_reset")
 
 
 class KvBatch:
@@ -670,53 +689,20 @@ class KvBatch:
         self.R, self.T = R, T
         self.cu_q, self.kv_len, self.slot, self.pos, self.refused = i32(R + 1), i32(R), i32(T), i32(T), i32(1)
         self.c = _KvBatch(R, T, *[_ptr(t) for t in (self.cu_q, self.kv_len, self.slot, self.pos, self.refused)])
-        self.ref = ctypes.byref(self.c)
+        self.addr = ctypes.addressof(self.c)
 
 
-# These checks stand before every step of a generation loop: few attribute reads, each costs a tenth of a microsecond.
-_bf16, _int32, _fp32 = torch.bfloat16, torch.int32, torch.float32
-
-
-def _i32(t: torch.Tensor, n: int) -> int:
-    """Address of an int32 vector of n entries."""
-    if t.dtype is not _int32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
-        raise MoinError(f"expected {n} contiguous int32 values on a CUDA device, got {tuple(t.shape)} of {t.dtype} on {t.device}")
-    return t.data_ptr()
+def _handle(stream) -> Optional[int]:
+    return None if stream is None else stream.cuda_stream
 
 
 def kv_update(tables: KvTables, want: torch.Tensor, batch: KvBatch, rows: Optional[torch.Tensor] = None,
               lens_out: Optional[torch.Tensor] = None, n_free_out: Optional[torch.Tensor] = None, stream=None) -> KvBatch:
     """moin_kv_update: request i (row ``rows[i]`` of the tables, or i) becomes ``want[i]`` tokens long.  Returns ``batch``."""
-    R = batch.R
-    st = lib().moin_kv_update(tables.ref, None if rows is None else _i32(rows, R), _i32(want, R), batch.ref,
-                              None if lens_out is None else _i32(lens_out, tables.n_rows),
-                              None if n_free_out is None else _i32(n_free_out, 1), _stream(stream))
+    st = (_steps or _load_steps()).update(tables.addr, batch.addr, rows, want, lens_out, n_free_out, _handle(stream))
     if st:
         _check(st, "moin_kv_update")
     return batch
-
-
-def _tokens_ptr(t: torch.Tensor, T: int, heads: int, head_dim: int) -> tuple:
-    """(address, elements between tokens) of [T, heads, head_dim] bf16 (or [T, heads * head_dim]) whose tokens may lie apart."""
-    if t.dtype is not _bf16 or t.numel() != T * heads * head_dim or not t.is_cuda or t.shape[0] != T:
-        raise MoinError(f"expected bf16 [{T}, {heads}, {head_dim}] on a CUDA device, got {tuple(t.shape)} of {t.dtype} on {t.device}")
-    if t.is_contiguous():
-        return t.data_ptr(), heads * head_dim
-    if t.dim() == 3:
-        if t.shape[1] != heads or t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
-            raise MoinError("the heads of a token must lie side by side")
-    elif t.dim() != 2 or t.stride(1) != 1:
-        raise MoinError("the heads of a token must lie side by side")
-    return t.data_ptr(), (t.stride(0) if T > 1 else heads * head_dim)
-
-
-def _rope_arg(rope: Optional[torch.Tensor], head_dim: int) -> tuple:
-    if rope is None:
-        return None, 0
-    n, more = divmod(rope.numel(), head_dim)
-    if rope.dtype is not _fp32 or more or not rope.is_contiguous() or not rope.is_cuda:
-        raise MoinError(f"expected a float32 table [positions, {head_dim // 2}, 2] on a CUDA device, got {tuple(rope.shape)} of {rope.dtype}")
-    return rope.data_ptr(), n
 
 
 def rope_table(n_pos: int, head_dim: int, base: float, device, stream=None) -> torch.Tensor:
@@ -728,26 +714,16 @@ def rope_table(n_pos: int, head_dim: int, base: float, device, stream=None) -> t
 
 def kv_append(cache: KvCache, slot: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: Optional[torch.Tensor] = None,
               rope: Optional[torch.Tensor] = None, stream=None) -> None:
-    """moin_kv_append: quantise row t of ``k`` (rotated by ``rope`` at ``pos[t]`` if given) and ``v`` and store them in ``slot[t]``."""
-    T = slot.shape[0]
-    kp, ks = _tokens_ptr(k, T, cache.n_kv_heads, cache.head_dim)
-    vp, vs = _tokens_ptr(v, T, cache.n_kv_heads, cache.head_dim)
-    rp, rn = _rope_arg(rope, cache.head_dim)
-    st = lib().moin_kv_append(cache.ref, _i32(slot, T), kp, ks, vp, vs, None if pos is None else _i32(pos, T), rp, rn, T, _stream(stream))
+    """moin_kv_append: quantise row t of ``k`` (rotated by ``rope`` at ``pos[t]`` if given) and ``v`` and store them in ``slot[t]``.
+    k and v: bf16 [T, n_kv_heads, head_dim] or [T, n_kv_heads * head_dim], tokens may lie apart."""
+    st = (_steps or _load_steps()).append(cache.addr, slot, k, v, pos, rope, _handle(stream))
     if st:
         _check(st, "moin_kv_append")
 
 
 def kv_read(cache: KvCache, slot: torch.Tensor, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None, stream=None) -> tuple:
     """moin_kv_read: (k, v), bf16 [T, n_kv_heads, head_dim], of what the slots hold."""
-    T, H, D = slot.shape[0], cache.n_kv_heads, cache.head_dim
-    if k is None:
-        k = torch.empty(T, H, D, dtype=torch.bfloat16, device=slot.device)
-    if v is None:
-        v = torch.empty_like(k) if k.is_contiguous() else torch.empty(T, H, D, dtype=torch.bfloat16, device=slot.device)
-    kp, ks = _tokens_ptr(k, T, H, D)
-    vp, vs = _tokens_ptr(v, T, H, D)
-    st = lib().moin_kv_read(cache.ref, _i32(slot, T), kp, ks, vp, vs, T, _stream(stream))
+    st, k, v = (_steps or _load_steps()).read(cache.addr, slot, k, v, _handle(stream))
     if st:
         _check(st, "moin_kv_read")
     return k, v
@@ -757,29 +733,9 @@ def kv_attention(cache: KvCache, tables: KvTables, q: torch.Tensor, cu_q: torch.
                  max_kv: int = 0, rows: Optional[torch.Tensor] = None, scale: Optional[float] = None,
                  rope: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """moin_kv_attention: q [T, n_heads, head_dim] over the cached tokens of each token's request.  Returns out, like q; rows of a new
-    ``out`` behind the last request are undefined."""
-    T, n_heads, D = q.shape
-    R = kv_len.shape[0]
-    qp, qs = _tokens_ptr(q, T, n_heads, cache.head_dim)
-    if out is None:
-        out = torch.empty(T, n_heads, D, dtype=torch.bfloat16, device=q.device)
-        op, os_ = out.data_ptr(), n_heads * D
-    else:
-        op, os_ = _tokens_ptr(out, T, n_heads, D)
-    rp, rn = _rope_arg(rope, D)
-    max_q = T if max_q < 1 or max_q > T else max_q
-    L, s = lib(), _stream(stream)
-    n = cache.ws_bytes.get((max_q, n_heads))
-    if n is None:
-        if len(cache.ws_bytes) >= 1024:
-            cache.ws_bytes.clear()
-        n = cache.ws_bytes[max_q, n_heads] = L.moin_kv_attention_workspace_bytes(max_q, n_heads, cache.n_kv_heads, D)
-    ws = _scratch_alloc(n, s)
-    try:
-        st = L.moin_kv_attention(cache.ref, tables.ref, None if rows is None else _i32(rows, R), _i32(cu_q, R + 1), _i32(kv_len, R), R, T, max_q,
-                                 max_kv, qp, qs, n_heads, D ** -0.5 if scale is None else scale, rp, rn, op, os_, ws, n, s)
-    finally:
-        _scratch_free(ws)
+    ``out`` behind the last request are undefined.  scale: 1 / sqrt(head_dim) unless given.  The scratch comes from the caching
+    allocator and is this call's alone: calls, streams and captured graphs may overlap."""
+    st, out = (_steps or _load_steps()).attention(cache.addr, tables.addr, q, cu_q, kv_len, max_q, max_kv, rows, scale, rope, out, _handle(stream))
     if st:
         _check(st, "moin_kv_attention")
     return out
@@ -804,22 +760,26 @@ def decoder_forward_cached(model: DecoderModel, tokens: torch.Tensor, layers: Kv
     if len(layers.caches) != cfg.n_layers:
         raise MoinError(f"{len(layers.caches)} caches for {cfg.n_layers} layers")
     for t, shape in ((hidden_in, (T, cfg.hidden)), (hidden_out, (T, cfg.hidden))):
-        if t is not None and (t.dtype is not _fp32 or t.shape != shape):
+        if t is not None and (t.dtype != torch.float32 or t.shape != shape):
             raise MoinError(f"expected float32 {shape}, got {tuple(t.shape)} of {t.dtype}")
     if logits_mode != LOGITS_NONE:
         shape = (T if logits_mode == LOGITS_ALL else R, cfg.vocab)
         if logits is None:
             logits = torch.empty(*shape, dtype=torch.bfloat16, device=tokens.device)
-        elif logits.dtype is not _bf16 or logits.shape != shape:
+        elif logits.dtype != torch.bfloat16 or logits.shape != shape:
             raise MoinError(f"expected bf16 {shape}, got {tuple(logits.shape)} of {logits.dtype}")
     taps = _Taps(_ptr(hidden_in), _ptr(hidden_out), layer_begin, cfg.n_layers if layer_end is None else layer_end)
-    rp, rn = _rope_arg(rope, cfg.head_dim)
+    if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[1:] != (cfg.head_dim // 2, 2):
+        raise MoinError(f"expected a float32 table [positions, {cfg.head_dim // 2}, 2], got {tuple(rope.shape)} of {rope.dtype}")
+    for t, n in ((tokens, T), (rows, R), (req_expert, R)):
+        if t is not None and (t.dtype != torch.int32 or t.shape != (n,)):
+            raise MoinError(f"expected {n} int32 values, got {tuple(t.shape)} of {t.dtype}")
     s = _stream(stream)
     n = lib().moin_decoder_cached_workspace_bytes(ctypes.byref(model.c), R, T, max_q)
     ws = workspace.data_ptr() if workspace is not None else _scratch_alloc(n, s)
     try:
-        st = lib().moin_decoder_forward_cached(ctypes.byref(model.c), _i32(tokens, T), layers.c, tables.ref, None if rows is None else _i32(rows, R),
-                                               batch.ref, None if req_expert is None else _i32(req_expert, R), max_q, max_kv, rp, rn, _ptr(logits),
+        st = lib().moin_decoder_forward_cached(ctypes.byref(model.c), _ptr(tokens), layers.c, ctypes.byref(tables.c), _ptr(rows),
+                                               ctypes.byref(batch.c), _ptr(req_expert), max_q, max_kv, _ptr(rope), rope.shape[0], _ptr(logits),
                                                logits_mode, ctypes.byref(taps), ws, n if workspace is None else workspace.numel(), s)
     finally:
         if workspace is None:

@@ -10,6 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmoin.so")
+STEPS = os.path.join(HERE, "_steps.so")   # Python extension: marshalling of the calls of a generation loop
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "-Xcompiler", "-fPIC", "-Xptxas", "-v"] + os.environ.get("MOIN_EXTRA_NVCC_FLAGS", "").split()
@@ -54,7 +55,28 @@ def build(force: bool = False, verbose: bool = False) -> str:
         tmp = LIB + f".tmp{os.getpid()}"
         subprocess.check_call([NVCC, "-shared", "-Wno-deprecated-gpu-targets", "-o", tmp] + objs + ["-lcudart"])
         os.replace(tmp, LIB)
+    build_steps(force)
     return LIB
+
+
+def build_steps(force: bool = False) -> str:
+    src = os.path.join(CSRC, "steps.cpp")
+    if not force and not _stale(STEPS, [src, os.path.join(os.path.dirname(HERE), "include", "moin.h")]):
+        return STEPS
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"],
+           os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include")]
+    tmp = STEPS + f".tmp{os.getpid()}"
+    p = subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] +
+                       [f"-isystem{d}" for d in inc] + [src, "-o", tmp, "-L" + os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu",
+                                                        "-ltorch_python"], capture_output=True, text=True)
+    if p.returncode != 0:
+        raise RuntimeError(f"g++ failed for {src}:\n{p.stdout}\n{p.stderr}")
+    os.replace(tmp, STEPS)
+    return STEPS
 
 
 if __name__ == "__main__":

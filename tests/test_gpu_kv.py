@@ -473,6 +473,45 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(big, one)
 
 
+def test_calls_with_other_tensors_are_refused():
+    """Types, shapes, places and orders that the calls do not take: an error before anything is launched."""
+    T, H, D = 5, 2, 64
+    cache, tables = moin.KvCache.empty(3, 16, H, D, DEV), moin.KvTables.empty(2, 2, 3, 16, DEV)
+    batch, rope = moin.KvBatch(2, T, DEV), moin.rope_table(32, D, 1e4, DEV)
+    want = i32([3, 2])
+    k = torch.zeros(T, H, D, dtype=torch.bfloat16, device=DEV)
+    q, cu = torch.zeros(T, 4, D, dtype=torch.bfloat16, device=DEV), i32([0, 3, 5])
+    moin.kv_update(tables, want, batch)
+    slot, pos = batch.slot.clone(), batch.pos.clone()
+    moin.kv_append(cache, slot, k, k, pos=pos, rope=rope)
+    good = moin.kv_attention(cache, tables, q, cu, want, rope=rope)
+    assert good.shape == q.shape
+    bad = [lambda: moin.kv_update(tables, want.long(), batch), lambda: moin.kv_update(tables, want[:1], batch), lambda: moin.kv_update(tables, want.cpu(), batch),
+           lambda: moin.kv_update(tables, want, batch, rows=i32([0])), lambda: moin.kv_update(tables, want, batch, lens_out=i32([0])),
+           lambda: moin.kv_update(tables, want, batch, n_free_out=i32([0, 0])), lambda: moin.kv_update(tables, torch.stack([want, want], 1)[:, 0], batch),
+           lambda: moin.kv_update(tables, [3, 2], batch),
+           lambda: moin.kv_append(cache, slot, k.float(), k), lambda: moin.kv_append(cache, slot, k, k[:4]), lambda: moin.kv_append(cache, slot, k, k.cpu()),
+           lambda: moin.kv_append(cache, slot, k.transpose(0, 1).contiguous().transpose(0, 1), k), lambda: moin.kv_append(cache, slot, k, k.view(T, D, H)),
+           lambda: moin.kv_append(cache, slot.short(), k, k), lambda: moin.kv_append(cache, slot, k, k, pos=pos[:4], rope=rope),
+           lambda: moin.kv_append(cache, slot, k, k, rope=rope), lambda: moin.kv_append(cache, slot, k, k, pos=pos, rope=rope.bfloat16()),
+           lambda: moin.kv_append(cache, slot, k, k, pos=pos, rope=rope[:, :16]), lambda: moin.kv_append(cache, slot, torch.zeros(T, H + 1, D + 4, dtype=torch.bfloat16, device=DEV)[:, :H, :D], k),
+           lambda: moin.kv_read(cache, slot.cpu()), lambda: moin.kv_read(cache, slot, k=k.half()), lambda: moin.kv_read(cache, slot, v=k[:2]),
+           lambda: moin.kv_attention(cache, tables, q.float(), cu, want), lambda: moin.kv_attention(cache, tables, q.view(T, -1), cu, want),
+           lambda: moin.kv_attention(cache, tables, q[:, :3].contiguous(), cu, want), lambda: moin.kv_attention(cache, tables, q, cu[:2], want),
+           lambda: moin.kv_attention(cache, tables, q, cu, want.long()), lambda: moin.kv_attention(cache, tables, q, cu, want, rows=i32([0, 1, 0])),
+           lambda: moin.kv_attention(cache, tables, q, cu, want, out=q[:3]), lambda: moin.kv_attention(cache, tables, q, cu, want, out=q.float()),
+           lambda: moin.kv_attention(cache, tables, q, cu, want, rope=rope[:31].contiguous()),
+           lambda: moin.kv_attention(cache, moin.KvTables.empty(2, 2, 3, 32, DEV), q, cu, want)]
+    for i, call in enumerate(bad):
+        with pytest.raises(moin.MoinError):
+            call()
+            pytest.fail(f"call {i} went through")
+    assert torch.equal(moin.kv_attention(cache, tables, q, cu, want, rope=rope), good)
+    # nothing to do: no tokens, no requests
+    moin.kv_append(cache, slot[:0], k[:0], k[:0])
+    assert moin.kv_read(cache, slot[:0])[0].shape == (0, H, D) and moin.kv_attention(cache, tables, q[:0], i32([0]), want[:0]).shape == (0, 4, D)
+
+
 # ------------------------------------------------------------------------------------------------------------ together
 def _steps(rng, R, page):
     """Wanted lengths of a few steps: prompts of which one comes late, tokens one by one, a request that ends, its row reused."""
