@@ -32,6 +32,8 @@ constexpr int kKvItemCost = 8;       // what beginning an item costs, in tiles
 constexpr float kKvTop = 10.f;       // log2 of the largest weight after a rescale
 constexpr float kKvMost = 15.f;      // log2 of the largest weight at all
 
+// Who takes what: a CTA an item; warps equal shares of all items; or, of one request, each of gridDim.x CTAs its part of each item.
+enum { KV_WHOLE = 0, KV_SHARES = 1, KV_CUT = 2 };
 struct KvAttParams {
   KvView kv;
   const int *table, *rows, *cu_q, *kv_len;
@@ -45,7 +47,7 @@ struct KvAttParams {
   long long q_stride, out_stride;
   const float2* rope;      // [rope_len, D / 2] or nullptr
   float scale_log2;
-  int split;               // items are cut: CTAs take equal shares of all tiles (else a CTA takes an item)
+  int split;               // KV_WHOLE, KV_SHARES, KV_CUT
   float* part;             // [worker][2][row][64 P + 4]: sums of items that several workers share
   int4* desc;              // [CTA][2]: the item that it begins without ending it (head, first row, first token, CTAs behind), its rows
 };
@@ -493,18 +495,20 @@ kv_attention_kernel(const KvAttParams p) {
   const int tpp = 1 << p.tpp_log2;
   KvShare share;
   long long run = 1;
-  if (p.split) {
+  if (p.split == KV_SHARES) {
     run = kv_share<NT, U>(p, s_sum, s_share);
     share = s_share[warp];
-  } else {   // the CTA's item in four
-    const int n = kv_count(p.kv_len[blockIdx.z], p.max_kv) - kKvItemCost;
-    share = {(long long)(n * warp / kKvAttWarps), (long long)(n * (warp + 1) / kKvAttWarps), 0, (int)blockIdx.z};
+  } else {   // the warp's part of the item
+    const int req = p.split == KV_CUT ? 0 : blockIdx.z, warps = p.split == KV_CUT ? kKvAttWarps * gridDim.x : kKvAttWarps;
+    const long long n = kv_count(p.kv_len[req], p.max_kv) - kKvItemCost;
+    const int w = (p.split == KV_CUT ? blockIdx.x * kKvAttWarps : 0) + warp;
+    share = {n * w / warps, n * (w + 1) / warps, 0, req};
   }
   while (share.at < share.end) {
     // ---- the piece: tiles tile0 .. tile1 of an item of n_tiles
     KvItem it;
     int tile0, tile1, left;
-    if (p.split) {
+    if (p.split == KV_SHARES) {
       long long c = kv_cost(p, share.req, kRows);
       while (share.at >= share.base + c) {
         share.base += c;
@@ -521,10 +525,11 @@ kv_attention_kernel(const KvAttParams p) {
       const int block = item / p.kv.H;
       it = kv_item(p, share.req, item - block * p.kv.H, block * kRows);
     } else {
-      it = kv_item(p, blockIdx.z, blockIdx.y, blockIdx.x * kRows);
+      const int block = p.split == KV_CUT ? blockIdx.z : blockIdx.x;
+      it = kv_item(p, share.req, blockIdx.y, block * kRows);
       tile0 = (int)share.at;
       tile1 = (int)share.end;
-      left = kv_count(p.kv_len[blockIdx.z], p.max_kv) - kKvItemCost - tile1;
+      left = kv_count(p.kv_len[share.req], p.max_kv) - kKvItemCost - tile1;
       share.at = share.end;
     }
     const int n_rows = it.q_len * p.G;
@@ -608,7 +613,7 @@ kv_attention_kernel(const KvAttParams p) {
     }
     // ---- the rows to shared memory: the ring is idle, a piece to be joined with the warp before has its own place
     __syncwarp();
-    const bool inside = tile0 > 0, whole = !inside && left == 0;
+    const bool inside = tile0 > 0, whole = !inside && left == 0 && p.split != KV_CUT;
     float* rows = reinterpret_cast<float*>(ring + (inside ? kRing : 0));
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -655,13 +660,14 @@ kv_attention_kernel(const KvAttParams p) {
   }
   __syncthreads();
   // ---- pieces of the CTA's warps, in order, a thread for four channels of a row
-  float* part = p.part + (size_t)blockIdx.x * 2 * kRows * kPitch;
+  const size_t cta = p.split == KV_CUT ? ((size_t)blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x : blockIdx.x;
+  float* part = p.part + cta * 2 * kRows * kPitch;
   int4 open_item = make_int4(0, 0, 0, 0);   // of an item that this CTA begins and does not end: head, first row, t0 | rows, CTAs behind
   int open_rows = 0;
 #pragma unroll 1
   for (int i = threadIdx.x; i < kRows * kCh / 4; i += 32 * kKvAttWarps) {
     const int row = i / (kCh / 4), ch = 4 * (i % (kCh / 4));
-    KvSum sum = {0.f, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    KvSum sum = {-FLT_MAX, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
     KvPiece d = {0, 0, 0, 0, -1};
     bool open = false, outside = false;   // the item began in a CTA before
     auto leave = [&](int slot) {
@@ -676,6 +682,10 @@ kv_attention_kernel(const KvAttParams p) {
       const float* src = reinterpret_cast<const float*>(smem + (k >> 1) * (kRing + kPiece) + ((k & 1) ? 0 : kRing)) + row * kPitch;
       const float2 ml = *reinterpret_cast<const float2*>(src + kCh);
       const float4 v = *reinterpret_cast<const float4*>(src + ch);
+      if (p.split == KV_CUT) {   // everything belongs to one item
+        sum.add(ml.x, ml.y, v);
+        continue;
+      }
       if (!open) {
         sum = {ml.x, ml.y, v};
         outside = (k & 1) == 0;
@@ -690,6 +700,7 @@ kv_attention_kernel(const KvAttParams p) {
         else if (d.row0 + row < d.n_rows) *reinterpret_cast<uint2*>(kv_out(p, d.t0, d.head, d.row0 + row, ch, kCh)) = sum.result();
       }
     }
+    if (p.split == KV_CUT) leave(0);
     if (open) {
       leave(outside ? 0 : 1);
       if (!outside) {
@@ -698,30 +709,40 @@ kv_attention_kernel(const KvAttParams p) {
       }
     }
   }
-  if (p.split && threadIdx.x == 0) {
+  if (p.split == KV_SHARES && threadIdx.x == 0) {
     p.desc[blockIdx.x * 2] = open_item;
     p.desc[blockIdx.x * 2 + 1].x = open_rows;
   }
 }
 
-// Items that several CTAs share: CTA (w, y) looks at the item that CTA w begins without ending it, and adds up, for some of its
-// rows, that piece (slot 1) and those of the CTAs behind (slot 0).  Bound by latency: the chain item, pieces, result.
+// Items that several CTAs share.  KV_SHARES: CTA (w, y) looks at the item that CTA w begins without ending it, and adds up, for ROWS
+// of its rows, that piece (slot 1) and those of the CTAs behind (slot 0).  KV_CUT: CTA (head, block, y) adds up the item's `cuts`
+// pieces (slot 0).  Bound by latency: the chain item, pieces, result.
 // SETS = 1: a thread for four channels of every row walks the pieces (most items have two: a step of 256 requests spends 3 us
-// less here than with sets).  Few long items of many pieces: CTAs of two rows, whose sets of threads take a run of pieces each.
-template <int P, int NT, int SETS>
-__global__ void __launch_bounds__(SETS == 1 ? 128 * P * NT : 256)
-kv_join_kernel(const KvAttParams p) {
-  constexpr int kRows = 8 * NT, kCh = 64 * P, kPitch = kCh + 4, kThreads = SETS == 1 ? kRows * kCh / 4 : 2 * kCh / 4, kAhead = SETS == 1 ? 2 : 6;
+// less here than with sets).  Few long items of many pieces: several sets of threads take a run of pieces each.
+template <int P, int NT, int ROWS, int SETS>
+__global__ void __launch_bounds__(ROWS * 16 * P * SETS)
+kv_join_kernel(const KvAttParams p, int cuts) {
+  constexpr int kRows = 8 * NT, kCh = 64 * P, kPitch = kCh + 4, kThreads = ROWS * kCh / 4, kAhead = SETS == 1 ? 2 : 6;
   __shared__ float4 s_acc[SETS][SETS == 1 ? 1 : kThreads];
-  __shared__ float2 s_ml[SETS][2];
+  __shared__ float2 s_ml[SETS][ROWS];
   pdl_begin();
-  const int w0 = blockIdx.x;
-  const int4 d = p.desc[w0 * 2];
-  const int n_rows = p.desc[w0 * 2 + 1].x;
   const int set = SETS == 1 ? 0 : threadIdx.x / kThreads, e = threadIdx.x % kThreads;
-  const int row = blockIdx.y * 2 + e / (kCh / 4), ch = 4 * (e % (kCh / 4)), r = d.y + row;
-  if (d.w == 0 || d.y + (int)blockIdx.y * 2 >= n_rows) return;
-  const int n = d.w + 1;   // pieces
+  const int row_at = e / (kCh / 4), ch = 4 * (e % (kCh / 4));
+  int head, row0, t0, n_rows, n, y;   // of the item; its pieces; which rows
+  size_t first;
+  if (p.split == KV_CUT) {
+    const KvItem it = kv_item(p, 0, blockIdx.x, blockIdx.y * kRows);
+    head = it.head; row0 = it.row0; t0 = it.t0; n_rows = it.q_len * p.G; n = cuts; y = blockIdx.z;
+    first = ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * cuts;
+  } else {
+    const int4 d = p.desc[blockIdx.x * 2];
+    n_rows = p.desc[blockIdx.x * 2 + 1].x;
+    head = d.x; row0 = d.y; t0 = d.z; n = d.w == 0 ? 0 : d.w + 1; y = blockIdx.y;
+    first = blockIdx.x;
+  }
+  if (n == 0 || row0 + y * ROWS >= n_rows) return;
+  const int row = y * ROWS + row_at, r = row0 + row;
   // (each set of threads takes a run of pieces: the order of the sums is that of the tokens)
   const int sets = min(n, SETS), i0 = set < sets ? n * set / sets : 0, i1 = set < sets ? n * (set + 1) / sets : 0;
   KvSum sum = {-FLT_MAX, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
@@ -731,7 +752,7 @@ kv_join_kernel(const KvAttParams p) {
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
       if (i + k < i1) {
-        const float* part = p.part + ((size_t)(w0 + i + k) * 2 + (i + k == 0 ? 1 : 0)) * kRows * kPitch + row * kPitch;
+        const float* part = p.part + ((first + i + k) * 2 + (i + k == 0 && p.split == KV_SHARES ? 1 : 0)) * kRows * kPitch + row * kPitch;
         ml[k] = *reinterpret_cast<const float2*>(part + kCh);
         v[k] = *reinterpret_cast<const float4*>(part + ch);
       }
@@ -742,13 +763,13 @@ kv_join_kernel(const KvAttParams p) {
   if (SETS > 1) {
     if (set > 0 && set < sets) {
       s_acc[set][e] = sum.v;
-      if (ch == 0) s_ml[set][e / (kCh / 4)] = make_float2(sum.m, sum.l);
+      if (ch == 0) s_ml[set][row_at] = make_float2(sum.m, sum.l);
     }
     __syncthreads();
     if (set != 0) return;
-    for (int i = 1; i < sets; ++i) sum.add(s_ml[i][e / (kCh / 4)].x, s_ml[i][e / (kCh / 4)].y, s_acc[i][e]);
+    for (int i = 1; i < sets; ++i) sum.add(s_ml[i][row_at].x, s_ml[i][row_at].y, s_acc[i][e]);
   }
-  if (r < n_rows) *reinterpret_cast<uint2*>(kv_out(p, d.z, d.x, r, ch, kCh)) = sum.result();
+  if (r < n_rows) *reinterpret_cast<uint2*>(kv_out(p, t0, head, r, ch, kCh)) = sum.result();
 }
 
 template <int P, int NT, int U>
@@ -762,10 +783,10 @@ static moin_status kv_att_launch(HostState* hs, int optin, KvAttParams& p, cudaS
   const size_t smem = kv_att_smem<P, NT, U>();
   cudaError_t e = ensure_smem_optin(optin, kv_attention_kernel<P, NT, U>, smem);
   if (e != cudaSuccess) return record_cuda(e);
-  const long long blocks = ((long long)p.max_q * p.G + 8 * NT - 1) / (8 * NT);
-  p.split = p.max_kv > 256;
-  ProfScope prof(MOIN_K_KV_ATTENTION, p.split ? 2 : 1, s);
-  if (!p.split)
+  const long long blocks = ((long long)p.max_q * p.G + 8 * NT - 1) / (8 * NT), items = blocks * p.kv.H * p.R;
+  p.split = p.max_kv <= 256 ? KV_WHOLE : p.R == 1 && blocks <= 65535 ? KV_CUT : KV_SHARES;
+  ProfScope prof(MOIN_K_KV_ATTENTION, p.split == KV_WHOLE ? 1 : 2, s);
+  if (p.split == KV_WHOLE)
     return record_cuda(launch_pdl(kv_attention_kernel<P, NT, U>, dim3((unsigned)blocks, (unsigned)p.kv.H, (unsigned)p.R), 32 * kKvAttWarps, smem, s, p));
   static int per_sm = 0;   // (the same on every device this library runs on)
   if (per_sm == 0) {
@@ -773,15 +794,24 @@ static moin_status kv_att_launch(HostState* hs, int optin, KvAttParams& p, cudaS
     if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kv_attention_kernel<P, NT, U>, 32 * kKvAttWarps, smem)) != cudaSuccess) return record_cuda(e);
     per_sm = n < 1 ? 1 : n;
   }
-  // no more CTAs than there can be shares
-  const long long most = ((p.max_kv + kKvTile - 1) / kKvTile + kKvItemCost) * blocks * p.kv.H * p.R / (kKvAttWarps * (kKvItemCost + 2 * U)) + 1;
   long long workers = (long long)per_sm * hs->n_sms;
   if (workers > kKvMaxWorkers) workers = kKvMaxWorkers;
+  const int tiles = (p.max_kv + kKvTile - 1) / kKvTile;
+  if (p.split == KV_CUT && items <= workers) {   // of one request all items are alike: no places to be found, no more joins than items
+    long long cuts = workers / items, most = (tiles + kKvAttWarps * U - 1) / (kKvAttWarps * U);
+    if (cuts > most) cuts = most;
+    e = launch_pdl(kv_attention_kernel<P, NT, U>, dim3((unsigned)cuts, (unsigned)p.kv.H, (unsigned)blocks), 32 * kKvAttWarps, smem, s, p);
+    if (e != cudaSuccess) return record_cuda(e);
+    return record_cuda(launch_pdl(kv_join_kernel<P, NT, 1, 16 / P>, dim3((unsigned)p.kv.H, (unsigned)blocks, 8 * NT), 256, 0, s, p, (int)cuts));
+  }
+  p.split = KV_SHARES;
+  // no more CTAs than there can be shares
+  const long long most = (long long)(tiles + kKvItemCost) * items / (kKvAttWarps * (kKvItemCost + 2 * U)) + 1;
   if (workers > most) workers = most;
   e = launch_pdl(kv_attention_kernel<P, NT, U>, (unsigned)workers, 32 * kKvAttWarps, smem, s, p);
   if (e != cudaSuccess) return record_cuda(e);
-  if (workers > 8 * blocks * p.kv.H * p.R) e = launch_pdl(kv_join_kernel<P, NT, 8 / P>, dim3((unsigned)workers, 4 * NT), 256, 0, s, p);
-  else e = launch_pdl(kv_join_kernel<P, NT, 1>, (unsigned)workers, 128 * P * NT, 0, s, p);
+  if (workers > 8 * items) e = launch_pdl(kv_join_kernel<P, NT, 2, 8 / P>, dim3((unsigned)workers, 4 * NT), 256, 0, s, p, 0);
+  else e = launch_pdl(kv_join_kernel<P, NT, 8 * NT, 1>, (unsigned)workers, 128 * P * NT, 0, s, p, 0);
   return record_cuda(e);
 }
 

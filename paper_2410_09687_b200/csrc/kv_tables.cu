@@ -118,6 +118,7 @@ kv_update_kernel(const KvTabParams p) {
     s_row[tid] = q.row;
     s_at[tid] = need - (inc - back);   // k-th page given back by the chunk, of this request: its table entry s_at + k
     __syncthreads();
+#pragma unroll 4
     for (int k = tid; k < (int)sum[0]; k += THREADS) {
       const int i = first_above(s_inc, THREADS, k);
       if (top + k < p.n_pages) p.stack[top + k] = p.table[(size_t)s_row[i] * p.max_pages + s_at[i] + k];
@@ -168,6 +169,7 @@ kv_update_kernel(const KvTabParams p) {
     if (ok && ask > 0) atomicMax(&s_got, (int)upto);
     __syncthreads();
     const int got = s_got;
+#pragma unroll 4
     for (int k = taken + tid; k < got; k += THREADS) {
       const int j = first_above(s_inc, THREADS, k);
       p.table[(size_t)s_row[j] * p.max_pages + s_at[j] + k] = p.stack[top - 1 - k];
