@@ -784,10 +784,6 @@ static moin_status kv_att_launch(HostState* hs, int optin, KvAttParams& p, cudaS
   cudaError_t e = ensure_smem_optin(optin, kv_attention_kernel<P, NT, U>, smem);
   if (e != cudaSuccess) return record_cuda(e);
   const long long blocks = ((long long)p.max_q * p.G + 8 * NT - 1) / (8 * NT), items = blocks * p.kv.H * p.R;
-  p.split = p.max_kv <= 256 ? KV_WHOLE : p.R == 1 && blocks <= 65535 ? KV_CUT : KV_SHARES;
-  ProfScope prof(MOIN_K_KV_ATTENTION, p.split == KV_WHOLE ? 1 : 2, s);
-  if (p.split == KV_WHOLE)
-    return record_cuda(launch_pdl(kv_attention_kernel<P, NT, U>, dim3((unsigned)blocks, (unsigned)p.kv.H, (unsigned)p.R), 32 * kKvAttWarps, smem, s, p));
   static int per_sm = 0;   // (the same on every device this library runs on)
   if (per_sm == 0) {
     int n = 0;
@@ -795,6 +791,19 @@ static moin_status kv_att_launch(HostState* hs, int optin, KvAttParams& p, cudaS
     per_sm = n < 1 ? 1 : n;
   }
   long long workers = (long long)per_sm * hs->n_sms;
+  // A CTA per item needs neither places nor joins: 3 to 5 us less, until the longest item outlasts that.  One token each for R requests
+  // of at most 256, 512, 1024, 1536 tokens, in us, whole items / shares:
+  //   heads 32 of 64, 4 kv heads    R = 4    5.8 / 11.7    7.2 / 11.9    9.6 / 11.9   12.3 / 12.3
+  //                                 R = 64   6.6 / 12.9    8.3 / 13.3   11.3 / 16.0   14.3 / 17.7
+  //                                 R = 256 14.4 / 17.0   19.4 / 20.3   27.7 / 27.7   36.9 / 35.4   (1.7 waves of items)
+  //   heads 32 of 128, 8 kv heads   R = 64  16.2 / 19.3   20.7 / 20.7   27.8 / 26.8   37.2 / 34.0   (1.2 waves)
+  //                                 R = 256 42.3 / 29.8   60.0 / 43.8   83.2 / 67.2  106.3 / 90.4   (4.6 waves)
+  //   one request, whole / cut                5.7 / 6.9     7.0 / 7.0     9.1 / 7.1   11.6 / 7.3
+  const int longest = p.R == 1 ? 512 : items <= workers ? 1536 : items <= 2 * workers ? 512 : 0;
+  p.split = p.max_kv <= longest && blocks <= 0x7FFFFFFF ? KV_WHOLE : p.R == 1 && blocks <= 65535 ? KV_CUT : KV_SHARES;
+  ProfScope prof(MOIN_K_KV_ATTENTION, p.split == KV_WHOLE ? 1 : 2, s);
+  if (p.split == KV_WHOLE)
+    return record_cuda(launch_pdl(kv_attention_kernel<P, NT, U>, dim3((unsigned)blocks, (unsigned)p.kv.H, (unsigned)p.R), 32 * kKvAttWarps, smem, s, p));
   if (workers > kKvMaxWorkers) workers = kKvMaxWorkers;
   const int tiles = (p.max_kv + kKvTile - 1) / kKvTile;
   if (p.split == KV_CUT && items <= workers) {   // of one request all items are alike: no places to be found, no more joins than items
