@@ -541,9 +541,11 @@ moin_status moin_rope_table(float* table, int32_t n_pos, int32_t head_dim, float
  * A query that sees nothing (kv_len 0, a position before the first) gets zeros; so do the queries of a request whose row or kv_len is
  * out of range.  A page id outside [0, n_pages) hides its tokens.  Rows of out behind cu_q[R] stay as they were.  fp32 scores, softmax and
  * sums; the un-normalised weights times the value's scale enter the second product rounded to fp16, relative to the row's largest.
- * Scratch: workspace, moin_kv_attention_workspace_bytes(max_q, ...) bytes with max_q at most T, 16-byte aligned, of this call alone while it runs.
+ * Scratch: workspace, moin_kv_attention_workspace_bytes(...) bytes with the bounds that the call goes by (up to about 1 GiB where long
+ * chunks attend to long requests: keys and values are then laid out in 16 bits for the tensor cores), 16-byte aligned, of this call alone while it runs.
  * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED, WORKSPACE.  R == 0 or T == 0 is a no-op. */
-size_t moin_kv_attention_workspace_bytes(int32_t max_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+size_t moin_kv_attention_workspace_bytes(int32_t R, int32_t T, int32_t max_q, int32_t max_kv, int32_t n_heads, int32_t n_kv_heads,
+                                         int32_t head_dim);
 moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables* tables, const int32_t* rows, const int32_t* cu_q,
                               const int32_t* kv_len, int32_t R, int32_t T, int32_t max_q, int32_t max_kv, const void* q,
                               int64_t q_stride, int32_t n_heads, float scale, const float* rope, int32_t rope_len, void* out,
@@ -560,9 +562,9 @@ moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables* tables, c
  *   max_q, max_kv   host upper bounds as for moin_kv_attention
  *   logits     [batch->T, vocab] or [R, vocab], as logits_mode says (MOIN_LOGITS_LAST: zeros for a request without new tokens)
  * Reads nothing back; can be captured together with moin_kv_update.  workspace: 256-byte aligned,
- * moin_decoder_cached_workspace_bytes(...) bytes.  Errors: as for moin_decoder_forward and moin_kv_attention, before anything
+ * moin_decoder_cached_workspace_bytes(...) bytes with the bounds that the call goes by.  Errors: as for moin_decoder_forward and moin_kv_attention, before anything
  * is launched. */
-size_t moin_decoder_cached_workspace_bytes(const moin_model* model, int32_t R, int32_t T, int32_t max_q);
+size_t moin_decoder_cached_workspace_bytes(const moin_model* model, int32_t R, int32_t T, int32_t max_q, int32_t max_kv);
 moin_status moin_decoder_forward_cached(const moin_model* model, const int32_t* tokens, const moin_kv* caches,
                                         const moin_kv_tables* tables, const int32_t* rows, const moin_kv_batch* batch,
                                         const int32_t* req_expert, int32_t max_q, int32_t max_kv, const float* rope,

@@ -162,11 +162,11 @@ def lib() -> ctypes.CDLL:
         L.moin_kv_read.argtypes = [ctypes.POINTER(_Kv), vp, vp, i64, vp, i64, i32, vp]
         L.moin_rope_table.argtypes = [vp, i32, i32, f32, vp]
         L.moin_kv_attention_workspace_bytes.restype = sz
-        L.moin_kv_attention_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.moin_kv_attention_workspace_bytes.argtypes = [i32] * 7
         L.moin_kv_attention.argtypes = [ctypes.POINTER(_Kv), ctypes.POINTER(_KvTables), vp, vp, vp, i32, i32, i32, i32, vp, i64,
                                         i32, f32, vp, i32, vp, i64, vp, sz, vp]
         L.moin_decoder_cached_workspace_bytes.restype = sz
-        L.moin_decoder_cached_workspace_bytes.argtypes = [ctypes.POINTER(_Model), i32, i32, i32]
+        L.moin_decoder_cached_workspace_bytes.argtypes = [ctypes.POINTER(_Model), i32, i32, i32, i32]
         L.moin_decoder_forward_cached.argtypes = [ctypes.POINTER(_Model), vp, ctypes.POINTER(_Kv), ctypes.POINTER(_KvTables), vp,
                                                   ctypes.POINTER(_KvBatch), vp, i32, i32, vp, i32, vp, i32, ctypes.POINTER(_Taps), vp, sz, vp]
         L.moin_profile_enable.argtypes = [i32]
@@ -775,7 +775,9 @@ def decoder_forward_cached(model: DecoderModel, tokens: torch.Tensor, layers: Kv
         if t is not None and (t.dtype != torch.int32 or t.shape != (n,)):
             raise MoinError(f"expected {n} int32 values, got {tuple(t.shape)} of {t.dtype}")
     s = _stream(stream)
-    n = lib().moin_decoder_cached_workspace_bytes(ctypes.byref(model.c), R, T, max_q)
+    capacity = tables.max_pages * tables.page_tokens
+    max_kv = max_kv if 1 <= max_kv <= capacity else capacity
+    n = lib().moin_decoder_cached_workspace_bytes(ctypes.byref(model.c), R, T, max_q, max_kv)
     ws = workspace.data_ptr() if workspace is not None else _scratch_alloc(n, s)
     try:
         st = lib().moin_decoder_forward_cached(ctypes.byref(model.c), _ptr(tokens), layers.c, ctypes.byref(tables.c), _ptr(rows),

@@ -281,7 +281,7 @@ moin_status record_cuda(cudaError_t e);       // MOIN_OK or MOIN_ERR_CUDA (remem
 enum {
   OPTIN_ROUTE_CLUSTER = 0, /* .. 7 */ OPTIN_ROUTE_SIMPLE = 8, OPTIN_ATTENTION = 9, OPTIN_DECODE_GEMM = 10,
   OPTIN_DECODE_GEMM_FP8 = 11, OPTIN_TC_SHRINK = 12, OPTIN_TC_PAIR = 13, /* .. 17 */ OPTIN_DECODE_GEMM_EARLY = 18,
-  OPTIN_KV_ATTENTION = 19, /* .. 23 */
+  OPTIN_KV_ATTENTION = 19, /* .. 22 */ OPTIN_KV_CHUNK = 23
 };
 template <class Fn>
 inline cudaError_t ensure_smem_optin(int slot, Fn* fn, size_t bytes) {

@@ -486,7 +486,7 @@ static moin_status decoder_forward_impl(const moin_model* m, const int32_t* toke
   if (!from_hidden && (!tokens || !m->embed)) return MOIN_ERR_INVALID_ARG;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return MOIN_ERR_WORKSPACE;
   DecoderWorkspace w = carve(m, R, T, T, workspace);
-  const size_t att_bytes = kv ? moin_kv_attention_workspace_bytes(kv->max_q, m->n_heads, m->n_kv_heads, m->head_dim) : 0;
+  const size_t att_bytes = kv ? moin_kv_attention_workspace_bytes(R, T, kv->max_q, kv->max_kv, m->n_heads, m->n_kv_heads, m->head_dim) : 0;
   if (workspace_bytes < w.total + att_bytes) return MOIN_ERR_WORKSPACE;
   HostState* hs;
   moin_status st = host_state(&hs);
@@ -683,10 +683,10 @@ extern "C" moin_status moin_dequant_fp8(const void* codes, const float* scale, i
   return launch_dequant(jobs, d_in, (cudaStream_t)stream);
 }
 
-extern "C" size_t moin_decoder_cached_workspace_bytes(const moin_model* model, int32_t R, int32_t T, int32_t max_q) {
+extern "C" size_t moin_decoder_cached_workspace_bytes(const moin_model* model, int32_t R, int32_t T, int32_t max_q, int32_t max_kv) {
   if (!model || R < 0 || T < 0) return 0;
   if (max_q < 1 || max_q > T) max_q = T;
-  return carve(model, R, T, T, nullptr).total + moin_kv_attention_workspace_bytes(max_q, model->n_heads, model->n_kv_heads, model->head_dim) + 256;
+  return carve(model, R, T, T, nullptr).total + moin_kv_attention_workspace_bytes(R, T, max_q, max_kv, model->n_heads, model->n_kv_heads, model->head_dim) + 256;
 }
 
 extern "C" moin_status moin_decoder_forward_cached(const moin_model* m, const int32_t* tokens, const moin_kv* caches,

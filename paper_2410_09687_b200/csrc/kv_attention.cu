@@ -163,7 +163,7 @@ __device__ __forceinline__ void kv_load_query(const KvAttParams& p, const KvItem
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
     // 2^(9 - exponent of the largest element); a row of zeros, subnormals or infinities stays as it is
     const int e = (int)(__float_as_uint(top) >> 23) - 127;
-    const float f = (e > -120 && e < 128) ? __uint_as_float((uint32_t)(9 - e + 127) << 23) : 1.f;
+    const float f = (e > -118 && e < 128) ? __uint_as_float((uint32_t)(9 - e + 127) << 23) : 1.f;
     float sum[P];
 #pragma unroll
     for (int pl = 0; pl < P; ++pl) {
@@ -855,10 +855,25 @@ extern "C" moin_status moin_rope_table(float* table, int32_t n_pos, int32_t head
 // Row blocks of 8 NT rows: as many as a request has, up to what the registers hold.
 static int kv_nt(long long tall) { return tall <= 8 ? 1 : 2; }
 
-extern "C" size_t moin_kv_attention_workspace_bytes(int32_t max_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
-  if (max_q < 1 || n_kv_heads < 1 || n_heads < n_kv_heads || (head_dim != 64 && head_dim != 128)) return 256;
+// Long chunks go to the tcgen05 kernel: TODO
+static bool kv_use_chunk(int R, int T, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim, float scale) {
+  const long long G = n_heads / n_kv_heads, tiles = ((long long)max_kv + 63) / 64;
+  if (head_dim != 64 || !(scale > 0.f) || max_q * G < 128) return false;
+  // (the tensors that are laid out: at most 1 GiB; their blocks and rows, and the work items, within 32 bits)
+  return (max_q * G / 128 + 1) * R * n_kv_heads < (1ll << 30) && (long long)R * tiles * 64 * n_kv_heads * 256 + (long long)T * n_heads * 132 <= (1ll << 30) && (long long)T * n_heads <= (1ll << 30);
+}
+
+extern "C" size_t moin_kv_attention_workspace_bytes(int32_t R, int32_t T, int32_t max_q, int32_t max_kv, int32_t n_heads, int32_t n_kv_heads,
+                                                    int32_t head_dim) {
+  if (R < 1 || T < 1 || max_q < 1 || max_kv < 1 || n_kv_heads < 1 || n_heads < n_kv_heads || (head_dim != 64 && head_dim != 128)) return 256;
+  if (max_q > T) max_q = T;
   const int planes = head_dim / 64, nt = kv_nt((long long)max_q * (n_heads / n_kv_heads));
-  return kv_part_bytes(planes, nt) + (size_t)kKvMaxWorkers * 2 * sizeof(int4);
+  size_t bytes = kv_part_bytes(planes, nt) + (size_t)kKvMaxWorkers * 2 * sizeof(int4);
+  if (kv_use_chunk(R, T, max_q, max_kv, n_heads, n_kv_heads, head_dim, 1.f)) {
+    const size_t chunk = kv_chunk_bytes(R, T, max_kv, n_heads, n_kv_heads);
+    bytes = chunk > bytes ? chunk : bytes;
+  }
+  return bytes;
 }
 
 extern "C" moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables* tables, const int32_t* rows, const int32_t* cu_q,
@@ -881,7 +896,7 @@ extern "C" moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables
   if (!aligned16(q) || !aligned16(out) || (rope && !aligned16(rope))) return MOIN_ERR_MISALIGNED;
   const long long group = n_heads / kv->n_kv_heads;
   if (R > 65535 || max_q * group * group > 0xFFFFFFFFll) return MOIN_ERR_BAD_SHAPE;
-  if (!workspace || !aligned16(workspace) || workspace_bytes < moin_kv_attention_workspace_bytes(max_q, n_heads, kv->n_kv_heads, kv->head_dim))
+  if (!workspace || !aligned16(workspace) || workspace_bytes < moin_kv_attention_workspace_bytes(R, T, max_q, max_kv, n_heads, kv->n_kv_heads, kv->head_dim))
     return MOIN_ERR_WORKSPACE;
   HostState* hs;
   if ((st = host_state(&hs))) return st;
@@ -892,6 +907,9 @@ extern "C" moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables
   p.rope = (const float2*)rope;
   p.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t s = (cudaStream_t)stream;
+  if (kv_use_chunk(R, T, max_q, max_kv, n_heads, kv->n_kv_heads, kv->head_dim, scale))
+    return launch_kv_chunk(hs, p.kv, p.table, rows, cu_q, kv_len, p.n_rows, p.max_pages, R, T, max_q, max_kv, n_heads, p.q, q_stride, p.out, out_stride,
+                           p.rope, p.scale_log2, workspace, s);
   p.page_bytes = (uint32_t)p.kv.tile_at(1, 0, 0);
   p.tpp_log2 = kv->page_tokens == 16 ? 0 : kv->page_tokens == 32 ? 1 : kv->page_tokens == 64 ? 2 : 3;
   const int nt = kv_nt((long long)max_q * p.G);

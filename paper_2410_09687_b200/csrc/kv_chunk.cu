@@ -1,0 +1,726 @@
+// Attention of long chunks over the 4-bit cache on tcgen05 (head_dim 64): the products of prompts, where kv_attention.cu's warp
+// MMAs, made for a few rows, are bound by their instructions.
+//
+// kv_dense_kernel lays the requests' keys and values out as fp16 [request, position, kv head, 64] in the workspace, each tile of 64
+// tokens times a power of two that brings its largest value to 2^13 .. 2^14 (a value is off by 2^-12 of itself, or by 2^-39 of the
+// tile's largest) - or, in a tile whose tokens are unlike (their largest values differ by more than 2^12), each token times its own,
+// so that no token's precision depends on another, which a row may not even see -, and the queries as fp16 rows (rotated; times a power of two per row: exact) in the order the tiles take
+// them, [kv head, token, head of the group]: a tile of 128 rows is one box whatever the group is.  What is stored as NaN is laid
+// out as 0 and noted in the tile's mask; a row that sees such a token becomes NaN, no other row meets it.
+//
+// kv_chunk_kernel: work items are (request, kv head, 128 rows), persistent CTAs, two per SM, longest first, each with two chains of
+// (scores, softmax, product), as the attention of whole prompts has them: even and odd key tiles, a stream of four softmax
+// warps each with its own scores, maximum, sum and accumulator, which meet at the item's end.
+//   warp 0      producer: Q tiles into two buffers, K and V tiles [64 keys x 64 dims] into rings of four, by TMA
+//   warp 1      MMA issuer: S_h = Q K^T or O_h += P_h V, whatever is ready
+//   warps 2-5   stream 0, warps 6-9 stream 1: a thread per row
+// With the tile's factors (K: 2^a, V: 2^b) a weight is w = 2^(s 2^a + b - m), at most 2^15 (m lags and is moved to leave 2^10, as in
+// kv_attention.cu), P = fp16(w), and the row's sum takes w 2^-b in fp32.
+// Tensor memory: S_h / P_h at columns 64 h, O_h at 128 + 64 h.  Every mbarrier wait is bounded; on expiry the CTA raises the status
+// flag, drains and returns.
+#include <cuda.h>
+#include <float.h>
+
+#include "kv.cuh"
+#include "ptx.cuh"
+#include "tc_gemm.cuh"
+
+namespace moin {
+
+constexpr int kChThreads = 320;
+constexpr int kChKeys = 64, kChRows = 128;
+constexpr int kChQ = kChRows * 64 * 2, kChKV = kChKeys * 64 * 2, kChRing = 4;
+constexpr int kChMerge = 4096;               // (maximum, sum) of every row by stream, for two items
+constexpr int kChSmem = 2 * kChQ + 2 * kChRing * kChKV + 1024 /*align*/ + 256 /*barriers*/ + kChMerge;
+constexpr int kChTmemCols = 256;
+constexpr float kChTop = 10.f, kChMost = 15.f;   // log2 of the largest weight after a move of the maximum, and at all
+
+constexpr uint32_t kChIdesc = (1u << 4) | ((uint32_t)(64 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);   // D fp32, A and B fp16, 128 x 64
+constexpr uint32_t kChIdescPV = kChIdesc | (1u << 16);   // B with its rows along the output dimension
+constexpr uint64_t kChVStep = 2048 >> 4;                 // 16 keys further on
+
+struct ChunkParams {
+  KvView kv;
+  const int *table, *rows, *cu_q, *kv_len;
+  int n_rows, max_pages, R, T, max_q, max_kv, G, n_heads, n_blk, tiles;   // row blocks of the longest request, tiles of 64 of the longest
+  uint32_t inv_g;
+  const __nv_bfloat16* q;
+  __nv_bfloat16* out;
+  long long q_stride, out_stride;
+  const float2* rope;
+  float scale_log2;
+  __half *kd, *vd, *qd;     // dense keys, values [R tiles 64, H 64]; queries [H, T G, 64]
+  float* q_fac;             // [H, T G] 1 / (what the row was multiplied with)
+  uint4* info;              // [R, H, tiles]: scale log2(e) 2^a, b (fp32; low bits: hidden groups, unlike tokens), mask of NaN tokens
+  float2* tok;              // [R, H, tiles, 64], of tiles of unlike tokens: (scale log2(e) 2^a, b) of every token
+  int dense_blocks;
+  DeviceStatus* status;
+};
+
+__device__ __forceinline__ int ch_div_g(const ChunkParams& p, int row) { return p.G == 1 ? row : (int)__umulhi((uint32_t)row, p.inv_g); }
+struct ChReq { int t0, q_len, kv_len, row; };
+__device__ __forceinline__ ChReq ch_request(const ChunkParams& p, int req) {   // as kv_item of kv_attention.cu
+  ChReq r;
+  r.t0 = min(max(p.cu_q[req], 0), p.T);
+  r.q_len = min(max(p.cu_q[req + 1], r.t0), p.T) - r.t0;
+  r.kv_len = p.kv_len[req];
+  r.row = p.rows ? p.rows[req] : req;
+  if (r.kv_len < 0 || r.kv_len > p.max_kv || r.q_len > p.max_q || r.row < 0 || r.row >= p.n_rows) r.kv_len = 0;
+  return r;
+}
+
+// Blocks below dense_blocks: 64 tokens of a request and kv head, a warp per 16 of them.  The others: eight query rows, a warp each.
+// Bound by the traffic of what they write; small beside the products.
+constexpr uint32_t kChUnlike = 0x10u;   // in the low bits of b
+constexpr int kChRange = 12;            // powers of two between the tokens of a tile that are alike
+constexpr int kDensePitch = 36;   // words of a row in shared memory: neither side meets a bank twice
+__global__ void __launch_bounds__(128)
+kv_dense_kernel(const ChunkParams p) {
+  __shared__ __align__(16) uint32_t s_rows[4][kKvTile * kDensePitch];
+  __shared__ float s_max[4][2], s_min[4][2];
+  __shared__ uint32_t s_bad[4];
+  pdl_begin();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  if ((int)blockIdx.x >= p.dense_blocks) {
+    const long long n = (long long)p.T * p.n_heads;
+    for (int k = 0; k < 2; ++k) {   // row: token and query head
+      const long long i = ((long long)blockIdx.x - p.dense_blocks) * 8 + 2 * warp + k;
+      if (i >= n) return;
+      const int tok = (int)(i / p.n_heads), h = (int)(i % p.n_heads);
+      // the request of the token: the last one that begins at or before it
+      int lo = 0, hi = p.R;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (p.cu_q[mid + 1] > tok) hi = mid; else lo = mid + 1;
+      }
+      float a = 0.f, b = 0.f;
+      if (lo < p.R) {
+        const ChReq r = ch_request(p, lo);
+        const int pos = r.kv_len - r.q_len + tok - r.t0;
+        if (tok >= r.t0 && tok < r.t0 + r.q_len && pos >= 0) {
+          const __nv_bfloat16* src = p.q + (long long)tok * p.q_stride + (long long)h * 64;
+          a = __bfloat162float(src[lane]);
+          b = __bfloat162float(src[lane + 32]);
+          if (p.rope != nullptr) {
+            const float2 cs = __ldg(p.rope + (size_t)pos * 32 + lane);
+            const float x = round_bf16(kv_rot_lo(a, b, cs)), y = round_bf16(kv_rot_hi(a, b, cs));
+            a = x;
+            b = y;
+          }
+        }
+      }
+      float top = fmaxf(fabsf(a), fabsf(b));
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const int e = (int)(__float_as_uint(top) >> 23) - 127;
+      const float f = (e > -118 && e < 128) ? __uint_as_float((uint32_t)(9 - e + 127) << 23) : 1.f;
+      const long long row = (long long)(h / p.G) * p.T * p.G + (long long)tok * p.G + h % p.G;
+      p.qd[row * 64 + lane] = __float2half_rn(a * f);
+      p.qd[row * 64 + 32 + lane] = __float2half_rn(b * f);
+      if (lane == 0) p.q_fac[row] = 1.f / f;
+    }
+    return;
+  }
+  const int tile = blockIdx.x % p.tiles, rh = blockIdx.x / p.tiles, head = rh % p.kv.H, req = rh / p.kv.H;
+  const ChReq r = ch_request(p, req);
+  if (tile * kChKeys >= r.kv_len || r.q_len == 0) return;
+  const int first = tile * kChKeys + warp * kKvTile;   // this warp's tokens
+  uint4 k4 = make_uint4(0u, 0u, 0u, 0u), v4 = k4, pr = k4;
+  uint32_t gone = 0xFFFFu;   // of its tokens: not there
+  if (first < r.kv_len) {
+    const int page = p.table[(size_t)r.row * p.max_pages + first / p.kv.page_tokens];
+    if (page >= 0 && page < p.kv.n_pages) {
+      const uint8_t* at = p.kv.pages + p.kv.tile_at(page, head, first % p.kv.page_tokens / kKvTile);
+      k4 = *reinterpret_cast<const uint4*>(at + 16 * lane);
+      v4 = *reinterpret_cast<const uint4*>(at + 512 + 16 * lane);
+      pr = *reinterpret_cast<const uint4*>(at + kKvPairs + 16 * g);
+      gone = r.kv_len - first >= kKvTile ? 0u : 0xFFFFu & ~((1u << (r.kv_len - first)) - 1u);
+    }
+  }
+  const uint32_t kw[4] = {k4.x, k4.y, k4.z, k4.w};
+  const uint32_t vw[4] = {movmatrix_trans(v4.x), movmatrix_trans(v4.y), movmatrix_trans(v4.z), movmatrix_trans(v4.w)};
+  const uint32_t pk[2] = {pr.x, pr.y}, pv[2] = {pr.z, pr.w};
+  float x[2][2][16];                                    // [key, value][token g, g + 8][2 j + half .. as words]
+  float tok[2][2], top[2] = {0.f, 0.f}, low[2] = {INFINITY, INFINITY};   // largest values: of the tokens, of the tile, of its least token
+  uint32_t bad = 0;
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const bool out = gone >> (g + 8 * s) & 1u;
+    bool nan = false;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const uint32_t pair = c == 0 ? pk[s] : pv[s];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {   // word i / 4, nibble (i / 2) & 1, half i & 1
+        const uint32_t w = c == 0 ? kw[i >> 2] : vw[i >> 2];
+        const float v = fmaf((float)(w >> (8 * s + 4 * ((i >> 1) & 1) + 16 * (i & 1)) & 15u), kv_scale(pair), kv_zero(pair));
+        x[c][s][i] = v;
+        nan = nan || !(fabsf(v) < INFINITY);
+      }
+    }
+    // (the four lanes of a token agree)
+    nan = __ballot_sync(0xffffffffu, nan) >> (4 * g) & 0xFu;
+    if (nan && !out) bad |= 1u << (g + 8 * s);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      tok[c][s] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if (nan || out) x[c][s][i] = 0.f;
+        tok[c][s] = fmaxf(tok[c][s], fabsf(x[c][s][i]));
+      }
+      tok[c][s] = fmaxf(tok[c][s], __shfl_xor_sync(0xffffffffu, tok[c][s], 1));
+      tok[c][s] = fmaxf(tok[c][s], __shfl_xor_sync(0xffffffffu, tok[c][s], 2));
+      top[c] = fmaxf(top[c], tok[c][s]);
+      if (tok[c][s] > 0.f) low[c] = fminf(low[c], tok[c][s]);
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], o));
+    top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], o));
+    low[0] = fminf(low[0], __shfl_xor_sync(0xffffffffu, low[0], o));
+    low[1] = fminf(low[1], __shfl_xor_sync(0xffffffffu, low[1], o));
+    bad |= __shfl_xor_sync(0xffffffffu, bad, o);
+  }
+  // tokens of a page that is not there are hidden, not NaN: noted apart, in the upper half
+  const bool hidden = first < r.kv_len && (gone & 1u);
+  if (lane == 0) {
+    s_max[warp][0] = top[0];
+    s_max[warp][1] = top[1];
+    s_min[warp][0] = low[0];
+    s_min[warp][1] = low[1];
+    s_bad[warp] = bad | (hidden ? 0x10000u : 0u);
+  }
+  __syncthreads();
+  auto power = [](float m) { return max((int)(__float_as_uint(m) >> 23) - 127 - 13, -64); };   // 2^it times 2^13 .. 2^14 is the largest value
+  auto two_to = [](int e) { return __uint_as_float((uint32_t)(127 + e) << 23); };
+  float f[2][2];   // [key, value][token g, g + 8]
+  int e[2], et[2][2];
+  bool unlike = false;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const float m = fmaxf(fmaxf(s_max[0][c], s_max[1][c]), fmaxf(s_max[2][c], s_max[3][c]));
+    const float l = fminf(fminf(s_min[0][c], s_min[1][c]), fminf(s_min[2][c], s_min[3][c]));
+    e[c] = power(m);
+    unlike = unlike || (l < INFINITY && e[c] - power(l) > kChRange);
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      et[c][s] = unlike ? power(tok[c][s]) : e[c];
+      f[c][s] = two_to(-et[c][s]);
+    }
+  const size_t at_tile = ((size_t)req * p.kv.H + head) * p.tiles + tile;
+  if (unlike && t == 0) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) p.tok[at_tile * kChKeys + warp * kKvTile + g + 8 * s] = make_float2(p.scale_log2 * two_to(et[0][s]), (float)et[1][s]);
+  }
+  if (threadIdx.x == 0) {
+    uint32_t hide = 0;
+    for (int w = 0; w < 4; ++w) hide |= (s_bad[w] >> 16) << w;
+    const uint32_t lo = (s_bad[0] & 0xFFFFu) | s_bad[1] << 16, hi = (s_bad[2] & 0xFFFFu) | s_bad[3] << 16;
+    // b is a whole number of at most 114: its low mantissa bits are free
+    p.info[at_tile] = make_uint4(__float_as_uint(p.scale_log2 * two_to(e[0])), __float_as_uint((float)e[1]) | hide | (unlike ? kChUnlike : 0u), lo, hi);
+  }
+  uint32_t* stage = s_rows[warp];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const __half2 h = __floats2half2_rn(x[c][s][2 * i] * f[c][s], x[c][s][2 * i + 1] * f[c][s]);
+        stage[(g + 8 * s) * kDensePitch + 4 * i + t] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+    __syncwarp();
+    __half* dst = (c == 0 ? p.kd : p.vd) + (((size_t)req * p.tiles * kChKeys + first) * p.kv.H + head) * 64;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int row = 4 * k + (lane >> 3);
+      *reinterpret_cast<uint4*>(dst + (size_t)row * p.kv.H * 64 + 8 * (lane & 7)) = *reinterpret_cast<const uint4*>(stage + row * kDensePitch + 4 * (lane & 7));
+    }
+    __syncwarp();
+  }
+}
+
+struct ChItem { int req, head, row0, t0, n_rows, past, first_pos, last_pos, n_tiles; bool on; };
+__device__ __forceinline__ ChItem ch_item(const ChunkParams& p, int idx) {
+  ChItem it;
+  const int per = p.R * p.kv.H;
+  const int blk = p.n_blk - 1 - idx / per, rem = idx % per;   // longest blocks first
+  it.req = rem / p.kv.H;
+  it.head = rem % p.kv.H;
+  it.row0 = blk * kChRows;
+  const ChReq r = ch_request(p, it.req);
+  it.t0 = r.t0;
+  it.n_rows = r.q_len * p.G;
+  it.on = it.row0 < it.n_rows;
+  it.past = r.kv_len - r.q_len;
+  it.first_pos = it.past + ch_div_g(p, it.row0);
+  it.last_pos = it.on ? it.past + ch_div_g(p, min(it.row0 + kChRows, it.n_rows) - 1) : -1;
+  it.n_tiles = it.last_pos < 0 || r.kv_len == 0 ? 0 : it.last_pos / kChKeys + 1;
+  return it;
+}
+__device__ __forceinline__ float ch_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float ch_rescale(float l, float d) {   // l 2^d, where 2^d alone may be too small (kv_attention.cu)
+  const float f = ch_exp2(0.5f * d);
+  return l * f * f;
+}
+
+__global__ void __launch_bounds__(kChThreads, 2)
+kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const ChunkParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* base_ptr = smem_raw + (base - raw);
+  const uint32_t sQ = base, sK = base + 2 * kChQ, sV = sK + kChRing * kChKV, bars = sV + kChRing * kChKV;
+  uint8_t* bar_ptr = base_ptr + (bars - base);
+  const uint32_t kfull = bars, kempty = bars + 32, vfull = bars + 64, vempty = bars + 96, sready = bars + 128, pready = bars + 144,
+                 pvdone = bars + 160, oready = bars + 176, ofree = bars + 184, qfull = bars + 192, qfree = bars + 208;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_ptr + 224);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bar_ptr + 228);
+  volatile int* sm_fail = reinterpret_cast<volatile int*>(bar_ptr + 232);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kChRing; ++i) {
+      mbar_init(kfull + 8 * i, 1); mbar_init(kempty + 8 * i, 1);
+      mbar_init(vfull + 8 * i, 1); mbar_init(vempty + 8 * i, 1);
+    }
+    for (int h = 0; h < 2; ++h) {
+      mbar_init(sready + 8 * h, 1); mbar_init(pready + 8 * h, 128); mbar_init(pvdone + 8 * h, 1);
+      mbar_init(qfull + 8 * h, 1); mbar_init(qfree + 8 * h, 1);
+    }
+    mbar_init(oready, 1);
+    mbar_init(ofree, 256);
+    *abort_flag = 0;
+    sm_fail[0] = sm_fail[1] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(tmem_slot), kChTmemCols);
+    tmem_relinquish();
+  }
+  pdl_begin();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const int n_items = p.n_blk * p.R * p.kv.H;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ producer
+    if (lane == 0) {
+      uint32_t tq = 0, nq = 0;   // tiles, Q tiles so far
+      bool ok = true;
+      auto load_q = [&](const ChItem& n) -> bool {
+        const uint32_t b = nq & 1u;
+        if (!mbar_wait(qfree + 8 * b, ((nq >> 1) & 1u) ^ 1u, abort_flag, p.status, 61)) return false;
+        mbar_expect_tx(qfull + 8 * b, kChQ);
+        tma_load_2d(sQ + b * kChQ, &tmQ, qfull + 8 * b, 0, n.head * p.T * p.G + n.t0 * p.G + n.row0);
+        ++nq;
+        return true;
+      };
+      auto next = [&](int& i, ChItem& out) -> bool {   // the next item that has tiles
+        for (i += gridDim.x; i < n_items; i += gridDim.x) {
+          out = ch_item(p, i);
+          if (out.n_tiles > 0) return true;
+        }
+        return false;
+      };
+      int idx = (int)blockIdx.x - (int)gridDim.x;
+      ChItem it, nx;
+      bool have = next(idx, it);
+      if (have) ok = load_q(it);
+      while (have && ok) {
+        int nidx = idx;
+        const bool have_nx = next(nidx, nx);
+        const int row = it.req * p.tiles * kChKeys;
+        for (int j = 0; j < it.n_tiles && ok; ++j, ++tq) {
+          const uint32_t s = tq % kChRing, ph = (tq / kChRing) & 1u;
+          if (!(ok = mbar_wait(kempty + 8 * s, ph ^ 1u, abort_flag, p.status, 62))) break;
+          mbar_expect_tx(kfull + 8 * s, kChKV);
+          tma_load_2d(sK + s * kChKV, &tmK, kfull + 8 * s, it.head * 64, row + j * kChKeys);
+          if (!(ok = mbar_wait(vempty + 8 * s, ph ^ 1u, abort_flag, p.status, 63))) break;
+          mbar_expect_tx(vfull + 8 * s, kChKV);
+          tma_load_2d(sV + s * kChKV, &tmV, vfull + 8 * s, it.head * 64, row + j * kChKeys);
+          if (have_nx && j == min(1, it.n_tiles - 1)) ok = load_q(nx);   // (its buffer: since the item before's last scores)
+        }
+        it = nx;
+        idx = nidx;
+        have = have_nx;
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer: the whole warp walks, one lane issues
+    const bool leader = elect_one();
+    uint32_t tq = 0, nit = 0;
+    uint32_t n_p[2] = {0, 0};   // products issued per stream
+    bool ok = true;
+    for (int idx = blockIdx.x; idx < n_items && ok; idx += gridDim.x) {
+      const ChItem it = ch_item(p, idx);
+      if (it.n_tiles == 0) continue;
+      const uint32_t qb = nit & 1u;
+      if (!(ok = mbar_wait_warp(qfull + 8 * qb, (nit >> 1) & 1u, abort_flag, p.status, 64))) break;
+      tc_fence_after();
+      const uint64_t dq = sdesc_k128(sQ + qb * kChQ);
+      int tile[2] = {0, 1}, left = it.n_tiles, left_s = it.n_tiles;   // next tile of each stream; products, scores to go
+      bool scores[2] = {false, false};
+      bool o_free = false;
+      unsigned long long t0 = 0;
+      uint32_t spins = 0;
+      while (left > 0) {
+        bool moved = false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (tile[h] >= it.n_tiles) continue;
+          const uint32_t gt = tq + (uint32_t)tile[h], s = gt % kChRing, ph = (gt / kChRing) & 1u;
+          if (!scores[h]) {
+            // P of the product before lies where these scores go
+            if (!__all_sync(0xffffffffu, (n_p[h] == 0 || mbar_test_wait(pvdone + 8 * h, (n_p[h] - 1) & 1u)) && mbar_test_wait(kfull + 8 * s, ph))) continue;
+            tc_fence_after();
+            const uint64_t dk = sdesc_k128(sK + s * kChKV);
+            --left_s;
+            if (leader) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) tc_mma_bf16(tmem + h * 64, dq + (uint64_t)(2 * k), dk + (uint64_t)(2 * k), kChIdesc, k > 0 ? 1u : 0u);
+              tc_commit(kempty + 8 * s);
+              tc_commit(sready + 8 * h);
+              if (left_s == 0) tc_commit(qfree + 8 * qb);
+            }
+            scores[h] = true;
+            moved = true;
+          } else {
+            // the accumulators are free once the O of the item before has been read
+            if (!o_free && !(o_free = __all_sync(0xffffffffu, mbar_test_wait(ofree, (nit & 1u) ^ 1u)))) continue;
+            if (!__all_sync(0xffffffffu, mbar_test_wait(pready + 8 * h, n_p[h] & 1u) && mbar_test_wait(vfull + 8 * s, ph))) continue;
+            tc_fence_after();
+            const uint64_t dv = sdesc_k128(sV + s * kChKV);
+            const uint32_t first = tile[h] == h ? 0u : 1u;
+            if (leader) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                tc_mma_bf16_ta(tmem + 128 + h * 64, tmem + h * 64 + 8 * k, dv + kChVStep * k, kChIdescPV, k > 0 ? 1u : first);
+              tc_commit(vempty + 8 * s);
+              tc_commit(pvdone + 8 * h);
+            }
+            ++n_p[h];
+            scores[h] = false;
+            tile[h] += 2;
+            --left;
+            moved = true;
+          }
+        }
+        if (moved) {
+          spins = 0;
+          t0 = 0;
+        } else if ((++spins & 0x3FFu) == 0) {   // bounded, as every wait
+          int stop = *abort_flag;
+          const unsigned long long now = global_ns();
+          if (t0 == 0) t0 = now;
+          if (now - t0 > kWaitLimitNs) {
+            stop = *abort_flag = 1;
+            atomicExch(&p.status->timeout_flag, 1);
+            atomicExch(&p.status->timeout_site, 65);
+          }
+          if (__any_sync(0xffffffffu, stop != 0)) {
+            ok = false;
+            break;
+          }
+        }
+      }
+      if (ok && leader) tc_commit(oready);
+      tq += (uint32_t)it.n_tiles;
+      ++nit;
+    }
+  } else {
+    // ------------------------------------------------------------------ softmax and result: a thread per row and stream
+    // The streams of an item meet at a named barrier that all 256 threads reach whatever happened before; the decision to give
+    // up is taken from the item's flag, which is only written before it (two flags in turn).
+    const int quarter = warp & 3, half = (warp - 2) >> 2, row = quarter * 32 + lane;
+    const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16, s_addr = tmem + lane_addr + half * 64;
+    float2* xml = reinterpret_cast<float2*>(bar_ptr + 256);   // [item parity][stream][row]: (maximum, sum)
+    uint32_t n_s = 0, nit = 0;
+    bool ok = true;
+    for (int idx = blockIdx.x; idx < n_items; idx += gridDim.x) {
+      const ChItem it = ch_item(p, idx);
+      if (!it.on) continue;
+      const int r = it.row0 + row, qi = ch_div_g(p, min(r, it.n_rows - 1));
+      const bool live = r < it.n_rows;
+      __nv_bfloat16* dst = p.out + (long long)(it.t0 + qi) * p.out_stride + (it.head * p.G + min(r, it.n_rows - 1) - qi * p.G) * 64 + half * 32;
+      if (it.n_tiles == 0) {   // nothing to see for any row
+        if (live) {
+#pragma unroll
+          for (int c = 0; c < 32; c += 8) *reinterpret_cast<uint4*>(dst + c) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        continue;
+      }
+      const int pos = it.past + qi;
+      const float fac = live ? __ldg(p.q_fac + (long long)it.head * p.T * p.G + (long long)it.t0 * p.G + r) : 1.f;
+      const uint4* info = p.info + ((size_t)it.req * p.kv.H + it.head) * p.tiles;
+      float m = 0.f, l = 0.f;   // maximum (powers of two), sum of 2^(s - m)
+      bool fresh = true;        // no key seen yet: m means nothing
+      uint4 at = half < it.n_tiles ? __ldg(info + half) : make_uint4(0u, 0u, 0u, 0u);
+      for (int j = half; j < it.n_tiles && ok; j += 2, ++n_s) {
+        const uint4 now = at;
+        if (j + 2 < it.n_tiles) at = __ldg(info + j + 2);
+        const float c = __uint_as_float(now.x) * fac, ev = __uint_as_float(now.y & ~0x1Fu);
+        const uint32_t hide = now.y & 0xFu;
+        const float2* unlike = (now.y & kChUnlike) ? p.tok + (((size_t)it.req * p.kv.H + it.head) * p.tiles + j) * kChKeys : nullptr;
+        if (!(ok = mbar_wait_warp(sready + 8 * half, n_s & 1u, abort_flag, p.status, 66))) break;
+        tc_fence_after();
+        // twice over the scores in groups of 16 keys, the next group's read in flight (a thread that keeps all 64 spills)
+        const int kr0 = j * kChKeys;
+        uint32_t va[16], vb[16];
+        float ma = -INFINITY, mc = -INFINITY;
+        auto all_seen = [&](int k) { return kr0 + 16 * k + 15 <= it.first_pos && !(hide >> k & 1u); };
+        auto any_seen = [&](int k) { return kr0 + 16 * k <= it.last_pos && !(hide >> k & 1u); };
+        auto group_max = [&](const uint32_t (&v)[16], int k) {
+          if (all_seen(k)) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+              ma = fmax3(ma, __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+              mc = fmax3(mc, __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+            }
+          } else if (any_seen(k)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (kr0 + 16 * k + i <= pos) ma = fmaxf(ma, __uint_as_float(v[i]));
+          }
+        };
+        float tm = -INFINITY;
+        if (unlike == nullptr) {
+          tmem_ld16(s_addr, va);
+          tmem_ld16(s_addr + 16, vb);
+          tmem_ld_wait();
+          group_max(va, 0);
+          group_max(vb, 1);
+          tmem_ld16(s_addr + 32, va);
+          tmem_ld16(s_addr + 48, vb);
+          tmem_ld_wait();
+          group_max(va, 2);
+          group_max(vb, 3);
+          const float mx = fmaxf(ma, mc);
+          if (mx > -INFINITY) tm = fmaf(mx, c, ev);
+        } else {
+#pragma unroll 1
+          for (int k = 0; k < 4; ++k) {
+            tmem_ld16(s_addr + 16 * k, va);
+            tmem_ld_wait();
+            if (hide >> k & 1u) continue;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float2 tk = __ldg(unlike + 16 * k + i);
+              if (kr0 + 16 * k + i <= pos) tm = fmaxf(tm, fmaf(__uint_as_float(va[i]), tk.x * fac, tk.y));
+            }
+          }
+        }
+        tmem_ld16(s_addr, va);
+        const bool grow = fresh ? tm > -INFINITY : tm > m + kChMost;
+        if (__any_sync(0xffffffffu, grow)) {
+          const float m_new = grow ? tm - kChTop : m, corr = grow && !fresh ? ch_exp2(m - m_new) : 1.f;
+          if (grow && !fresh) l = ch_rescale(l, m - m_new);
+          m = m_new;
+          fresh = fresh && !grow;
+          if (j != half) {   // (these scores exist only because the product before is complete)
+#pragma unroll
+            for (int q = 0; q < 64; q += 16) {
+              uint32_t o[16];
+              tmem_ld16(s_addr + 128 + q, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
+              tmem_st16(s_addr + 128 + q, o);
+            }
+          }
+        }
+        const uint64_t off2 = pair_f32(ev - m, ev - m), c2 = pair_f32(c, c);
+        uint64_t l2 = pair_f32(0.f, 0.f);
+        auto group_p = [&](const uint32_t (&v)[16], int k, uint32_t* w) {
+          if (all_seen(k)) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+              float x0, x1;
+              unpair_f32(fma2(pair_f32(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), c2, off2), x0, x1);
+              const float p0 = ch_exp2(x0), p1 = ch_exp2(x1);
+              l2 = add2(l2, pair_f32(p0, p1));
+              const __half2 h2 = __floats2half2_rn(p0, p1);
+              w[i >> 1] = *reinterpret_cast<const uint32_t*>(&h2);
+            }
+          } else if (any_seen(k)) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+              const float p0 = kr0 + 16 * k + i <= pos ? ch_exp2(fmaf(__uint_as_float(v[i]), c, ev - m)) : 0.f;
+              const float p1 = kr0 + 16 * k + i + 1 <= pos ? ch_exp2(fmaf(__uint_as_float(v[i + 1]), c, ev - m)) : 0.f;
+              l2 = add2(l2, pair_f32(p0, p1));
+              const __half2 h2 = __floats2half2_rn(p0, p1);
+              w[i >> 1] = *reinterpret_cast<const uint32_t*>(&h2);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = 0u;
+          }
+        };
+        // One by one: unlike tokens; or weights too small for fp32 (the maximum comes from values 2^80 times this tile's) of keys
+        // whose 2^(s - m) still counts in the sum.
+        if (unlike != nullptr || __any_sync(0xffffffffu, tm < m - 80.f && tm - ev > m - 60.f)) {
+#pragma unroll 1
+          for (int hq = 0; hq < 2; ++hq) {
+            uint32_t w[16];
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+              const int k = 2 * hq + kk;
+              tmem_ld16(s_addr + 16 * k, va);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; i += 2) {
+                float pr[2];
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                  const float2 tk = unlike != nullptr ? __ldg(unlike + 16 * k + i + b) : make_float2(__uint_as_float(now.x), ev);
+                  const bool seen = kr0 + 16 * k + i + b <= pos && !(hide >> k & 1u);
+                  const float pk = seen ? ch_exp2(fmaf(__uint_as_float(va[i + b]), tk.x * fac, -m)) : 0.f;
+                  l += pk;
+                  pr[b] = pk * ch_exp2(tk.y);
+                }
+                const __half2 h2 = __floats2half2_rn(pr[0], pr[1]);
+                w[8 * kk + (i >> 1)] = *reinterpret_cast<const uint32_t*>(&h2);
+              }
+            }
+            tmem_st16(s_addr + 16 * hq, w);
+          }
+        } else
+#pragma unroll
+        for (int hq = 0; hq < 2; ++hq) {   // P of 32 keys into columns whose scores have been read
+          uint32_t w[16];
+          tmem_ld_wait();
+          tmem_ld16(s_addr + 32 * hq + 16, vb);
+          group_p(va, 2 * hq, w);
+          tmem_ld_wait();
+          if (hq == 0) tmem_ld16(s_addr + 32, va);
+          group_p(vb, 2 * hq + 1, w + 8);
+          tmem_st16(s_addr + 16 * hq, w);
+        }
+        float la, lb;
+        unpair_f32(l2, la, lb);
+        l = fmaf(la + lb, ch_exp2(-ev), l);
+        if (now.z | now.w) {   // tokens stored as NaN: for the rows that see one
+          const int seen = pos - kr0;
+          const unsigned long long mask = (unsigned long long)now.w << 32 | now.z;
+          if (seen >= 0 && (mask & (seen >= 63 ? ~0ull : (1ull << (seen + 1)) - 1ull))) l = NAN;
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(pready + 8 * half);
+      }
+      float2* mine = xml + (nit & 1u) * 256;
+      mine[half * 128 + row] = make_float2(fresh ? -FLT_MAX : m, l);
+      if (!ok) sm_fail[nit & 1u] = 1;
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      if (sm_fail[nit & 1u]) break;              // the same for all 256 threads
+      const float2 own = mine[half * 128 + row], other = mine[(half ^ 1) * 128 + row];
+      const float top = fmaxf(own.x, other.x);
+      const float a_me = ch_exp2(own.x - top), a_ot = ch_exp2(other.x - top);
+      const float sum = ch_rescale(own.y, own.x - top) + ch_rescale(other.y, other.x - top);
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;   // nothing to see: zeros
+      const float f0 = (half == 0 ? a_me : a_ot) * inv, f1 = (half == 0 ? a_ot : a_me) * inv;
+      // ---- (O_0 f_0 + O_1 f_1) -> out: this thread's 32 of the row's 64 dims
+      if ((ok = mbar_wait_warp(oready, nit & 1u, abort_flag, p.status, 67))) {
+        tc_fence_after();
+        uint32_t v[16], u[16];
+#pragma unroll
+        for (int c = 0; c < 32; c += 16) {
+          tmem_ld16(tmem + lane_addr + 128 + half * 32 + c, v);
+          if (it.n_tiles > 1) {
+            tmem_ld16(tmem + lane_addr + 192 + half * 32 + c, u);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) u[i] = 0u;   // (nothing was ever accumulated there)
+          }
+          tmem_ld_wait();
+          if (c == 16) {                          // O is in registers: the accumulators may be written again
+            tc_fence_before();
+            mbar_arrive(ofree);
+          }
+          uint32_t o[8];
+#pragma unroll
+          for (int i = 0; i < 16; i += 2)
+            o[i >> 1] = pack_bf16(fmaf(__uint_as_float(u[i]), f1, __uint_as_float(v[i]) * f0), fmaf(__uint_as_float(u[i + 1]), f1, __uint_as_float(v[i + 1]) * f0));
+          if (live) {
+            *reinterpret_cast<uint4*>(dst + c) = make_uint4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<uint4*>(dst + c + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+          }
+        }
+      }
+      ++nit;
+    }
+  }
+  // ------------------------------------------------------------------ teardown
+  if (*abort_flag) {
+    const unsigned long long t0 = global_ns();
+    while (global_ns() - t0 < 2000000ull) __nanosleep(1000);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kChTmemCols);
+  }
+}
+
+// ---- host
+struct ChunkSpace { size_t kd, vd, qd, fac, info, tok, total; };
+static ChunkSpace chunk_space(long long R, long long T, long long max_kv, long long n_heads, long long H) {
+  ChunkSpace c;
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes, 256); return o; };
+  const size_t tiles = (size_t)((max_kv + kChKeys - 1) / kChKeys), rows = (size_t)R * tiles * kChKeys;
+  c.kd = take(rows * H * 128);
+  c.vd = take(rows * H * 128);
+  c.qd = take((size_t)T * n_heads * 128);
+  c.fac = take((size_t)T * n_heads * 4);
+  c.info = take((size_t)R * H * tiles * 16);
+  c.tok = take(rows * H * 8);
+  c.total = off;
+  return c;
+}
+
+size_t kv_chunk_bytes(int R, int T, int max_kv, int n_heads, int H) { return chunk_space(R, T, max_kv, n_heads, H).total; }
+
+moin_status launch_kv_chunk(HostState* hs, const KvView& kv, const int* table, const int* rows, const int* cu_q, const int* kv_len, int n_rows,
+                            int max_pages, int R, int T, int max_q, int max_kv, int n_heads, const __nv_bfloat16* q, long long q_stride,
+                            __nv_bfloat16* out, long long out_stride, const float2* rope, float scale_log2, void* workspace, cudaStream_t s) {
+  const ChunkSpace c = chunk_space(R, T, max_kv, n_heads, kv.H);
+  char* w = (char*)workspace;
+  ChunkParams p = {};
+  p.kv = kv; p.table = table; p.rows = rows; p.cu_q = cu_q; p.kv_len = kv_len; p.n_rows = n_rows; p.max_pages = max_pages;
+  p.R = R; p.T = T; p.max_q = max_q; p.max_kv = max_kv; p.n_heads = n_heads; p.G = n_heads / kv.H;
+  p.inv_g = (uint32_t)((0x100000000ull + p.G - 1) / p.G);
+  p.n_blk = (int)(((long long)max_q * p.G + kChRows - 1) / kChRows);
+  p.tiles = (max_kv + kChKeys - 1) / kChKeys;
+  p.q = q; p.q_stride = q_stride; p.out = out; p.out_stride = out_stride; p.rope = rope; p.scale_log2 = scale_log2;
+  p.kd = (__half*)(w + c.kd); p.vd = (__half*)(w + c.vd); p.qd = (__half*)(w + c.qd); p.q_fac = (float*)(w + c.fac); p.info = (uint4*)(w + c.info); p.tok = (float2*)(w + c.tok);
+  p.dense_blocks = R * kv.H * p.tiles;
+  p.status = hs->status;
+  CUtensorMap mq, mk, mv;
+  const uint64_t dense_rows = (uint64_t)R * p.tiles * kChKeys;
+  moin_status st = make_map(&mq, p.qd, (uint64_t)T * n_heads, 64, kChRows);
+  if (!st) st = make_map(&mk, p.kd, dense_rows, (uint64_t)kv.H * 64, kChKeys);
+  if (!st) st = make_map(&mv, p.vd, dense_rows, (uint64_t)kv.H * 64, kChKeys);
+  if (st) return st;
+  cudaError_t e = ensure_smem_optin(OPTIN_KV_CHUNK, kv_chunk_kernel, kChSmem);
+  if (e != cudaSuccess) return record_cuda(e);
+  const long long q_blocks = ((long long)T * n_heads + 7) / 8, items = (long long)p.n_blk * R * kv.H;
+  ProfScope prof(MOIN_K_KV_ATTENTION, 2, s);
+  e = launch_pdl(kv_dense_kernel, (unsigned)(p.dense_blocks + q_blocks), 128, 0, s, p);
+  if (e == cudaSuccess)
+    e = launch_pdl(kv_chunk_kernel, (unsigned)(items < 2L * hs->n_sms ? items : 2L * hs->n_sms), kChThreads, kChSmem, s, mq, mk, mv, p);
+  return record_cuda(e);
+}
+
+}  // namespace moin

@@ -10,6 +10,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <string>
 
 #include "../../include/moin.h"
@@ -166,7 +167,9 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Rope rope = rope_of(a[9], kv->head_dim);
     int32_t max_q = size32(a[5]);
     if (max_q < 1 || max_q > T) max_q = T;
-    const int32_t max_kv = size32(a[6]);
+    int32_t max_kv = size32(a[6]);
+    const int64_t capacity = (int64_t)tables->max_pages * tables->page_tokens;
+    if (max_kv < 1 || max_kv > capacity) max_kv = (int32_t)std::min<int64_t>(capacity, INT32_MAX);
     double scale = 0;
     if (a[8] != Py_None) {
       scale = PyFloat_AsDouble(a[8]);
@@ -176,7 +179,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     const int32_t *cu = vec(a[3], (int64_t)R + 1), *len = vec(a[4], R), *rows = vec(a[7], R);
     const cudaStream_t s = stream_of(a[11]);
-    const size_t bytes = f_ws(max_q, heads, kv->n_kv_heads, kv->head_dim);
+    const size_t bytes = f_ws(R, T, max_q, max_kv, heads, kv->n_kv_heads, kv->head_dim);
     void* ws = c10::cuda::CUDACachingAllocator::raw_alloc_with_stream(bytes, s);
     const int32_t st = f_attention(kv, tables, rows, cu, len, R, T, max_q, max_kv, qr.p, qr.stride, heads, (float)scale, rope.p, rope.n, outr.p,
                                    outr.stride, ws, bytes, s);

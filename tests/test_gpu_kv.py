@@ -399,6 +399,97 @@ def test_attention_of_unbalanced_scales():
         _check_attention(cache, tables, table, lens, [1, 3, 2], 2, rng, scale=scale)
 
 
+# Chunks of 128 rows and more (queries x heads of a group) take another kernel where heads are 64 wide.
+CHUNK = [40, 3, 90, 17, 65]
+
+
+@pytest.mark.parametrize("heads,H", [(16, 2), (14, 2), (4, 4), (150, 1)])
+def test_chunks_behind_pasts(heads, H):
+    rng = np.random.default_rng(heads)
+    lens = [40, 300, 513, 64, 700]
+    cache, tables, table, _ = _serve(rng, lens, H, 64, 32)
+    q = CHUNK if heads < 100 else [2, 1, 3, 0, 2]
+    _check_attention(cache, tables, table, lens, q if heads // H > 1 else [40, 190, 200, 64, 129], heads, rng, rope=True, strided=heads == 14)
+
+
+def test_chunks_of_empty_requests_hidden_pages_and_unseen_positions():
+    rng = np.random.default_rng(21)
+    lens = [0, 20, 513, 64, 130, 0]
+    cache, tables, table, _ = _serve(rng, lens, 2, 64, 16)
+    table[2, 3], table[2, 4], table[2, 20], table[4, 8], table[3, :] = -1, cache.n_pages, 2 ** 31 - 1, -7, -1
+    tables.block_table.copy_(i32(table))
+    for q in ([5, 100, 70, 9, 64, 0], [0, 0, 128, 64, 1, 3], [0, 0, 0, 0, 129, 1], [70, 70, 70, 70, 70, 70]):
+        got = _check_attention(cache, tables, table, lens, q, 16, rng, rope=True)
+        assert (got[:q[0]] == 0).all()
+
+
+def test_chunks_nan_stays_where_it_is_seen():
+    rng = np.random.default_rng(22)
+    lens, H = [200, 90], 2
+    cache, tables, table, slot = _serve(rng, lens, H, 64, 16)
+    k, v = _rows(rng, 3, H, 64), _rows(rng, 3, H, 64)
+    k[0, 1, 3], v[1, 0, 63], v[2, 1, 0] = np.inf, np.nan, -np.inf
+    at = [slot[127], slot[130], slot[200]]       # request 0: a key of head 1 at 127, a value of head 0 at 130; request 1: a value of head 1 at 0
+    moin.kv_append(cache, i32(at), _dev(k), _dev(v))
+    got = _check_attention(cache, tables, table, lens, [120, 90], H * 4, rng)
+    nan = np.isnan(got).all(-1)
+    pos = np.concatenate([np.arange(80, 200), np.arange(90)])
+    first = np.arange(210) < 120
+    assert np.array_equal(np.isnan(got).any(-1), nan)
+    assert np.array_equal(nan[:, :4], np.repeat((first & (pos >= 130))[:, None], 4, 1))
+    assert np.array_equal(nan[:, 4:], np.repeat((~first | (pos >= 127))[:, None], 4, 1))
+
+
+def test_chunks_of_unbalanced_scales():
+    rng = np.random.default_rng(23)
+    lens = [500, 200, 77]
+    cache, tables, table, slot = _serve(rng, lens, 2, 64, 32, spread=6)
+    for q_scale in (0.01, 1.0, 30.0):
+        _check_attention(cache, tables, table, lens, [150, 64, 77], 8, rng, q_scale=q_scale)
+    v = np.zeros((77, 2, 64), np.float32)
+    v[::3], v[1::3] = 5.0, -1e30
+    moin.kv_append(cache, i32(slot[700:]), _dev(_rows(rng, 77, 2, 64)), _dev(ref.bf16(v)))
+    _check_attention(cache, tables, table, lens, [1, 1, 77], 16, rng)
+    for scale in (0.0, -0.3, 2.0):
+        _check_attention(cache, tables, table, lens, [1, 30, 70], 8, rng, scale=scale)
+
+
+def test_chunk_rows_do_not_reach_one_another():
+    rng = np.random.default_rng(24)
+    lens, G = [300], 4
+    cache, tables, _, _ = _serve(rng, lens, 1, 64, 16)
+    q = ref.bf16(rng.standard_normal((100, G, 64)).astype(np.float32))
+    plain = moin.kv_attention(cache, tables, _dev(q), i32([0, 100]), i32(lens), 100, 300)
+    changed = torch.zeros(100, G, dtype=torch.bool, device=DEV)
+    for (i, h), x in {(0, 1): 1e30, (31, 2): np.nan, (32, 0): np.inf, (50, 3): 1e-30, (99, 3): -np.inf}.items():
+        q[i, h, 3:] = x
+        changed[i, h] = True
+    out = moin.kv_attention(cache, tables, _dev(q), i32([0, 100]), i32(lens), 100, 300)
+    assert torch.equal(out[~changed], plain[~changed])
+    assert out[31, 2].isnan().all() and out[32, 0].isnan().all() and out[99, 3].isnan().all() and out[50, 3].isfinite().all()
+
+
+def test_chunk_and_rows_agree():
+    """The same queries as a chunk and in pieces too small for its kernel: both within the bound of the formula, bit for bit the same
+    whenever they are asked again, and with a second call on another stream at the same time."""
+    rng = np.random.default_rng(25)
+    lens = [900, 513]
+    cache, tables, table, _ = _serve(rng, lens, 2, 64, 64)
+    got = _check_attention(cache, tables, table, lens, [64, 40], 8, rng, rope=True)
+    assert np.isfinite(got).all()
+    q = _dev(_rows(rng, 104, 8, 64) * 0 + ref.bf16(rng.standard_normal((104, 8, 64)).astype(np.float32)))
+    args = (cache, tables, q, i32([0, 64, 104]), i32(lens), 64, 900)
+    first = moin.kv_attention(*args)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        with torch.cuda.stream(side):
+            other = moin.kv_attention(*args)
+        again = moin.kv_attention(*args)
+        torch.cuda.synchronize()
+        assert torch.equal(again, first) and torch.equal(other, first)
+
+
 def test_attention_query_rows_do_not_reach_one_another():
     """Queries of 1e30, of 1e-30, infinite ones and NaN beside ordinary ones, in the same head group and chunk."""
     rng = np.random.default_rng(7)
