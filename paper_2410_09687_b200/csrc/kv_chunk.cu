@@ -31,7 +31,8 @@ constexpr int kChThreads = 320;
 constexpr int kChKeys = 64, kChRows = 128;
 constexpr int kChQ = kChRows * 64 * 2, kChKV = kChKeys * 64 * 2, kChRing = 4;
 constexpr int kChMerge = 4096;               // (maximum, sum) of every row by stream, for two items
-constexpr int kChSmem = 2 * kChQ + 2 * kChRing * kChKV + 1024 /*align*/ + 256 /*barriers*/ + kChMerge;
+constexpr int kChOrder = 256;                // requests that are put in order
+constexpr int kChSmem = 2 * kChQ + 2 * kChRing * kChKV + 1024 /*align*/ + 256 /*barriers*/ + kChMerge + kChOrder * 8;
 constexpr int kChTmemCols = 256;
 constexpr float kChTop = 10.f, kChMost = 15.f;   // log2 of the largest weight after a move of the maximum, and at all
 
@@ -53,7 +54,7 @@ struct ChunkParams {
   float* q_fac;             // [H, T G] 1 / (what the row was multiplied with)
   uint4* info;              // [R, H, tiles]: scale log2(e) 2^a, b (fp32; low bits: hidden groups, unlike tokens), mask of NaN tokens
   float2* tok;              // [R, H, tiles, 64], of tiles of unlike tokens: (scale log2(e) 2^a, b) of every token
-  int dense_blocks;
+  int dense_blocks, by_request;
   DeviceStatus* status;
 };
 
@@ -69,7 +70,7 @@ __device__ __forceinline__ ChReq ch_request(const ChunkParams& p, int req) {   /
   return r;
 }
 
-// Blocks below dense_blocks: 64 tokens of a request and kv head, a warp per 16 of them.  The others: eight query rows, a warp each.
+// Blocks below dense_blocks: 64 tokens of a request and kv head, a warp per 16 of them.  The others: the queries of a token.
 // Bound by the traffic of what they write; small beside the products.
 constexpr uint32_t kChUnlike = 0x10u;   // in the low bits of b
 constexpr int kChRange = 12;            // powers of two between the tokens of a tile that are alike
@@ -82,42 +83,54 @@ kv_dense_kernel(const ChunkParams p) {
   pdl_begin();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   if ((int)blockIdx.x >= p.dense_blocks) {
-    const long long n = (long long)p.T * p.n_heads;
-    for (int k = 0; k < 2; ++k) {   // row: token and query head
-      const long long i = ((long long)blockIdx.x - p.dense_blocks) * 8 + 2 * warp + k;
-      if (i >= n) return;
-      const int tok = (int)(i / p.n_heads), h = (int)(i % p.n_heads);
-      // the request of the token: the last one that begins at or before it
-      int lo = 0, hi = p.R;
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (p.cu_q[mid + 1] > tok) hi = mid; else lo = mid + 1;
+    const int tok = (int)blockIdx.x - p.dense_blocks;
+    // the request of the token: the first one that ends behind it
+    int lo = 0, hi = p.R;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (p.cu_q[mid + 1] > tok) hi = mid; else lo = mid + 1;
+    }
+    int pos = -1;
+    if (lo < p.R) {
+      const ChReq r = ch_request(p, lo);
+      if (tok >= r.t0 && tok < r.t0 + r.q_len) pos = r.kv_len - r.q_len + tok - r.t0;
+    }
+    // two heads at a time, a lane the pairs (c, c + 32), (c + 1, c + 33) of one
+    const int c = 2 * (lane & 15);
+    float4 cs = make_float4(1.f, 0.f, 1.f, 0.f);
+    if (p.rope != nullptr && pos >= 0) cs = __ldg(reinterpret_cast<const float4*>(p.rope + (size_t)pos * 32 + c));
+#pragma unroll 2
+    for (int h0 = 2 * warp; h0 < p.n_heads; h0 += 8) {
+      const int h = h0 + (lane >> 4);
+      const bool there = h < p.n_heads;
+      uint32_t a = 0u, b = 0u;
+      if (pos >= 0 && there) {
+        const __nv_bfloat16* src = p.q + (long long)tok * p.q_stride + (long long)h * 64 + c;
+        a = __ldg(reinterpret_cast<const uint32_t*>(src));
+        b = __ldg(reinterpret_cast<const uint32_t*>(src + 32));
       }
-      float a = 0.f, b = 0.f;
-      if (lo < p.R) {
-        const ChReq r = ch_request(p, lo);
-        const int pos = r.kv_len - r.q_len + tok - r.t0;
-        if (tok >= r.t0 && tok < r.t0 + r.q_len && pos >= 0) {
-          const __nv_bfloat16* src = p.q + (long long)tok * p.q_stride + (long long)h * 64;
-          a = __bfloat162float(src[lane]);
-          b = __bfloat162float(src[lane + 32]);
-          if (p.rope != nullptr) {
-            const float2 cs = __ldg(p.rope + (size_t)pos * 32 + lane);
-            const float x = round_bf16(kv_rot_lo(a, b, cs)), y = round_bf16(kv_rot_hi(a, b, cs));
-            a = x;
-            b = y;
-          }
-        }
+      float x0 = bf16_lo(a), x1 = bf16_hi(a), y0 = bf16_lo(b), y1 = bf16_hi(b);
+      if (p.rope != nullptr) {
+        const float2 c0 = make_float2(cs.x, cs.y), c1 = make_float2(cs.z, cs.w);
+        const float u0 = round_bf16(kv_rot_lo(x0, y0, c0)), u1 = round_bf16(kv_rot_lo(x1, y1, c1));
+        y0 = round_bf16(kv_rot_hi(x0, y0, c0));
+        y1 = round_bf16(kv_rot_hi(x1, y1, c1));
+        x0 = u0;
+        x1 = u1;
       }
-      float top = fmaxf(fabsf(a), fabsf(b));
+      float top = fmaxf(fmaxf(fabsf(x0), fabsf(x1)), fmaxf(fabsf(y0), fabsf(y1)));
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      // 2^(9 - exponent of the largest element); a row of zeros, subnormals or infinities stays as it is
       const int e = (int)(__float_as_uint(top) >> 23) - 127;
       const float f = (e > -118 && e < 128) ? __uint_as_float((uint32_t)(9 - e + 127) << 23) : 1.f;
-      const long long row = (long long)(h / p.G) * p.T * p.G + (long long)tok * p.G + h % p.G;
-      p.qd[row * 64 + lane] = __float2half_rn(a * f);
-      p.qd[row * 64 + 32 + lane] = __float2half_rn(b * f);
-      if (lane == 0) p.q_fac[row] = 1.f / f;
+      if (!there) continue;
+      const int kvh = h / p.G;
+      const long long row = (long long)kvh * p.T * p.G + (long long)tok * p.G + (h - kvh * p.G);
+      const __half2 lo2 = __floats2half2_rn(x0 * f, x1 * f), hi2 = __floats2half2_rn(y0 * f, y1 * f);
+      *reinterpret_cast<__half2*>(p.qd + row * 64 + c) = lo2;
+      *reinterpret_cast<__half2*>(p.qd + row * 64 + c + 32) = hi2;
+      if ((lane & 15) == 0) p.q_fac[row] = 1.f / f;
     }
     return;
   }
@@ -246,12 +259,24 @@ kv_dense_kernel(const ChunkParams p) {
 }
 
 struct ChItem { int req, head, row0, t0, n_rows, past, first_pos, last_pos, n_tiles; bool on; };
-__device__ __forceinline__ ChItem ch_item(const ChunkParams& p, int idx) {
+// The k-th item of a CTA: items stand longest first as far as their place tells, and CTAs take them there and back again, so that one
+// that began with a long item ends with a short one.  Where pasts are longer than chunks the requests count (`order`: longest
+// first), else the row blocks.
+__device__ __forceinline__ int ch_index(int k) { return (k & 1) ? (k + 1) * (int)gridDim.x - 1 - (int)blockIdx.x : k * (int)gridDim.x + (int)blockIdx.x; }
+__device__ __forceinline__ ChItem ch_item(const ChunkParams& p, const int* order, int idx) {
   ChItem it;
-  const int per = p.R * p.kv.H;
-  const int blk = p.n_blk - 1 - idx / per, rem = idx % per;   // longest blocks first
-  it.req = rem / p.kv.H;
-  it.head = rem % p.kv.H;
+  int blk;
+  if (p.by_request) {
+    const int per = p.n_blk * p.kv.H, at = idx / per, rem = idx % per;
+    it.req = order[at];
+    blk = p.n_blk - 1 - rem / p.kv.H;
+    it.head = rem % p.kv.H;
+  } else {
+    const int per = p.R * p.kv.H, rem = idx % per;
+    blk = p.n_blk - 1 - idx / per;
+    it.req = rem / p.kv.H;
+    it.head = rem % p.kv.H;
+  }
   it.row0 = blk * kChRows;
   const ChReq r = ch_request(p, it.req);
   it.t0 = r.t0;
@@ -307,6 +332,17 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     tmem_relinquish();
   }
   pdl_begin();
+  int* order = reinterpret_cast<int*>(bar_ptr + 256 + kChMerge);
+  if (p.by_request) {
+    int* len = order + kChOrder;
+    for (int i = threadIdx.x; i < p.R; i += kChThreads) len[i] = p.kv_len[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.R; i += kChThreads) {
+      int rank = 0;
+      for (int k = 0; k < p.R; ++k) rank += len[k] > len[i] || (len[k] == len[i] && k < i);
+      order[rank] = i;
+    }
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -326,14 +362,16 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         ++nq;
         return true;
       };
-      auto next = [&](int& i, ChItem& out) -> bool {   // the next item that has tiles
-        for (i += gridDim.x; i < n_items; i += gridDim.x) {
-          out = ch_item(p, i);
+      auto next = [&](int& k, ChItem& out) -> bool {   // the next item that has tiles
+        for (++k; k * (int)gridDim.x < n_items; ++k) {
+          const int i = ch_index(k);
+          if (i >= n_items) continue;
+          out = ch_item(p, order, i);
           if (out.n_tiles > 0) return true;
         }
         return false;
       };
-      int idx = (int)blockIdx.x - (int)gridDim.x;
+      int idx = -1;
       ChItem it, nx;
       bool have = next(idx, it);
       if (have) ok = load_q(it);
@@ -362,8 +400,10 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     uint32_t tq = 0, nit = 0;
     uint32_t n_p[2] = {0, 0};   // products issued per stream
     bool ok = true;
-    for (int idx = blockIdx.x; idx < n_items && ok; idx += gridDim.x) {
-      const ChItem it = ch_item(p, idx);
+    for (int k = 0; k * (int)gridDim.x < n_items && ok; ++k) {
+      const int idx = ch_index(k);
+      if (idx >= n_items) continue;
+      const ChItem it = ch_item(p, order, idx);
       if (it.n_tiles == 0) continue;
       const uint32_t qb = nit & 1u;
       if (!(ok = mbar_wait_warp(qfull + 8 * qb, (nit >> 1) & 1u, abort_flag, p.status, 64))) break;
@@ -447,8 +487,10 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     float2* xml = reinterpret_cast<float2*>(bar_ptr + 256);   // [item parity][stream][row]: (maximum, sum)
     uint32_t n_s = 0, nit = 0;
     bool ok = true;
-    for (int idx = blockIdx.x; idx < n_items; idx += gridDim.x) {
-      const ChItem it = ch_item(p, idx);
+    for (int kk = 0; kk * (int)gridDim.x < n_items; ++kk) {
+      const int idx = ch_index(kk);
+      if (idx >= n_items) continue;
+      const ChItem it = ch_item(p, order, idx);
       if (!it.on) continue;
       const int r = it.row0 + row, qi = ch_div_g(p, min(r, it.n_rows - 1));
       const bool live = r < it.n_rows;
@@ -706,6 +748,7 @@ moin_status launch_kv_chunk(HostState* hs, const KvView& kv, const int* table, c
   p.q = q; p.q_stride = q_stride; p.out = out; p.out_stride = out_stride; p.rope = rope; p.scale_log2 = scale_log2;
   p.kd = (__half*)(w + c.kd); p.vd = (__half*)(w + c.vd); p.qd = (__half*)(w + c.qd); p.q_fac = (float*)(w + c.fac); p.info = (uint4*)(w + c.info); p.tok = (float2*)(w + c.tok);
   p.dense_blocks = R * kv.H * p.tiles;
+  p.by_request = R > 1 && R <= kChOrder && max_kv > 2 * (long long)max_q;
   p.status = hs->status;
   CUtensorMap mq, mk, mv;
   const uint64_t dense_rows = (uint64_t)R * p.tiles * kChKeys;
@@ -715,7 +758,7 @@ moin_status launch_kv_chunk(HostState* hs, const KvView& kv, const int* table, c
   if (st) return st;
   cudaError_t e = ensure_smem_optin(OPTIN_KV_CHUNK, kv_chunk_kernel, kChSmem);
   if (e != cudaSuccess) return record_cuda(e);
-  const long long q_blocks = ((long long)T * n_heads + 7) / 8, items = (long long)p.n_blk * R * kv.H;
+  const long long q_blocks = T, items = (long long)p.n_blk * R * kv.H;
   ProfScope prof(MOIN_K_KV_ATTENTION, 2, s);
   e = launch_pdl(kv_dense_kernel, (unsigned)(p.dense_blocks + q_blocks), 128, 0, s, p);
   if (e == cudaSuccess)
