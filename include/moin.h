@@ -91,7 +91,8 @@ moin_status moin_selftest_bounded_wait(int32_t limit_us, int32_t* result, moin_s
 
 /* Testing/tuning knobs (host-side path selection only; every path computes the same function).
  *   MOIN_OPT_GEMM_IMPL: 0 = automatic, 1 = force the warp-MMA kernels, 2 = force the tcgen05 kernels
- *                       (calls whose shapes the forced kernel cannot take fail with MOIN_ERR_BAD_SHAPE). */
+ *                       (calls whose shapes the forced kernel cannot take fail with MOIN_ERR_BAD_SHAPE; attention over a
+ *                       cache takes the other one then). */
 /*   MOIN_OPT_NVTX: 1 = every kernel group the library launches is wrapped in an NVTX range named like
  *   moin_kernel_name() (for timelines of tools that read NVTX); 0 (default) = no ranges. */
 enum { MOIN_OPT_GEMM_IMPL = 1, MOIN_OPT_NVTX = 3 };
@@ -111,7 +112,7 @@ enum {
   MOIN_K_ROUTE_SIMPLE = 0, MOIN_K_ROUTE_TC = 1, MOIN_K_ROUTE_FINISH = 2, MOIN_K_PLAN = 3, MOIN_K_GEMM_WARP = 4,
   MOIN_K_GEMM_TC = 5, MOIN_K_SHRINK_STREAM = 6, MOIN_K_EXPAND_STREAM = 7, MOIN_K_SHRINK_TC = 8,
   MOIN_K_FUSED_TC = 9, MOIN_K_GLUE = 10, MOIN_K_ATTENTION = 11, MOIN_K_ROUTE_CLUSTER = 12, MOIN_K_KMEANS_UPDATE = 13,
-  MOIN_K_KV_TABLES = 14, MOIN_K_KV_STORE = 15, MOIN_K_KV_ATTENTION = 16, MOIN_K_COUNT = 17
+  MOIN_K_KV_TABLES = 14, MOIN_K_KV_STORE = 15, MOIN_K_KV_ATTENTION = 16, MOIN_K_KV_CHUNK = 17, MOIN_K_COUNT = 18
 };
 moin_status moin_profile_enable(int32_t capacity);
 moin_status moin_profile_read(moin_profile_record* out, int32_t capacity, int32_t* n);

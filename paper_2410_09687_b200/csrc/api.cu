@@ -14,6 +14,8 @@ static thread_local int t_last_cuda_error = 0;
 static HostState g_states[kMaxDevices];
 static int g_opt_gemm_impl = 0, g_opt_nvtx = 0;   // moin_set_option: process-wide
 
+int gemm_impl_option() { return g_opt_gemm_impl; }
+
 moin_status record_cuda(cudaError_t e) {
   if (e == cudaSuccess) return MOIN_OK;
   t_last_cuda_error = (int)e;
@@ -187,7 +189,7 @@ const char* moin_kernel_name(int32_t k) {
   static const char* names[MOIN_K_COUNT] = {"route_simple", "route_tc", "route_finish", "plan", "gemm_warp", "gemm_tc",
                                             "lora_shrink_stream", "lora_expand_stream", "lora_shrink_tc",
                                             "lora_fused_tc", "decoder_glue", "attention", "route_cluster", "kmeans_update",
-                                            "kv_tables", "kv_store", "kv_attention"};
+                                            "kv_tables", "kv_store", "kv_attention", "kv_chunk"};
   return (k >= 0 && k < MOIN_K_COUNT) ? names[k] : "unknown";
 }
 

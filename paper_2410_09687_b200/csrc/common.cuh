@@ -274,6 +274,7 @@ struct HostState {
   size_t smem_optin[kOptinSlots] = {};   // dynamic shared memory already opted in, per kernel (see ensure_smem_optin)
 };
 moin_status host_state(HostState** out);      // lazily initialised for the current device
+int gemm_impl_option();                       // MOIN_OPT_GEMM_IMPL, also where there is no device (size queries)
 moin_status record_cuda(cudaError_t e);       // MOIN_OK or MOIN_ERR_CUDA (remembers e)
 
 // Kernels that need more than 48 KB of dynamic shared memory opt in with cudaFuncSetAttribute; the driver keeps

@@ -855,12 +855,27 @@ extern "C" moin_status moin_rope_table(float* table, int32_t n_pos, int32_t head
 // Row blocks of 8 NT rows: as many as a request has, up to what the registers hold.
 static int kv_nt(long long tall) { return tall <= 8 ? 1 : 2; }
 
-// Long chunks go to the tcgen05 kernel: TODO
+// Long chunks go to the tcgen05 kernel (kv_chunk.cu) where the times that both would take, in us as fitted to measurements, say so:
+// here a row of queries passes 0.7 keys per ns and pays for beginning an item; there 128 rows pass 1.9 keys per ns and row, an item costs
+// 11 us of one of 296 CTAs, a chain of tiles is as long as the longest request, and keys and values are laid out first.  Measured, here /
+// there, with heads 32 on 4 kv heads, chunks of q behind pasts of p tokens:
+//   R = 1    p 500   q 64 17.9 / 18.6   q 128 24.2 / 22.1   q 512 40 / 29      p 4000  q 64 30 / 75   q 256 65 / 78    q 512 119 / 95
+//   R = 8    p 500   q 32 23.0 / 22.1   q 128 48.6 / 29.4   q 512 210 / 105    p 4000  q 32 63 / 86   q 64 110 / 100   q 512 824 / 394
+//   R = 64   p 1     q 64 48 / 53       q 128 108 / 107     q 256 306 / 228    p 4000  q 16 201 / 198 q 64 758 / 464   q 256 3100 / 1390
 static bool kv_use_chunk(int R, int T, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim, float scale) {
-  const long long G = n_heads / n_kv_heads, tiles = ((long long)max_kv + 63) / 64;
-  if (head_dim != 64 || !(scale > 0.f) || max_q * G < 128) return false;
+  const double G = n_heads / n_kv_heads, H = n_kv_heads;
+  const int impl = gemm_impl_option();   // 1: the kernel here, 2: the other wherever it can take the call
+  if (head_dim != 64 || !(scale > 0.f) || impl == 1 || (impl == 0 && max_q * G < 64)) return false;
+  const double tiles = (max_kv + 63) / 64, queries = T < (double)R * max_q ? T : (double)R * max_q;
+  double items = (double)(long long)((max_q * G + 127) / 128) * R * H;
+  if (items > queries * n_heads / 128 + R * H) items = queries * n_heads / 128 + R * H;
   // (the tensors that are laid out: at most 1 GiB; their blocks and rows, and the work items, within 32 bits)
-  return (max_q * G / 128 + 1) * R * n_kv_heads < (1ll << 30) && (long long)R * tiles * 64 * n_kv_heads * 256 + (long long)T * n_heads * 132 <= (1ll << 30) && (long long)T * n_heads <= (1ll << 30);
+  if (R * tiles * 64 * H * 264 + (double)T * n_heads * 132 > (1ll << 30) || (max_q * G / 128 + 1) * R * H > (1ll << 30)) return false;
+  if (impl == 2) return true;
+  const double keys = max_kv - 0.5 * (max_q < max_kv ? max_q : max_kv);
+  const double here = 8 + queries * n_heads * (keys + 200) / 0.7e6;
+  const double chain = 0.0165 * max_kv, work = items / 296 * 11 + items * 128 * keys / 1.9e6;
+  return 12 + (chain > work ? chain : work) + 1e-4 * R * H * max_kv < here;
 }
 
 extern "C" size_t moin_kv_attention_workspace_bytes(int32_t R, int32_t T, int32_t max_q, int32_t max_kv, int32_t n_heads, int32_t n_kv_heads,

@@ -759,7 +759,7 @@ moin_status launch_kv_chunk(HostState* hs, const KvView& kv, const int* table, c
   cudaError_t e = ensure_smem_optin(OPTIN_KV_CHUNK, kv_chunk_kernel, kChSmem);
   if (e != cudaSuccess) return record_cuda(e);
   const long long q_blocks = T, items = (long long)p.n_blk * R * kv.H;
-  ProfScope prof(MOIN_K_KV_ATTENTION, 2, s);
+  ProfScope prof(MOIN_K_KV_CHUNK, 2, s);
   e = launch_pdl(kv_dense_kernel, (unsigned)(p.dense_blocks + q_blocks), 128, 0, s, p);
   if (e == cudaSuccess)
     e = launch_pdl(kv_chunk_kernel, (unsigned)(items < 2L * hs->n_sms ? items : 2L * hs->n_sms), kChThreads, kChSmem, s, mq, mk, mv, p);

@@ -5,6 +5,7 @@ import torch
 
 import kv_ref as ref
 import paper_2410_09687_b200 as moin
+from gpu_util import kernel_launches
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -399,12 +400,19 @@ def test_attention_of_unbalanced_scales():
         _check_attention(cache, tables, table, lens, [1, 3, 2], 2, rng, scale=scale)
 
 
-# Chunks of 128 rows and more (queries x heads of a group) take another kernel where heads are 64 wide.
+# Long chunks have a kernel of their own where heads are 64 wide; here every call is made with either.
 CHUNK = [40, 3, 90, 17, 65]
 
 
+@pytest.fixture(params=["rows", "tcgen05"])
+def kernel(request):
+    moin.set_option(moin.OPT_GEMM_IMPL, 1 + (request.param == "tcgen05"))
+    yield request.param
+    moin.set_option(moin.OPT_GEMM_IMPL, 0)
+
+
 @pytest.mark.parametrize("heads,H", [(16, 2), (14, 2), (4, 4), (150, 1)])
-def test_chunks_behind_pasts(heads, H):
+def test_chunks_behind_pasts(heads, H, kernel):
     rng = np.random.default_rng(heads)
     lens = [40, 300, 513, 64, 700]
     cache, tables, table, _ = _serve(rng, lens, H, 64, 32)
@@ -412,7 +420,7 @@ def test_chunks_behind_pasts(heads, H):
     _check_attention(cache, tables, table, lens, q if heads // H > 1 else [40, 190, 200, 64, 129], heads, rng, rope=True, strided=heads == 14)
 
 
-def test_chunks_of_empty_requests_hidden_pages_and_unseen_positions():
+def test_chunks_of_empty_requests_hidden_pages_and_unseen_positions(kernel):
     rng = np.random.default_rng(21)
     lens = [0, 20, 513, 64, 130, 0]
     cache, tables, table, _ = _serve(rng, lens, 2, 64, 16)
@@ -423,7 +431,7 @@ def test_chunks_of_empty_requests_hidden_pages_and_unseen_positions():
         assert (got[:q[0]] == 0).all()
 
 
-def test_chunks_nan_stays_where_it_is_seen():
+def test_chunks_nan_stays_where_it_is_seen(kernel):
     rng = np.random.default_rng(22)
     lens, H = [200, 90], 2
     cache, tables, table, slot = _serve(rng, lens, H, 64, 16)
@@ -440,7 +448,7 @@ def test_chunks_nan_stays_where_it_is_seen():
     assert np.array_equal(nan[:, 4:], np.repeat((~first | (pos >= 127))[:, None], 4, 1))
 
 
-def test_chunks_of_unbalanced_scales():
+def test_chunks_of_unbalanced_scales(kernel):
     rng = np.random.default_rng(23)
     lens = [500, 200, 77]
     cache, tables, table, slot = _serve(rng, lens, 2, 64, 32, spread=6)
@@ -454,7 +462,7 @@ def test_chunks_of_unbalanced_scales():
         _check_attention(cache, tables, table, lens, [1, 30, 70], 8, rng, scale=scale)
 
 
-def test_chunk_rows_do_not_reach_one_another():
+def test_chunk_rows_do_not_reach_one_another(kernel):
     rng = np.random.default_rng(24)
     lens, G = [300], 4
     cache, tables, _, _ = _serve(rng, lens, 1, 64, 16)
@@ -469,17 +477,15 @@ def test_chunk_rows_do_not_reach_one_another():
     assert out[31, 2].isnan().all() and out[32, 0].isnan().all() and out[99, 3].isnan().all() and out[50, 3].isfinite().all()
 
 
-def test_chunk_and_rows_agree():
-    """The same queries as a chunk and in pieces too small for its kernel: both within the bound of the formula, bit for bit the same
-    whenever they are asked again, and with a second call on another stream at the same time."""
+def test_chunks_the_same_bits_and_beside_one_another(kernel):
+    """Asked again, and with a second call on another stream at the same time; and the kernel is the one meant."""
     rng = np.random.default_rng(25)
     lens = [900, 513]
     cache, tables, table, _ = _serve(rng, lens, 2, 64, 64)
-    got = _check_attention(cache, tables, table, lens, [64, 40], 8, rng, rope=True)
-    assert np.isfinite(got).all()
-    q = _dev(_rows(rng, 104, 8, 64) * 0 + ref.bf16(rng.standard_normal((104, 8, 64)).astype(np.float32)))
+    q = _dev(ref.bf16(rng.standard_normal((104, 8, 64)).astype(np.float32)))
     args = (cache, tables, q, i32([0, 64, 104]), i32(lens), 64, 900)
     first = moin.kv_attention(*args)
+    assert list(kernel_launches(lambda: moin.kv_attention(*args))) == ["kv_chunk" if kernel == "tcgen05" else "kv_attention"]
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     for _ in range(5):
@@ -488,6 +494,22 @@ def test_chunk_and_rows_agree():
         again = moin.kv_attention(*args)
         torch.cuda.synchronize()
         assert torch.equal(again, first) and torch.equal(other, first)
+
+
+@pytest.mark.parametrize("lens,q", [([3000, 2990, 17], [300, 1, 17]), ([64] * 70, [64] * 70), ([700] * 5, [129, 128, 127, 1, 64])])
+def test_chunks_of_many_items(lens, q, kernel):
+    """More items than CTAs, rows of items that end in a request's last tile, the longest request first and last."""
+    rng = np.random.default_rng(len(lens))
+    cache, tables, table, _ = _serve(rng, lens, 1, 64, 16)
+    _check_attention(cache, tables, table, lens, q, 2 if len(lens) > 9 else 3, rng, rope=True)
+
+
+def test_the_rule_sends_long_chunks_to_the_tensor_cores():
+    rng = np.random.default_rng(26)
+    cache, tables, _, _ = _serve(rng, [600, 600], 4, 64, 64)
+    for n, name in ((1, "kv_attention"), (256, "kv_chunk")):
+        q = _dev(ref.bf16(rng.standard_normal((2 * n, 32, 64)).astype(np.float32)))
+        assert list(kernel_launches(lambda: moin.kv_attention(cache, tables, q, i32([0, n, 2 * n]), i32([600, 600]), n, 600))) == [name]
 
 
 def test_attention_query_rows_do_not_reach_one_another():
