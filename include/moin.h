@@ -479,7 +479,7 @@ size_t moin_kv_bytes(int32_t n_pages, int32_t page_tokens, int32_t n_kv_heads, i
 /* Page tables of up to n_rows requests, shared by the caches of all layers (a page id means the same page in each).  All
  * device memory, the caller's. */
 typedef struct {
-  int32_t* block_table; /* [n_rows, max_pages] page of every 16.. tokens of a row's request; only entries of held pages mean anything */
+  int32_t* block_table; /* [n_rows, max_pages] pages of a row's request in order; only entries of held pages mean anything */
   int32_t* free_pages;  /* [n_pages] a stack: entries below *n_free are the free pages, the last one is taken first */
   int32_t* lens;        /* [n_rows] cached tokens */
   int32_t* n_free;      /* [1] */
@@ -539,8 +539,8 @@ moin_status moin_rope_table(float* table, int32_t n_pos, int32_t head_dim, float
  *   rope     nullable, as for moin_kv_append, rope_len >= max_kv: queries are rotated by their position (fp32, rounded to bf16)
  *   rows     [R] rows of the tables, NULL: row i
  *   max_q, max_kv   host upper bounds of a request's queries and cached tokens (outside 1..T / 1..max_pages * page_tokens: those)
- * A query that sees nothing (kv_len 0, a position before the first) gets zeros; so do the queries of a request whose row or kv_len is
- * out of range.  A page id outside [0, n_pages) hides its tokens.  Rows of out behind cu_q[R] stay as they were.  fp32 scores, softmax and
+ * A query that sees nothing (kv_len 0, a position before the first) gets zeros; so do the queries (at most max_q of them) of a request
+ * whose row or kv_len is out of range or whose queries are more than max_q.  A page id outside [0, n_pages) hides its tokens.  Rows of out behind cu_q[R] stay as they were.  fp32 scores, softmax and
  * sums; the un-normalised weights times the value's scale enter the second product rounded to fp16, relative to the row's largest.
  * Scratch: workspace, moin_kv_attention_workspace_bytes(...) bytes with the bounds that the call goes by (up to about 1 GiB where long
  * chunks attend to long requests: keys and values are then laid out in 16 bits for the tensor cores), 16-byte aligned, of this call alone while it runs.

@@ -641,11 +641,14 @@ class KvCache:
         self.pages = pages
         self.n_pages, self.n_kv_heads = pages.shape[0], pages.shape[1]
         self.page_tokens, self.head_dim = pages.shape[2] * 16, pages.shape[3] * 64
+        self.device = pages.get_device()
         self.c = _Kv(_ptr(pages), self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim)
         self.addr = ctypes.addressof(self.c)
 
     @classmethod
     def empty(cls, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, device) -> "KvCache":
+        if page_tokens not in (16, 32, 64, 128) or head_dim not in (64, 128):
+            raise MoinError(f"pages of {page_tokens} tokens, heads of {head_dim}: pages hold 16, 32, 64 or 128 tokens, heads are 64 or 128 wide")
         return cls(torch.empty(n_pages, n_kv_heads, page_tokens // 16, head_dim // 64, 1152, dtype=torch.uint8, device=device))
 
 
@@ -665,6 +668,9 @@ class KvTables:
         self.block_table, self.free_pages, self.lens, self.n_free = block_table, free_pages, lens, n_free
         self.n_rows, self.max_pages = block_table.shape
         self.n_pages, self.page_tokens = free_pages.shape[0], page_tokens
+        self.device = block_table.get_device()
+        if any(t.get_device() != self.device for t in (free_pages, lens, n_free)):
+            raise MoinError("the tables' tensors must live on one device")
         self.c = _KvTables(_ptr(block_table), _ptr(free_pages), _ptr(lens), _ptr(n_free), self.n_rows, self.max_pages, self.n_pages,
                            page_tokens)
         self.addr = ctypes.addressof(self.c)
@@ -688,8 +694,17 @@ class KvBatch:
         i32 = lambda n: torch.empty(n, dtype=torch.int32, device=device)  # noqa: E731
         self.R, self.T = R, T
         self.cu_q, self.kv_len, self.slot, self.pos, self.refused = i32(R + 1), i32(R), i32(T), i32(T), i32(1)
+        self.device = self.cu_q.get_device()
         self.c = _KvBatch(R, T, *[_ptr(t) for t in (self.cu_q, self.kv_len, self.slot, self.pos, self.refused)])
         self.addr = ctypes.addressof(self.c)
+
+
+def _same_device(*holders) -> int:
+    first = holders[0].device
+    for h in holders:
+        if h.device != first:
+            raise MoinError("cache, tables and batch must live on one device")
+    return first
 
 
 def _handle(stream) -> Optional[int]:
@@ -699,7 +714,9 @@ def _handle(stream) -> Optional[int]:
 def kv_update(tables: KvTables, want: torch.Tensor, batch: KvBatch, rows: Optional[torch.Tensor] = None,
               lens_out: Optional[torch.Tensor] = None, n_free_out: Optional[torch.Tensor] = None, stream=None) -> KvBatch:
     """moin_kv_update: request i (row ``rows[i]`` of the tables, or i) becomes ``want[i]`` tokens long.  Returns ``batch``."""
-    st = (_steps or _load_steps()).update(tables.addr, batch.addr, rows, want, lens_out, n_free_out, _handle(stream))
+    if batch.device != tables.device:
+        raise MoinError("tables and batch must live on one device")
+    st = (_steps or _load_steps()).update(tables.addr, batch.addr, rows, want, lens_out, n_free_out, _handle(stream), tables.device)
     if st:
         _check(st, "moin_kv_update")
     return batch
@@ -716,14 +733,14 @@ def kv_append(cache: KvCache, slot: torch.Tensor, k: torch.Tensor, v: torch.Tens
               rope: Optional[torch.Tensor] = None, stream=None) -> None:
     """moin_kv_append: quantise row t of ``k`` (rotated by ``rope`` at ``pos[t]`` if given) and ``v`` and store them in ``slot[t]``.
     k and v: bf16 [T, n_kv_heads, head_dim] or [T, n_kv_heads * head_dim], tokens may lie apart."""
-    st = (_steps or _load_steps()).append(cache.addr, slot, k, v, pos, rope, _handle(stream))
+    st = (_steps or _load_steps()).append(cache.addr, slot, k, v, pos, rope, _handle(stream), cache.device)
     if st:
         _check(st, "moin_kv_append")
 
 
 def kv_read(cache: KvCache, slot: torch.Tensor, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None, stream=None) -> tuple:
     """moin_kv_read: (k, v), bf16 [T, n_kv_heads, head_dim], of what the slots hold."""
-    st, k, v = (_steps or _load_steps()).read(cache.addr, slot, k, v, _handle(stream))
+    st, k, v = (_steps or _load_steps()).read(cache.addr, slot, k, v, _handle(stream), cache.device)
     if st:
         _check(st, "moin_kv_read")
     return k, v
@@ -735,7 +752,8 @@ def kv_attention(cache: KvCache, tables: KvTables, q: torch.Tensor, cu_q: torch.
     """moin_kv_attention: q [T, n_heads, head_dim] over the cached tokens of each token's request.  Returns out, like q; rows of a new
     ``out`` behind the last request are undefined.  scale: 1 / sqrt(head_dim) unless given.  The scratch comes from the caching
     allocator and is this call's alone: calls, streams and captured graphs may overlap."""
-    st, out = (_steps or _load_steps()).attention(cache.addr, tables.addr, q, cu_q, kv_len, max_q, max_kv, rows, scale, rope, out, _handle(stream))
+    st, out = (_steps or _load_steps()).attention(cache.addr, tables.addr, q, cu_q, kv_len, max_q, max_kv, rows, scale, rope, out, _handle(stream),
+                                                   _same_device(cache, tables))
     if st:
         _check(st, "moin_kv_attention")
     return out
@@ -774,6 +792,9 @@ def decoder_forward_cached(model: DecoderModel, tokens: torch.Tensor, layers: Kv
     for t, n in ((tokens, T), (rows, R), (req_expert, R)):
         if t is not None and (t.dtype != torch.int32 or t.shape != (n,)):
             raise MoinError(f"expected {n} int32 values, got {tuple(t.shape)} of {t.dtype}")
+    where = _same_device(tables, batch, *layers.caches)
+    if where != torch.cuda.current_device() or any(t is not None and t.get_device() != where for t in (tokens, rows, req_expert, rope, logits, hidden_in, hidden_out, workspace)):
+        raise MoinError("caches, tables and tensors must live on the current device")
     s = _stream(stream)
     capacity = tables.max_pages * tables.page_tokens
     max_kv = max_kv if 1 <= max_kv <= capacity else capacity

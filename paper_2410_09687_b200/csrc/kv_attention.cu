@@ -95,6 +95,7 @@ __device__ __forceinline__ KvItem kv_item(const KvAttParams& p, int req, int hea
   it.kv_len = p.kv_len[req];
   const int row = p.rows ? p.rows[req] : req;
   if (it.kv_len < 0 || it.kv_len > p.max_kv || it.q_len > p.max_q || row < 0 || row >= p.n_rows) it.kv_len = 0;
+  it.q_len = min(it.q_len, p.max_q);   // (bounds that do not hold: nothing behind them is touched)
   it.table = p.table + (size_t)(it.kv_len ? row : 0) * p.max_pages;
   return it;
 }
@@ -391,7 +392,7 @@ __device__ __forceinline__ int kv_count(int kv_len, int max_kv) {
 }
 __device__ __forceinline__ long long kv_cost(const KvAttParams& p, int req, int rows) {
   const int t0 = min(max(p.cu_q[req], 0), p.T), t1 = min(max(p.cu_q[req + 1], t0), p.T);
-  const int blocks = (int)(((long long)(t1 - t0) * p.G + rows - 1) / rows);
+  const int blocks = (int)(((long long)min(t1 - t0, p.max_q) * p.G + rows - 1) / rows);
   return (long long)blocks * p.kv.H * kv_count(p.kv_len[req], p.max_kv);
 }
 

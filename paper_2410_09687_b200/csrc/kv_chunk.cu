@@ -67,6 +67,7 @@ __device__ __forceinline__ ChReq ch_request(const ChunkParams& p, int req) {   /
   r.kv_len = p.kv_len[req];
   r.row = p.rows ? p.rows[req] : req;
   if (r.kv_len < 0 || r.kv_len > p.max_kv || r.q_len > p.max_q || r.row < 0 || r.row >= p.n_rows) r.kv_len = 0;
+  r.q_len = min(r.q_len, p.max_q);
   return r;
 }
 

@@ -51,6 +51,11 @@ int32_t size32(PyObject* o) {
 }
 // The library launches on the current device.
 bool here(const at::Tensor& t) { return t.is_cuda() && t.get_device() == c10::cuda::current_device(); }
+void holder_here(PyObject* device) {   // of a cache, of tables
+  const int64_t d = integer(device);
+  if (d != c10::cuda::current_device())
+    refuse("the cache or tables are on device " + std::to_string(d) + ", the current one is " + std::to_string(c10::cuda::current_device()));
+}
 // int32 vector of n entries; None: no vector
 int32_t* vec(PyObject* o, int64_t n) {
   if (o == Py_None) return nullptr;
@@ -114,18 +119,20 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (tables, batch, rows, want, lens_out, n_free_out, stream) -> status; structs by address
+// (tables, batch, rows, want, lens_out, n_free_out, stream, their device) -> status; structs by address
 PyObject* update(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 7, [&] {
+  return guarded(n, 8, [&] {
+    holder_here(a[7]);
     const auto* tables = reinterpret_cast<const moin_kv_tables*>((intptr_t)integer(a[0]));
     const auto* batch = reinterpret_cast<const moin_kv_batch*>((intptr_t)integer(a[1]));
     return PyLong_FromLong(f_update(tables, vec(a[2], batch->R), vec(a[3], batch->R), batch, vec(a[4], tables->n_rows), vec(a[5], 1), stream_of(a[6])));
   });
 }
 
-// (cache, slot, k, v, pos, rope, stream) -> status
+// (cache, slot, k, v, pos, rope, stream, the cache's device) -> status
 PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 7, [&] {
+  return guarded(n, 8, [&] {
+    holder_here(a[7]);
     const auto* kv = reinterpret_cast<const moin_kv*>((intptr_t)integer(a[0]));
     const int32_t T = length(tensor(a[1]));
     const Rows k = rows_of(tensor(a[2]), T, kv->n_kv_heads, kv->head_dim), v = rows_of(tensor(a[3]), T, kv->n_kv_heads, kv->head_dim);
@@ -134,9 +141,10 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (cache, slot, k, v, stream) -> (status, k, v); None for k or v: a new tensor
+// (cache, slot, k, v, stream, the cache's device) -> (status, k, v); None for k or v: a new tensor
 PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 5, [&] {
+  return guarded(n, 6, [&] {
+    holder_here(a[5]);
     const auto* kv = reinterpret_cast<const moin_kv*>((intptr_t)integer(a[0]));
     const at::Tensor& slot = tensor(a[1]);
     const int32_t T = length(slot);
@@ -149,11 +157,12 @@ PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (cache, tables, q, cu_q, kv_len, max_q, max_kv, rows, scale, rope, out, stream) -> (status, out); None for out: a new tensor, for
+// (cache, tables, q, cu_q, kv_len, max_q, max_kv, rows, scale, rope, out, stream, device) -> (status, out); None for out: a new tensor, for
 // scale: 1 / sqrt(head_dim).  The scratch is a block of the caching allocator that belongs to the stream: given back when the call
 // has returned, it is handed out again only to work behind it.
 PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 12, [&] {
+  return guarded(n, 13, [&] {
+    holder_here(a[12]);
     const auto* kv = reinterpret_cast<const moin_kv*>((intptr_t)integer(a[0]));
     const auto* tables = reinterpret_cast<const moin_kv_tables*>((intptr_t)integer(a[1]));
     const at::Tensor& q = tensor(a[2]);

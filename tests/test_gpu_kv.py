@@ -356,6 +356,29 @@ def test_attention_rows_out_of_range_and_impossible_lengths():
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("impl", [1, 2])
+def test_attention_bounds_that_do_not_hold(impl):
+    """More queries or tokens than the call was told: zeros for the first max_q queries, nothing written behind them, others as they are."""
+    rng = np.random.default_rng(33)
+    lens = [100, 90, 40, 64]
+    cache, tables, table, _ = _serve(rng, lens, 2, 64, 16)
+    q = _dev(_rows(rng, 12, 20, 64))
+    cu = i32([0, 2, 9, 10, 12])
+    moin.set_option(moin.OPT_GEMM_IMPL, impl)
+    try:
+        good = moin.kv_attention(cache, tables, q, cu, i32(lens), 7, 100)
+        for max_q, max_kv, zero in ((3, 100, [1]), (7, 70, [0, 1]), (1, 64, [0, 1, 3])):
+            out = torch.full_like(q, 9.0)
+            moin.kv_attention(cache, tables, q, cu, i32(lens), max_q, max_kv, out=out)
+            for i, (a, b) in enumerate(((0, 2), (2, 9), (9, 10), (10, 12))):
+                if i in zero:
+                    assert (out[a:min(b, a + max_q)] == 0).all() and (out[a + max_q:b] == 9).all()
+                else:
+                    assert (out[a:b].double() - good[a:b].double()).abs().max() <= 2.0 ** -6 * good[a:b].double().abs().max()
+    finally:
+        moin.set_option(moin.OPT_GEMM_IMPL, 0)
+
+
 def test_attention_hides_pages_that_are_not_there():
     rng = np.random.default_rng(3)
     lens = [70, 70, 40]
@@ -615,6 +638,7 @@ def test_calls_with_other_tensors_are_refused():
            lambda: moin.kv_attention(cache, tables, q, cu, want, out=q[:3]), lambda: moin.kv_attention(cache, tables, q, cu, want, out=q.float()),
            lambda: moin.kv_attention(cache, tables, q, cu, want, rope=rope[:31].contiguous()),
            lambda: moin.kv_attention(cache, moin.KvTables.empty(2, 2, 3, 32, DEV), q, cu, want)]
+    bad += [lambda: moin.KvCache.empty(2, 48, 1, 64, DEV), lambda: moin.KvCache.empty(2, 16, 1, 96, DEV)]
     for i, call in enumerate(bad):
         with pytest.raises(moin.MoinError):
             call()
