@@ -5,8 +5,9 @@
 // so the codes enter the tensor cores as they are and every scale is applied to a score, not to 64 elements.  Both products
 // are warp MMAs (m16n8k16, fp16 operands, fp32 sums) with the codes as A, 16 tokens x 16 channels or their transpose, and
 // 8 query rows as the columns of B: the g query heads of a kv head fill them.  A code is put into the low mantissa bits of an
-// fp16 by one AND: c 2^-24, a subnormal that tensor cores multiply exactly (the upper nibble of a byte gives 16 c 2^-24;
-// its query channels are divided by 16, its value channels at the end).  Queries are bf16 times a power of two per row that
+// fp16 by one AND: c 2^-24, a subnormal that tensor cores multiply exactly.  The upper nibble of a byte gives 16 c 2^-24: its query
+// channels are divided by 16.  The values' upper nibbles stay beside the lower ones, c + 16 c', and the sums over c, which the same lane
+// holds, are taken off at the end.  Queries are bf16 times a power of two per row that
 // brings them into the middle of fp16: exact.  The weights p sv are the only operand that is rounded, to fp16 (2^-12
 // relative); their sums p are not.  To keep them inside fp16 whatever the scales are, m follows the maximum of s_t +
 // log2(sv_t): a weight is at most 2^15, and precise to 2^-24 of the row's largest.  m lags (a row is rescaled when a
@@ -373,9 +374,10 @@ __device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, in
       for (int n = 0; n < NT; ++n) d[n][0] = d[n][1] = d[n][2] = d[n][3] = 0.f;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const uint32_t w = j == 0 ? v4[u].x : j == 1 ? v4[u].y : j == 2 ? v4[u].z : v4[u].w, w8 = w >> 8;
+        const uint32_t w = j == 0 ? v4[u].x : j == 1 ? v4[u].y : j == 2 ? v4[u].z : v4[u].w;
+        const uint32_t even = w & 0x00FF00FFu, odd = __byte_perm(w, 0u, 0x4341);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) mma_f16_16816(d[n], w & kLo, w & kHi, w8 & kLo, w8 & kHi, b[u][n][pl][0], b[u][n][pl][1]);
+        for (int n = 0; n < NT; ++n) mma_f16_16816(d[n], w & kLo, even, odd & kLo, odd, b[u][n][pl][0], b[u][n][pl][1]);
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -641,7 +643,7 @@ kv_attention_kernel(const KvAttParams p) {
             unpair_f32(st.o[n][pl][j][0], x[0], x[1]);
             unpair_f32(st.o[n][pl][j][1], y[0], y[1]);
             row[64 * pl + 16 * j + g] = fmaf(x[c], 0x1p24f, z[pl][c]);
-            row[64 * pl + 16 * j + 8 + g] = fmaf(y[c], 0x1p20f, z[pl][c]);
+            row[64 * pl + 16 * j + 8 + g] = fmaf(y[c] - x[c], 0x1p20f, z[pl][c]);
           }
       }
     }
