@@ -119,11 +119,12 @@ __device__ __forceinline__ void kv_rotate_words(uint32_t& a, uint32_t& b, const 
 // A warp stores the keys or the values of a group, of one head and NP planes of it: its lanes load two token rows (g and g + 8 of
 // the tile, 16 channels a plane each), quantise them and hold the tile's words.  Whole tiles are written by 16-byte stores, others
 // byte by byte, a token's own bytes only.
-// Bound by the instructions of rotation and quantisation (about 480 a warp and tile) for prompts, by the chain slot, position,
-// (cos, sin), row, store for single tokens: 21 thousand tokens of 8 heads of 128 take 71 us with a warp per plane (a key's
-// partner plane is loaded and rotated twice then) and TODO with both planes in a warp; one token is 0.9 us faster the other way.
+// Bound by the instructions of rotation and quantisation (about 550 a warp, tile and plane) and the chain slot, position, (cos, sin),
+// store for prompts, by the chain alone for single tokens.  A wide head's planes in one warp (NP = 2): a key's partner plane is not
+// loaded and rotated twice; 21 thousand tokens of 8 heads of 128 take 52 us, with a warp per plane 71 (112 MB: 2.2 TB/s); for few
+// tokens a warp per plane is 0.9 us faster.  Seven CTAs an SM: 2 us less than the six that 80 registers leave.
 template <int D, int NP>
-__global__ void __launch_bounds__(32 * kKvStoreWarps)
+__global__ void __launch_bounds__(32 * kKvStoreWarps, 7)
 kv_append_kernel(const KvStoreParams p) {
   constexpr int kPer = D / 64 / NP;   // warps of a head's keys
   pdl_begin();
@@ -269,14 +270,21 @@ kv_read_kernel(const KvStoreParams p) {
   }
 }
 
-// Rows a CTA looks for groups in: one while warps are few, so that every token has its own; sixteen beyond, where groups are whole
-// tiles and most of the warps of single rows would find nothing.
-static bool kv_many(int T) { return T > 2048; }
+// Rows in which a CTA looks for groups.  One while warps are few, so that every token has its own; more beyond, where the groups of
+// prompts are whole tiles and most warps of single rows would find nothing.  Stored and read back in us, windows of 1, 4, 8, 32 rows:
+//   4 heads of 64    1024 single tokens  13 23 35 72     1024 of a prompt   7.8 7.5 7.2 10     4096 single  40 39 50 124    4096 of prompts  20 11 11 15
+//                    16384 of prompts    71 23 19 20
+//   8 heads of 128   256 single          15 26 46 108    1024 single        44 45 55 162       1024 of a prompt  23 13 13 22
+//                    8192 of prompts     107 40 32 29    16384              209 75 59 52
+static int kv_window(const KvStoreParams& p) {
+  const long long warps = (long long)p.T * 2 * p.kv.H * p.kv.planes;
+  return warps <= 12000 ? 1 : warps <= 66000 ? 4 : warps <= 200000 ? 8 : 32;
+}
 
 template <class Fn>
 static moin_status kv_store_launch(Fn* fn, KvStoreParams& p, int per_head, cudaStream_t s) {
-  p.window = kv_many(p.T) ? 16 : 1;
-  const dim3 grid((unsigned)((p.T + p.window - 1) / p.window), (unsigned)((2 * p.kv.H * per_head + kKvStoreWarps - 1) / kKvStoreWarps));
+  p.window = kv_window(p);
+  const dim3 grid((unsigned)((p.T + (long long)p.window - 1) / p.window), (unsigned)((2 * p.kv.H * per_head + kKvStoreWarps - 1) / kKvStoreWarps));
   ProfScope prof(MOIN_K_KV_STORE, 1, s);
   return record_cuda(launch_pdl(fn, grid, 32 * kKvStoreWarps, 0, s, p));
 }
@@ -307,7 +315,7 @@ extern "C" moin_status moin_kv_append(const moin_kv* kv, const int32_t* slot, co
   p.k_stride = k_stride; p.v_stride = v_stride;
   p.pos = pos; p.rope = (const float2*)rope; p.rope_len = rope_len; p.T = T;
   if (kv->head_dim == 64) return kv_store_launch(kv_append_kernel<64, 1>, p, 1, (cudaStream_t)stream);
-  if (kv_many(T)) return kv_store_launch(kv_append_kernel<128, 2>, p, 1, (cudaStream_t)stream);
+  if (kv_window(p) > 1) return kv_store_launch(kv_append_kernel<128, 2>, p, 1, (cudaStream_t)stream);
   return kv_store_launch(kv_append_kernel<128, 1>, p, 2, (cudaStream_t)stream);
 }
 

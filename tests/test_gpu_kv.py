@@ -198,6 +198,38 @@ def test_append_many(T, D):
     assert np.array_equal(rk.float().cpu().numpy(), ref.bf16(ref.values(k.reshape(T, H, -1, 64)).astype(np.float32)).reshape(T, H, D))
 
 
+@pytest.mark.parametrize("T,H,D,single", [(1500, 4, 64, True), (4100, 4, 64, True), (16500, 5, 64, False), (14100, 8, 128, False), (9000, 3, 128, True)])
+def test_append_windows(T, H, D, single):
+    """Every number of rows that a CTA looks for groups in: single tokens in pages of their own, prompts that begin inside a tile."""
+    rng = np.random.default_rng(T)
+    page, n = 16, (T if single else T // 16 + 200)
+    if single:
+        slot = rng.permutation(n) * page + rng.integers(0, page, n)
+    else:
+        lens = [int(x) for x in rng.integers(1, 900, 60)]
+        order, slot = list(rng.permutation(n)), []
+        for m in lens:
+            first = int(rng.integers(0, page))
+            run = np.concatenate([np.arange(p * page, (p + 1) * page) for p in [order.pop() for _ in range(-(-(m + first) // page))]])[first:first + m]
+            slot.append(run)
+            if sum(map(len, slot)) >= T:
+                break
+        slot = np.concatenate(slot)[:T]
+        slot = np.concatenate([slot, np.full(T - len(slot), -1)])
+    k, v = _rows(rng, T, H, D), _rows(rng, T, H, D)
+    cache = moin.KvCache(torch.zeros(n, H, 1, D // 64, 1152, dtype=torch.uint8, device=DEV))
+    moin.kv_append(cache, i32(slot), _dev(k), _dev(v))
+    pages, at = cache.pages.cpu().numpy(), np.nonzero(slot >= 0)[0]
+    for kv, x in ((0, k), (1, v)):
+        c, s, z = ref.load(pages, slot[at], kv)
+        qc, qs, qz = ref.quantise(x[at].reshape(len(at), H, D // 64, 64))
+        assert np.array_equal(c, qc) and np.array_equal(s, qs) and np.array_equal(z, qz)
+    for got, x in zip(moin.kv_read(cache, i32(slot)), (k, v)):
+        want = ref.bf16(ref.values(x.reshape(T, H, D // 64, 64)).astype(np.float32)).reshape(T, H, D)
+        want[slot < 0] = 0
+        assert np.array_equal(got.float().cpu().numpy(), want)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_append_rotates_at_the_position(D):
     rng = np.random.default_rng(D)
