@@ -154,37 +154,26 @@ kv_dense_kernel(const ChunkParams p) {
   const uint32_t kw[4] = {k4.x, k4.y, k4.z, k4.w};
   const uint32_t vw[4] = {movmatrix_trans(v4.x), movmatrix_trans(v4.y), movmatrix_trans(v4.z), movmatrix_trans(v4.w)};
   const uint32_t pk[2] = {pr.x, pr.y}, pv[2] = {pr.z, pr.w};
-  float x[2][2][16];                                    // [key, value][token g, g + 8][2 j + half .. as words]
+  // A row's largest value is at one of its ends: its pair tells, and whether it is NaN.
   float tok[2][2], top[2] = {0.f, 0.f}, low[2] = {INFINITY, INFINITY};   // largest values: of the tokens, of the tile, of its least token
   uint32_t bad = 0;
+  bool drop[2];                                                          // token g, g + 8: laid out as zeros
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     const bool out = gone >> (g + 8 * s) & 1u;
-    bool nan = false;
+    float end[2][2];
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const uint32_t pair = c == 0 ? pk[s] : pv[s];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {   // word i / 4, nibble (i / 2) & 1, half i & 1
-        const uint32_t w = c == 0 ? kw[i >> 2] : vw[i >> 2];
-        const float v = fmaf((float)(w >> (8 * s + 4 * ((i >> 1) & 1) + 16 * (i & 1)) & 15u), kv_scale(pair), kv_zero(pair));
-        x[c][s][i] = v;
-        nan = nan || !(fabsf(v) < INFINITY);
-      }
+      end[c][0] = fabsf(kv_zero(pair));
+      end[c][1] = fabsf(fmaf(15.f, kv_scale(pair), kv_zero(pair)));
     }
-    // (the four lanes of a token agree)
-    nan = __ballot_sync(0xffffffffu, nan) >> (4 * g) & 0xFu;
+    const bool nan = !(end[0][0] < INFINITY && end[0][1] < INFINITY && end[1][0] < INFINITY && end[1][1] < INFINITY);
     if (nan && !out) bad |= 1u << (g + 8 * s);
+    drop[s] = nan || out;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      tok[c][s] = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if (nan || out) x[c][s][i] = 0.f;
-        tok[c][s] = fmaxf(tok[c][s], fabsf(x[c][s][i]));
-      }
-      tok[c][s] = fmaxf(tok[c][s], __shfl_xor_sync(0xffffffffu, tok[c][s], 1));
-      tok[c][s] = fmaxf(tok[c][s], __shfl_xor_sync(0xffffffffu, tok[c][s], 2));
+      tok[c][s] = drop[s] ? 0.f : fmaxf(end[c][0], end[c][1]);
       top[c] = fmaxf(top[c], tok[c][s]);
       if (tok[c][s] > 0.f) low[c] = fminf(low[c], tok[c][s]);
     }
@@ -242,12 +231,19 @@ kv_dense_kernel(const ChunkParams p) {
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int s = 0; s < 2; ++s) {
+      // scale and zero times a power of two keep their 8 bits in fp16 (a step is above 2^-12 of its row's zero, a row above 2^-12 of
+      // its tile); a code becomes an fp16 by its bits (1024 + code, less 1024), a value by one fused multiply-add
+      const uint32_t pair = c == 0 ? pk[s] : pv[s];
+      const float by = drop[s] ? 0.f : f[c][s];
+      const __half2 scale2 = __float2half2_rn(drop[s] ? 0.f : kv_scale(pair) * by), zero2 = __float2half2_rn(drop[s] ? 0.f : kv_zero(pair) * by);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const __half2 h = __floats2half2_rn(x[c][s][2 * i] * f[c][s], x[c][s][2 * i + 1] * f[c][s]);
-        stage[(g + 8 * s) * kDensePitch + 4 * i + t] = *reinterpret_cast<const uint32_t*>(&h);
+        const uint32_t w = c == 0 ? kw[i >> 1] : vw[i >> 1], bits = (w >> (8 * s + 4 * (i & 1)) & 0x000F000Fu) | 0x64006400u;
+        const __half2 code = __hsub2(*reinterpret_cast<const __half2*>(&bits), __float2half2_rn(1024.f)), v = __hfma2(code, scale2, zero2);
+        stage[(g + 8 * s) * kDensePitch + 4 * i + t] = *reinterpret_cast<const uint32_t*>(&v);
       }
+    }
     __syncwarp();
     __half* dst = (c == 0 ? p.kd : p.vd) + (((size_t)req * p.tiles * kChKeys + first) * p.kv.H + head) * 64;
 #pragma unroll
