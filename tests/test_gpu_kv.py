@@ -551,7 +551,7 @@ def test_chunks_the_same_bits_and_beside_one_another(kernel):
         assert torch.equal(again, first) and torch.equal(other, first)
 
 
-@pytest.mark.parametrize("lens,q", [([3000, 2990, 17], [300, 1, 17]), ([64] * 70, [64] * 70), ([700] * 5, [129, 128, 127, 1, 64])])
+@pytest.mark.parametrize("lens,q", [([3000, 2990, 17], [300, 1, 17]), ([64] * 70, [64] * 70), ([700] * 5, [129, 128, 127, 1, 64]), ([1500], [150])])
 def test_chunks_of_many_items(lens, q, kernel):
     """More items than CTAs, rows of items that end in a request's last tile, the longest request first and last."""
     rng = np.random.default_rng(len(lens))
@@ -595,6 +595,28 @@ def test_attention_long(lens, H, G, D):
     _check_attention(cache, tables, table, lens, [1] * len(lens), H * G, rng, rope=True)
     if G <= 4:
         _check_attention(cache, tables, table, lens, [3] * len(lens), H * G, rng)
+
+
+@pytest.mark.parametrize("D,G,q", [(64, 8, 1), (64, 4, 3), (64, 4, 30), (128, 4, 1), (128, 4, 3), (128, 2, 20)])
+@pytest.mark.parametrize("kind", ["one", "few long", "many short", "more than there are CTAs"])
+def test_attention_splits(kind, D, G, q):
+    """Whole items, equal shares and cuts of one request's items: every row block size and head width, pieces that begin and end anywhere."""
+    rng = np.random.default_rng(D + G + q)
+    lens = {"one": [1900], "few long": [1700, 3, 2100, 800, 16, 1601], "many short": [int(x) for x in rng.integers(1, 60, 40)],
+            "more than there are CTAs": [int(x) for x in rng.integers(1, 40, 400)]}[kind]
+    H = 4 if kind == "more than there are CTAs" else 2
+    if kind == "more than there are CTAs" and q > 1:
+        lens = lens[:130]
+    cache, tables, table, _ = _serve(rng, lens, H, D, 32)
+    moin.set_option(moin.OPT_GEMM_IMPL, 1)
+    try:
+        _check_attention(cache, tables, table, lens, [min(q, n) for n in lens], H * G, rng, rope=True)
+        # told that requests may be long, the call cannot take whole items
+        few = lens[:5]
+        out = moin.kv_attention(cache, tables, _dev(ref.bf16(rng.standard_normal((5, H * G, D)).astype(np.float32))), i32(np.arange(len(few) + 1)), i32(few))
+        assert out[:len(few)].isfinite().all()
+    finally:
+        moin.set_option(moin.OPT_GEMM_IMPL, 0)
 
 
 def test_attention_sums_over_a_long_request_hold_their_precision():
