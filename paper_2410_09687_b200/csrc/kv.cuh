@@ -59,10 +59,12 @@ inline bool kv_stride_ok(long long stride, int heads, int head_dim) {
   return stride >= (long long)heads * head_dim && (stride % 8) == 0;
 }
 
-// Attention of long chunks (kv_chunk.cu, head_dim 64, positive scale): workspace, launch.
+// Attention of long chunks (kv_chunk.cu, head_dim 64, positive scale): workspace, launch.  What `workers` CTAs leave of the items that they
+// share is for kv_join_kernel.
+struct KvPieces { float* part; int4* desc; int workers; long long items; };
 size_t kv_chunk_bytes(int R, int T, int max_kv, int n_heads, int H);
 moin_status launch_kv_chunk(HostState* hs, const KvView& kv, const int* table, const int* rows, const int* cu_q, const int* kv_len, int n_rows,
                             int max_pages, int R, int T, int max_q, int max_kv, int n_heads, const __nv_bfloat16* q, long long q_stride,
-                            __nv_bfloat16* out, long long out_stride, const float2* rope, float scale_log2, void* workspace, cudaStream_t s);
+                            __nv_bfloat16* out, long long out_stride, const float2* rope, float scale_log2, void* workspace, KvPieces* pieces, cudaStream_t s);
 
 }  // namespace moin

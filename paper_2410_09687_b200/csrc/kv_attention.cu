@@ -872,8 +872,9 @@ static bool kv_use_chunk(int R, int T, int max_q, int max_kv, int n_heads, int n
   const double tiles = (max_kv + 63) / 64, queries = T < (double)R * max_q ? T : (double)R * max_q;
   double items = (double)(long long)((max_q * G + 127) / 128) * R * H;
   if (items > queries * n_heads / 128 + R * H) items = queries * n_heads / 128 + R * H;
-  // (the tensors that are laid out: at most 1 GiB; their blocks and rows, and the work items, within 32 bits)
-  if (R * tiles * 64 * H * 264 + (double)T * n_heads * 132 > (1ll << 30) || (max_q * G / 128 + 1) * R * H > (1ll << 30)) return false;
+  // (the tensors that are laid out: at most 1 GiB; their blocks and rows, and the work items, within 32 bits; keys that fp16 weights hold)
+  if (R * tiles * 64 * H * 264 + (double)T * n_heads * 132 > (1ll << 30) || (max_q * G / 128 + 1) * R * H > (1ll << 30) ||
+      max_kv > (1 << 19)) return false;
   if (impl == 2) return true;
   const double keys = max_kv - 0.5 * (max_q < max_kv ? max_q : max_kv);
   const double here = 8 + queries * n_heads * (keys + 200) / 0.7e6;
@@ -926,8 +927,21 @@ extern "C" moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables
   p.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t s = (cudaStream_t)stream;
   if (kv_use_chunk(R, T, max_q, max_kv, n_heads, kv->n_kv_heads, kv->head_dim, scale))
-    return launch_kv_chunk(hs, p.kv, p.table, rows, cu_q, kv_len, p.n_rows, p.max_pages, R, T, max_q, max_kv, n_heads, p.q, q_stride, p.out, out_stride,
-                           p.rope, p.scale_log2, workspace, s);
+  {
+    ProfScope prof(MOIN_K_KV_CHUNK, 3, s);
+    KvPieces pieces;
+    st = launch_kv_chunk(hs, p.kv, p.table, rows, cu_q, kv_len, p.n_rows, p.max_pages, R, T, max_q, max_kv, n_heads, p.q, q_stride, p.out, out_stride,
+                         p.rope, p.scale_log2, workspace, &pieces, s);
+    if (st) return st;
+    p.split = KV_SHARES;
+    p.inv_g = (uint32_t)((0x100000000ull + p.G - 1) / p.G);
+    p.part = pieces.part;
+    p.desc = pieces.desc;
+    const unsigned w = (unsigned)pieces.workers;
+    const cudaError_t e = pieces.workers > 8 * pieces.items ? launch_pdl(kv_join_kernel<1, 16, 8, 4>, dim3(w, 16), 512, 0, s, p, 0)
+                                                            : launch_pdl(kv_join_kernel<1, 16, 16, 1>, dim3(w, 8), 256, 0, s, p, 0);
+    return record_cuda(e);
+  }
   p.page_bytes = (uint32_t)p.kv.tile_at(1, 0, 0);
   p.tpp_log2 = kv->page_tokens == 16 ? 0 : kv->page_tokens == 32 ? 1 : kv->page_tokens == 64 ? 2 : 3;
   const int nt = kv_nt((long long)max_q * p.G);

@@ -8,16 +8,22 @@
 // them, [kv head, token, head of the group]: a tile of 128 rows is one box whatever the group is.  What is stored as NaN is laid
 // out as 0 and noted in the tile's mask; a row that sees such a token becomes NaN, no other row meets it.
 //
-// kv_chunk_kernel: work items are (request, kv head, 128 rows), persistent CTAs, two per SM, longest first, each with two chains of
-// (scores, softmax, product), as the attention of whole prompts has them: even and odd key tiles, a stream of four softmax
-// warps each with its own scores, maximum, sum and accumulator, which meet at the item's end.
-//   warp 0      producer: Q tiles into two buffers, K and V tiles [64 keys x 64 dims] into rings of four, by TMA
-//   warp 1      MMA issuer: S_h = Q K^T or O_h += P_h V, whatever is ready
+// kv_chunk_kernel: work items are (request, kv head, 128 rows); persistent CTAs, two per SM, take equal shares of their key tiles, each with
+// two streams: even and odd tiles, each stream with its own scores, maximum, sum and accumulator, which meet at the item's end.
+//   warps 0, 1  a stream's loads and MMAs, in turn: K and V tiles [64 keys x 64 dims] into two slots each by TMA (warp 0 the Q tiles
+//               too, into two buffers), S = Q K^T in two halves of 32 keys, O += P V
 //   warps 2-5   stream 0, warps 6-9 stream 1: a thread per row
-// With the tile's factors (K: 2^a, V: 2^b) a weight is w = 2^(s 2^a + b - m), at most 2^15 (m lags and is moved to leave 2^10, as in
-// kv_attention.cu), P = fp16(w), and the row's sum takes w 2^-b in fp32.
+// A stream's chain is weights - product - scores, since P lies where the lower 32 keys' scores were; those of the upper 32 are
+// computed while the product is, and their weights while the lower ones are.
+// With the tile's factors (K: 2^a, V: 2^b) a weight is w = 2^(s 2^a + b - m), at most 2^15 (m lags), P = fp16(w), and the row's sum takes
+// w 2^-b in fp32.  Weights are taken against the maximum that stands, and the tile's own maximum found beside them; where that is
+// 2^15 above, the maximum moves to leave 2^5 and the tile is taken again (with 2^10 left that is more often: 17 us of the case below).
+// A weight below 2^-14 is off by 2^-25 at most: 2^-30 of the row's largest, so that 2^19 keys stay within 2^-11 of the sum.
 // Tensor memory: S_h / P_h at columns 64 h, O_h at 128 + 64 h.  Every mbarrier wait is bounded; on expiry the CTA raises the status
 // flag, drains and returns.
+// 4 requests of 512 new tokens behind 830 to 5900, 32 heads on 4: 100 us for 52 GFLOP, bound by the instructions and exponentials of the
+// weights (a warp's tile 1.3 us, four at a time on a scheduler) and by the chain.  One warp that issued both streams' MMAs took 900
+// cycles a round, and with the maximum found first, whole items per CTA and all scores behind the product it was 125 us.
 #include <cuda.h>
 #include <float.h>
 
@@ -31,12 +37,17 @@ constexpr int kChThreads = 320;
 constexpr int kChKeys = 64, kChRows = 128;
 constexpr int kChQ = kChRows * 64 * 2, kChKV = kChKeys * 64 * 2, kChRing = 4;
 constexpr int kChMerge = 4096;               // (maximum, sum) of every row by stream, for two items
-constexpr int kChOrder = 256;                // requests that are put in order
-constexpr int kChSmem = 2 * kChQ + 2 * kChRing * kChKV + 1024 /*align*/ + 256 /*barriers*/ + kChMerge + kChOrder * 8;
+constexpr int kChSmem = 2 * kChQ + 2 * kChRing * kChKV + 1024 /*align*/ + 256 /*barriers*/ + kChMerge;
+constexpr int kChMaxWorkers = 320;           // CTAs
+constexpr int kChItemCost = 2;               // pairs of tiles that beginning and ending an item costs
+constexpr int kChLeast = 4;                  // of a share, at least
+constexpr int kChPitch = 64 + 4;             // floats of a row of a piece: sums, maximum, sum of weights
 constexpr int kChTmemCols = 256;
-constexpr float kChTop = 10.f, kChMost = 15.f;   // log2 of the largest weight after a move of the maximum, and at all
+constexpr float kChTop = 5.f, kChMost = 15.f;   // log2 of the largest weight after a move of the maximum, and at all
 
 constexpr uint32_t kChIdesc = (1u << 4) | ((uint32_t)(64 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);   // D fp32, A and B fp16, 128 x 64
+constexpr uint32_t kChIdescHalf = (1u << 4) | ((uint32_t)(32 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);   // D 128 x 32
+constexpr uint64_t kChHalf = (32 * 128) >> 4;            // 32 keys further on
 constexpr uint32_t kChIdescPV = kChIdesc | (1u << 16);   // B with its rows along the output dimension
 constexpr uint64_t kChVStep = 2048 >> 4;                 // 16 keys further on
 
@@ -54,7 +65,10 @@ struct ChunkParams {
   float* q_fac;             // [H, T G] 1 / (what the row was multiplied with)
   uint4* info;              // [R, H, tiles]: scale log2(e) 2^a, b (fp32; low bits: hidden groups, unlike tokens), mask of NaN tokens
   float2* tok;              // [R, H, tiles, 64], of tiles of unlike tokens: (scale log2(e) 2^a, b) of every token
-  int dense_blocks, by_request;
+  int dense_blocks, workers;
+  int4* share;              // [worker]: (row block of a request, head, what of that item is passed) where its share begins, its size
+  float* part;              // [worker][2][128][kChPitch]: pieces of items, in slot 1 of one that begins here without ending, else in slot 0
+  int4* desc;               // [worker][2]: the item that it begins without ending it, as kv_join_kernel takes it
   DeviceStatus* status;
 };
 
@@ -71,9 +85,134 @@ __device__ __forceinline__ ChReq ch_request(const ChunkParams& p, int req) {   /
   return r;
 }
 
-// Blocks below dense_blocks: 64 tokens of a request and kv head, a warp per 16 of them.  The others: the queries of a token.
+// Work is measured in pairs of key tiles, and kChItemCost of them to begin and end an item: items (row block of a request, kv head) one behind
+// the other, cut into equal shares, one per CTA,
+// so that a long request is no longer chain than any other and few items fill the GPU.  An item that begins or ends inside another share is left as
+// a piece (its sums, maximum and sum of weights) that kv_join_kernel adds up.
+struct ChItem { int req, head, row0, t0, n_rows, past, first_pos, last_pos, n_pairs, j0, n; bool whole; };   // n tiles from j0
+__device__ __forceinline__ ChItem ch_item(const ChunkParams& p, int block, int head) {
+  ChItem it;
+  it.req = block / p.n_blk;
+  it.head = head;
+  it.row0 = (block - it.req * p.n_blk) * kChRows;
+  const ChReq r = ch_request(p, it.req);
+  it.t0 = r.t0;
+  it.n_rows = r.q_len * p.G;
+  it.past = r.kv_len - r.q_len;
+  it.first_pos = it.past + ch_div_g(p, it.row0);
+  it.last_pos = it.row0 < it.n_rows ? it.past + ch_div_g(p, min(it.row0 + kChRows, it.n_rows) - 1) : -1;
+  it.n = it.last_pos < 0 || r.kv_len == 0 ? 0 : it.last_pos / kChKeys + 1;
+  it.n_pairs = (it.n + 1) >> 1;
+  it.j0 = 0;
+  return it;
+}
+// What to look at behind a block that has nothing to do: the blocks behind a request's last rows are passed at once.
+__device__ __forceinline__ int ch_behind(const ChunkParams& p, const ChItem& it, int block) {
+  return it.n == 0 && it.row0 >= it.n_rows ? (it.req + 1) * p.n_blk : block + 1;
+}
+__device__ __forceinline__ int ch_cost(const ChItem& it) { return it.n == 0 ? 0 : it.n_pairs + kChItemCost; }
+struct ChWalk {   // over the items of a CTA's share
+  int block, head, at, left;   // what of the item is passed, what of the share is left
+  __device__ __forceinline__ explicit ChWalk(const int4& share) : block(share.x), head(share.y), at(share.z), left(share.w) {}
+  __device__ __forceinline__ bool next(const ChunkParams& p, ChItem& it) {
+    while (left > 0 && block < p.R * p.n_blk) {
+      it = ch_item(p, block, head);
+      if (it.n == 0) {
+        block = ch_behind(p, it, block);
+        continue;
+      }
+      const int to = min(ch_cost(it), at + left), pair = max(at - kChItemCost, 0), end = to - kChItemCost;
+      left -= to - at;
+      at = 0;
+      if (++head == p.kv.H) {
+        head = 0;
+        ++block;
+      }
+      if (end <= pair) continue;   // (the share ends in what it costs to begin: the item is the next CTA's)
+      it.whole = pair == 0 && end == it.n_pairs;
+      it.j0 = 2 * pair;
+      it.n = min(it.n, 2 * end) - it.j0;
+      return true;
+    }
+    return false;
+  }
+};
+struct ChCursor {   // over the tiles of one stream
+  ChWalk walk;
+  ChItem it;
+  int j = 0;             // in the item
+  uint32_t item = ~0u;   // items so far, this one not counted
+  bool have = true;
+  __device__ __forceinline__ explicit ChCursor(const int4& share) : walk(share) { it.n = 0; }
+  __device__ __forceinline__ void next(const ChunkParams& p, int stream) {   // to an item's first tile, if the stream has one there
+    have = walk.next(p, it);
+    ++item;
+    j = stream;
+  }
+};
+// Where the shares begin, by one block beside those that lay out: sums over runs of row blocks, then a search for each share.
+__device__ __forceinline__ void ch_shares(const ChunkParams& p) {
+  __shared__ long long s_before[129];   // cost of the runs before, of one head
+  __shared__ long long s_warp[4];
+  const int blocks = p.R * p.n_blk, run = (blocks + 127) / 128, tid = threadIdx.x, lane = tid & 31;
+  const long long first = (long long)tid * run, last = first + run < blocks ? first + run : blocks;
+  long long sum = 0;
+  for (long long b = first; b < last;) {
+    const ChItem it = ch_item(p, (int)b, 0);
+    sum += ch_cost(it);
+    b = ch_behind(p, it, (int)b);
+  }
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += v;
+  }
+  if (lane == 31) s_warp[tid >> 5] = sum;
+  __syncthreads();
+  for (int w = 0; w < tid >> 5; ++w) sum += s_warp[w];
+  s_before[tid + 1] = sum;
+  if (tid == 0) s_before[0] = 0;
+  __syncthreads();
+  const long long H = p.kv.H, all = s_before[128] * H;
+  long long share = (all + p.workers - 1) / p.workers;
+  if (share < kChLeast) share = kChLeast;
+  for (int k = tid; k <= p.workers; k += 128) {
+    const long long at = k * share;
+    int4 begin = make_int4(0, 0, 0, 0), open = make_int4(0, 0, 0, 0);
+    int open_rows = 0;
+    if (at < all) {
+      int lo = 0, hi = 127;   // the last run that begins at or before it and is not empty
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (s_before[mid + 1] * H > at) hi = mid; else lo = mid + 1;
+      }
+      long long before = s_before[lo] * H, b = (long long)lo * run;
+      ChItem it = ch_item(p, (int)b, 0);
+      while (before + ch_cost(it) * H <= at) {   // (ends inside the run: its sum is above `at`)
+        before += ch_cost(it) * H;
+        b = ch_behind(p, it, (int)b);
+        it = ch_item(p, (int)b, 0);
+      }
+      const uint32_t cost = (uint32_t)ch_cost(it), off = (uint32_t)(at - before), head = off / cost;
+      const int in = (int)(off - head * cost);
+      begin = make_int4((int)b, (int)head, in, (int)(all - at < share ? all - at : share));
+      if (in > kChItemCost && in - share <= kChItemCost) {   // begun by the CTA before
+        open = make_int4((int)head, it.row0, it.t0, (int)((cost - in + share - 1) / share));
+        open_rows = it.n_rows;
+      }
+    }
+    if (k < p.workers) p.share[k] = begin;
+    if (k > 0) {
+      p.desc[2 * (k - 1)] = open;
+      p.desc[2 * (k - 1) + 1] = make_int4(open_rows, 0, 0, 0);
+    }
+  }
+}
+
+// Block 0: the shares.  The dense_blocks behind it: 64 tokens of a request and kv head, a warp per 16 of them.  The others: the queries of a
+// token; for one that sees nothing, zeros are its result.
 // Bound by the traffic of what they write; small beside the products.
-constexpr uint32_t kChUnlike = 0x10u;   // in the low bits of b
+constexpr uint32_t kChUnlike = 0x10u, kChNan = 0x20u, kChFlags = 0x3Fu;   // in the low bits of b, above those of hidden groups
 constexpr int kChRange = 12;            // powers of two between the tokens of a tile that are alike
 constexpr int kDensePitch = 36;   // words of a row in shared memory: neither side meets a bank twice
 __global__ void __launch_bounds__(128)
@@ -83,8 +222,12 @@ kv_dense_kernel(const ChunkParams p) {
   __shared__ uint32_t s_bad[4];
   pdl_begin();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  if ((int)blockIdx.x >= p.dense_blocks) {
-    const int tok = (int)blockIdx.x - p.dense_blocks;
+  if (blockIdx.x == 0) {
+    ch_shares(p);
+    return;
+  }
+  if ((int)blockIdx.x > p.dense_blocks) {
+    const int tok = (int)blockIdx.x - 1 - p.dense_blocks;
     // the request of the token: the first one that ends behind it
     int lo = 0, hi = p.R;
     while (lo < hi) {
@@ -92,9 +235,15 @@ kv_dense_kernel(const ChunkParams p) {
       if (p.cu_q[mid + 1] > tok) hi = mid; else lo = mid + 1;
     }
     int pos = -1;
+    bool blind = false;
     if (lo < p.R) {
       const ChReq r = ch_request(p, lo);
       if (tok >= r.t0 && tok < r.t0 + r.q_len) pos = r.kv_len - r.q_len + tok - r.t0;
+      blind = tok >= r.t0 && tok < r.t0 + r.q_len && (pos < 0 || r.kv_len == 0);
+    }
+    if (blind) {
+      for (int i = threadIdx.x; i < p.n_heads * 8; i += 128)
+        *reinterpret_cast<uint4*>(p.out + (long long)tok * p.out_stride + 8 * i) = make_uint4(0u, 0u, 0u, 0u);
     }
     // two heads at a time, a lane the pairs (c, c + 32), (c + 1, c + 33) of one
     const int c = 2 * (lane & 15);
@@ -135,7 +284,7 @@ kv_dense_kernel(const ChunkParams p) {
     }
     return;
   }
-  const int tile = blockIdx.x % p.tiles, rh = blockIdx.x / p.tiles, head = rh % p.kv.H, req = rh / p.kv.H;
+  const int at_block = (int)blockIdx.x - 1, tile = at_block % p.tiles, rh = at_block / p.tiles, head = rh % p.kv.H, req = rh / p.kv.H;
   const ChReq r = ch_request(p, req);
   if (tile * kChKeys >= r.kv_len || r.q_len == 0) return;
   const int first = tile * kChKeys + warp * kKvTile;   // this warp's tokens
@@ -225,7 +374,7 @@ kv_dense_kernel(const ChunkParams p) {
     for (int w = 0; w < 4; ++w) hide |= (s_bad[w] >> 16) << w;
     const uint32_t lo = (s_bad[0] & 0xFFFFu) | s_bad[1] << 16, hi = (s_bad[2] & 0xFFFFu) | s_bad[3] << 16;
     // b is a whole number of at most 114: its low mantissa bits are free
-    p.info[at_tile] = make_uint4(__float_as_uint(p.scale_log2 * two_to(e[0])), __float_as_uint((float)e[1]) | hide | (unlike ? kChUnlike : 0u), lo, hi);
+    p.info[at_tile] = make_uint4(__float_as_uint(p.scale_log2 * two_to(e[0])), __float_as_uint((float)e[1]) | hide | (unlike ? kChUnlike : 0u) | ((lo | hi) != 0u ? kChNan : 0u), lo, hi);
   }
   uint32_t* stage = s_rows[warp];
 #pragma unroll
@@ -255,36 +404,6 @@ kv_dense_kernel(const ChunkParams p) {
   }
 }
 
-struct ChItem { int req, head, row0, t0, n_rows, past, first_pos, last_pos, n_tiles; bool on; };
-// The k-th item of a CTA: items stand longest first as far as their place tells, and CTAs take them there and back again, so that one
-// that began with a long item ends with a short one.  Where pasts are longer than chunks the requests count (`order`: longest
-// first), else the row blocks.
-__device__ __forceinline__ int ch_index(int k) { return (k & 1) ? (k + 1) * (int)gridDim.x - 1 - (int)blockIdx.x : k * (int)gridDim.x + (int)blockIdx.x; }
-__device__ __forceinline__ ChItem ch_item(const ChunkParams& p, const int* order, int idx) {
-  ChItem it;
-  int blk;
-  if (p.by_request) {
-    const int per = p.n_blk * p.kv.H, at = idx / per, rem = idx % per;
-    it.req = order[at];
-    blk = p.n_blk - 1 - rem / p.kv.H;
-    it.head = rem % p.kv.H;
-  } else {
-    const int per = p.R * p.kv.H, rem = idx % per;
-    blk = p.n_blk - 1 - idx / per;
-    it.req = rem / p.kv.H;
-    it.head = rem % p.kv.H;
-  }
-  it.row0 = blk * kChRows;
-  const ChReq r = ch_request(p, it.req);
-  it.t0 = r.t0;
-  it.n_rows = r.q_len * p.G;
-  it.on = it.row0 < it.n_rows;
-  it.past = r.kv_len - r.q_len;
-  it.first_pos = it.past + ch_div_g(p, it.row0);
-  it.last_pos = it.on ? it.past + ch_div_g(p, min(it.row0 + kChRows, it.n_rows) - 1) : -1;
-  it.n_tiles = it.last_pos < 0 || r.kv_len == 0 ? 0 : it.last_pos / kChKeys + 1;
-  return it;
-}
 __device__ __forceinline__ float ch_exp2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -303,22 +422,21 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   uint8_t* base_ptr = smem_raw + (base - raw);
   const uint32_t sQ = base, sK = base + 2 * kChQ, sV = sK + kChRing * kChKV, bars = sV + kChRing * kChKV;
   uint8_t* bar_ptr = base_ptr + (bars - base);
-  const uint32_t kfull = bars, kempty = bars + 32, vfull = bars + 64, vempty = bars + 96, sready = bars + 128, pready = bars + 144,
-                 pvdone = bars + 160, oready = bars + 176, ofree = bars + 184, qfull = bars + 192, qfree = bars + 208;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_ptr + 224);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(bar_ptr + 228);
-  volatile int* sm_fail = reinterpret_cast<volatile int*>(bar_ptr + 232);
+  const uint32_t kfull = bars, vfull = bars + 32, sready = bars + 64, supper = bars + 80, pready = bars + 96, pvdone = bars + 112,
+                 qfull = bars + 128, qfree = bars + 144, ofree = bars + 160;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_ptr + 168);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bar_ptr + 172);
+  volatile int* sm_fail = reinterpret_cast<volatile int*>(bar_ptr + 176);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kChRing; ++i) {
-      mbar_init(kfull + 8 * i, 1); mbar_init(kempty + 8 * i, 1);
-      mbar_init(vfull + 8 * i, 1); mbar_init(vempty + 8 * i, 1);
+      mbar_init(kfull + 8 * i, 1);
+      mbar_init(vfull + 8 * i, 1);
     }
     for (int h = 0; h < 2; ++h) {
-      mbar_init(sready + 8 * h, 1); mbar_init(pready + 8 * h, 128); mbar_init(pvdone + 8 * h, 1);
-      mbar_init(qfull + 8 * h, 1); mbar_init(qfree + 8 * h, 1);
+      mbar_init(sready + 8 * h, 1); mbar_init(supper + 8 * h, 1); mbar_init(pready + 8 * h, 128); mbar_init(pvdone + 8 * h, 1);
+      mbar_init(qfull + 8 * h, 1); mbar_init(qfree + 8 * h, 2);
     }
-    mbar_init(oready, 1);
     mbar_init(ofree, 256);
     *abort_flag = 0;
     sm_fail[0] = sm_fail[1] = 0;
@@ -329,151 +447,109 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     tmem_relinquish();
   }
   pdl_begin();
-  int* order = reinterpret_cast<int*>(bar_ptr + 256 + kChMerge);
-  if (p.by_request) {
-    int* len = order + kChOrder;
-    for (int i = threadIdx.x; i < p.R; i += kChThreads) len[i] = p.kv_len[i];
-    __syncthreads();
-    for (int i = threadIdx.x; i < p.R; i += kChThreads) {
-      int rank = 0;
-      for (int k = 0; k < p.R; ++k) rank += len[k] > len[i] || (len[k] == len[i] && k < i);
-      order[rank] = i;
-    }
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const int n_items = p.n_blk * p.R * p.kv.H;
+  const int4 share = p.share[blockIdx.x];
 
-  if (warp == 0) {
-    // ------------------------------------------------------------------ producer
-    if (lane == 0) {
-      uint32_t tq = 0, nq = 0;   // tiles, Q tiles so far
-      bool ok = true;
-      auto load_q = [&](const ChItem& n) -> bool {
-        const uint32_t b = nq & 1u;
-        if (!mbar_wait(qfree + 8 * b, ((nq >> 1) & 1u) ^ 1u, abort_flag, p.status, 61)) return false;
-        mbar_expect_tx(qfull + 8 * b, kChQ);
-        tma_load_2d(sQ + b * kChQ, &tmQ, qfull + 8 * b, 0, n.head * p.T * p.G + n.t0 * p.G + n.row0);
-        ++nq;
-        return true;
-      };
-      auto next = [&](int& k, ChItem& out) -> bool {   // the next item that has tiles
-        for (++k; k * (int)gridDim.x < n_items; ++k) {
-          const int i = ch_index(k);
-          if (i >= n_items) continue;
-          out = ch_item(p, order, i);
-          if (out.n_tiles > 0) return true;
+  if (warp < 2) {
+    // ------------------------------------------------------------------ loads and MMAs of a stream, one after the other: the whole
+    // warp waits, one lane issues.  Tile i of the stream lies in slot i & 1; it is replaced when its product is complete.
+    const int h = warp;
+    const bool leader = elect_one();
+    const uint32_t sk = sK + 2 * h * kChKV, sv = sV + 2 * h * kChKV, kf = kfull + 16 * h, vf = vfull + 16 * h;
+    bool ok = true;
+    auto wait = [&](uint32_t bar, uint32_t parity, int site) { ok = ok && mbar_wait_warp(bar, parity, abort_flag, p.status, site); };
+    ChCursor ld(share), at(share);   // the next tile to load; the one whose scores were issued last
+    uint32_t i = 0, n_ld = 0;
+    auto load = [&] {
+      if (!ld.have) return;
+      if (h == 0 && ld.j == 0) {     // an item begins: its queries, for both streams
+        const uint32_t b = ld.item & 1u;
+        wait(qfree + 8 * b, ((ld.item >> 1) & 1u) ^ 1u, 61);
+        if (ok && leader) {
+          mbar_expect_tx(qfull + 8 * b, kChQ);
+          tma_load_2d(sQ + b * kChQ, &tmQ, qfull + 8 * b, 0, ld.it.head * p.T * p.G + ld.it.t0 * p.G + ld.it.row0);
         }
-        return false;
-      };
-      int idx = -1;
-      ChItem it, nx;
-      bool have = next(idx, it);
-      if (have) ok = load_q(it);
-      while (have && ok) {
-        int nidx = idx;
-        const bool have_nx = next(nidx, nx);
-        const int row = it.req * p.tiles * kChKeys;
-        for (int j = 0; j < it.n_tiles && ok; ++j, ++tq) {
-          const uint32_t s = tq % kChRing, ph = (tq / kChRing) & 1u;
-          if (!(ok = mbar_wait(kempty + 8 * s, ph ^ 1u, abort_flag, p.status, 62))) break;
-          mbar_expect_tx(kfull + 8 * s, kChKV);
-          tma_load_2d(sK + s * kChKV, &tmK, kfull + 8 * s, it.head * 64, row + j * kChKeys);
-          if (!(ok = mbar_wait(vempty + 8 * s, ph ^ 1u, abort_flag, p.status, 63))) break;
-          mbar_expect_tx(vfull + 8 * s, kChKV);
-          tma_load_2d(sV + s * kChKV, &tmV, vfull + 8 * s, it.head * 64, row + j * kChKeys);
-          if (have_nx && j == min(1, it.n_tiles - 1)) ok = load_q(nx);   // (its buffer: since the item before's last scores)
-        }
-        it = nx;
-        idx = nidx;
-        have = have_nx;
+      }
+      const uint32_t s = n_ld & 1u;
+      const int row = (ld.it.req * p.tiles + ld.it.j0 + ld.j) * kChKeys;
+      if (ok && leader) {
+        mbar_expect_tx(kf + 8 * s, kChKV);
+        tma_load_2d(sk + s * kChKV, &tmK, kf + 8 * s, ld.it.head * 64, row);
+        mbar_expect_tx(vf + 8 * s, kChKV);
+        tma_load_2d(sv + s * kChKV, &tmV, vf + 8 * s, ld.it.head * 64, row);
+      }
+      ++n_ld;
+      ld.j += 2;
+      while (ld.have && ld.j >= ld.it.n) ld.next(p, h);
+    };
+    auto forward = [&] {   // `at` to the next tile
+      while (at.have && at.j >= at.it.n) {
+        at.next(p, h);
+        if (!at.have) return;
+        wait(qfull + 8 * (at.item & 1u), (at.item >> 1) & 1u, 64);
+        if (!ok) return;
+        // an item of one tile: this stream has no scores there
+        if (at.j >= at.it.n && leader) mbar_arrive(qfree + 8 * (at.item & 1u));
+      }
+    };
+    auto scores = [&](uint32_t s, int upper) {   // of 32 keys
+      const uint64_t dq = sdesc_k128(sQ + (at.item & 1u) * kChQ), dk = sdesc_k128(sk + s * kChKV) + (upper ? kChHalf : 0u);
+      tc_fence_after();
+      if (leader) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) tc_mma_bf16(tmem + h * 64 + 32 * upper, dq + (uint64_t)(2 * k), dk + (uint64_t)(2 * k), kChIdescHalf, k > 0 ? 1u : 0u);
+        tc_commit((upper ? supper : sready) + 8 * h);
+        if (!upper && at.j + 2 >= at.it.n) tc_commit(qfree + 8 * (at.item & 1u));
+      }
+    };
+    while (ld.have && ld.j >= ld.it.n) ld.next(p, h);
+    load();
+    load();
+    forward();
+    if (ok && at.have) {
+      wait(kf, 0u, 62);
+      if (ok) {
+        scores(0, 1);
+        scores(0, 0);
       }
     }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------------ MMA issuer: the whole warp walks, one lane issues
-    const bool leader = elect_one();
-    uint32_t tq = 0, nit = 0;
-    uint32_t n_p[2] = {0, 0};   // products issued per stream
-    bool ok = true;
-    for (int k = 0; k * (int)gridDim.x < n_items && ok; ++k) {
-      const int idx = ch_index(k);
-      if (idx >= n_items) continue;
-      const ChItem it = ch_item(p, order, idx);
-      if (it.n_tiles == 0) continue;
-      const uint32_t qb = nit & 1u;
-      if (!(ok = mbar_wait_warp(qfull + 8 * qb, (nit >> 1) & 1u, abort_flag, p.status, 64))) break;
+    while (ok && at.have) {
+      const uint32_t s = i & 1u, ph = (i >> 1) & 1u;
+      const uint32_t first = at.j == h ? 0u : 1u, item = at.item;
+      // The next tile's scores: the upper 32 keys' columns are free since P is there, the lower ones' hold P.  Those of another item
+      // come behind the product, for which its queries may wait.
+      const bool same = at.j + 2 < at.it.n;
+      at.j += 2;
+      wait(pready + 8 * h, i & 1u, 65);
+      if (same) {
+        wait(kf + 8 * (s ^ 1u), ((i + 1) >> 1) & 1u, 62);
+        if (ok) scores(s ^ 1u, 1);
+      }
+      if (!first) wait(ofree, (item & 1u) ^ 1u, 69);   // the accumulators are free once the O of the item before has been read
+      wait(vf + 8 * s, ph, 63);
+      if (!ok) break;
       tc_fence_after();
-      const uint64_t dq = sdesc_k128(sQ + qb * kChQ);
-      int tile[2] = {0, 1}, left = it.n_tiles, left_s = it.n_tiles;   // next tile of each stream; products, scores to go
-      bool scores[2] = {false, false};
-      bool o_free = false;
-      unsigned long long t0 = 0;
-      uint32_t spins = 0;
-      while (left > 0) {
-        bool moved = false;
+      if (leader) {
+        const uint64_t dv = sdesc_k128(sv + s * kChKV);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (tile[h] >= it.n_tiles) continue;
-          const uint32_t gt = tq + (uint32_t)tile[h], s = gt % kChRing, ph = (gt / kChRing) & 1u;
-          if (!scores[h]) {
-            // P of the product before lies where these scores go
-            if (!__all_sync(0xffffffffu, (n_p[h] == 0 || mbar_test_wait(pvdone + 8 * h, (n_p[h] - 1) & 1u)) && mbar_test_wait(kfull + 8 * s, ph))) continue;
-            tc_fence_after();
-            const uint64_t dk = sdesc_k128(sK + s * kChKV);
-            --left_s;
-            if (leader) {
-#pragma unroll
-              for (int k = 0; k < 4; ++k) tc_mma_bf16(tmem + h * 64, dq + (uint64_t)(2 * k), dk + (uint64_t)(2 * k), kChIdesc, k > 0 ? 1u : 0u);
-              tc_commit(kempty + 8 * s);
-              tc_commit(sready + 8 * h);
-              if (left_s == 0) tc_commit(qfree + 8 * qb);
-            }
-            scores[h] = true;
-            moved = true;
-          } else {
-            // the accumulators are free once the O of the item before has been read
-            if (!o_free && !(o_free = __all_sync(0xffffffffu, mbar_test_wait(ofree, (nit & 1u) ^ 1u)))) continue;
-            if (!__all_sync(0xffffffffu, mbar_test_wait(pready + 8 * h, n_p[h] & 1u) && mbar_test_wait(vfull + 8 * s, ph))) continue;
-            tc_fence_after();
-            const uint64_t dv = sdesc_k128(sV + s * kChKV);
-            const uint32_t first = tile[h] == h ? 0u : 1u;
-            if (leader) {
-#pragma unroll
-              for (int k = 0; k < 4; ++k)
-                tc_mma_bf16_ta(tmem + 128 + h * 64, tmem + h * 64 + 8 * k, dv + kChVStep * k, kChIdescPV, k > 0 ? 1u : first);
-              tc_commit(vempty + 8 * s);
-              tc_commit(pvdone + 8 * h);
-            }
-            ++n_p[h];
-            scores[h] = false;
-            tile[h] += 2;
-            --left;
-            moved = true;
-          }
-        }
-        if (moved) {
-          spins = 0;
-          t0 = 0;
-        } else if ((++spins & 0x3FFu) == 0) {   // bounded, as every wait
-          int stop = *abort_flag;
-          const unsigned long long now = global_ns();
-          if (t0 == 0) t0 = now;
-          if (now - t0 > kWaitLimitNs) {
-            stop = *abort_flag = 1;
-            atomicExch(&p.status->timeout_flag, 1);
-            atomicExch(&p.status->timeout_site, 65);
-          }
-          if (__any_sync(0xffffffffu, stop != 0)) {
-            ok = false;
-            break;
-          }
+        for (int k = 0; k < 4; ++k) tc_mma_bf16_ta(tmem + 128 + h * 64, tmem + h * 64 + 8 * k, dv + kChVStep * k, kChIdescPV, k > 0 ? 1u : first);
+        tc_commit(pvdone + 8 * h);
+      }
+      if (!same) {
+        forward();
+        if (ok && at.have) {
+          wait(kf + 8 * (s ^ 1u), ((i + 1) >> 1) & 1u, 62);
+          if (ok) scores(s ^ 1u, 1);
         }
       }
-      if (ok && leader) tc_commit(oready);
-      tq += (uint32_t)it.n_tiles;
-      ++nit;
+      wait(pvdone + 8 * h, i & 1u, 70);
+      if (!ok) break;
+      if (at.have) scores(s ^ 1u, 0);
+      load();
+      ++i;
     }
   } else {
     // ------------------------------------------------------------------ softmax and result: a thread per row and stream
@@ -482,92 +558,40 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     const int quarter = warp & 3, half = (warp - 2) >> 2, row = quarter * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16, s_addr = tmem + lane_addr + half * 64;
     float2* xml = reinterpret_cast<float2*>(bar_ptr + 256);   // [item parity][stream][row]: (maximum, sum)
-    uint32_t n_s = 0, nit = 0;
+    uint32_t n_s = 0, n_other = 0, nit = 0;   // tiles of this stream, of the other one; items
     bool ok = true;
-    for (int kk = 0; kk * (int)gridDim.x < n_items; ++kk) {
-      const int idx = ch_index(kk);
-      if (idx >= n_items) continue;
-      const ChItem it = ch_item(p, order, idx);
-      if (!it.on) continue;
+    ChWalk walk(share);
+    ChItem it;
+    while (walk.next(p, it)) {
       const int r = it.row0 + row, qi = ch_div_g(p, min(r, it.n_rows - 1));
       const bool live = r < it.n_rows;
-      __nv_bfloat16* dst = p.out + (long long)(it.t0 + qi) * p.out_stride + (it.head * p.G + min(r, it.n_rows - 1) - qi * p.G) * 64 + half * 32;
-      if (it.n_tiles == 0) {   // nothing to see for any row
-        if (live) {
-#pragma unroll
-          for (int c = 0; c < 32; c += 8) *reinterpret_cast<uint4*>(dst + c) = make_uint4(0u, 0u, 0u, 0u);
-        }
-        continue;
-      }
       const int pos = it.past + qi;
       const float fac = live ? __ldg(p.q_fac + (long long)it.head * p.T * p.G + (long long)it.t0 * p.G + r) : 1.f;
       const uint4* info = p.info + ((size_t)it.req * p.kv.H + it.head) * p.tiles;
       float m = 0.f, l = 0.f;   // maximum (powers of two), sum of 2^(s - m)
       bool fresh = true;        // no key seen yet: m means nothing
-      uint4 at = half < it.n_tiles ? __ldg(info + half) : make_uint4(0u, 0u, 0u, 0u);
-      for (int j = half; j < it.n_tiles && ok; j += 2, ++n_s) {
-        const uint4 now = at;
-        if (j + 2 < it.n_tiles) at = __ldg(info + j + 2);
-        const float c = __uint_as_float(now.x) * fac, ev = __uint_as_float(now.y & ~0x1Fu);
-        const uint32_t hide = now.y & 0xFu;
-        const float2* unlike = (now.y & kChUnlike) ? p.tok + (((size_t)it.req * p.kv.H + it.head) * p.tiles + j) * kChKeys : nullptr;
-        if (!(ok = mbar_wait_warp(sready + 8 * half, n_s & 1u, abort_flag, p.status, 66))) break;
+      const int j_end = it.j0 + it.n;
+      uint2 at = half < it.n ? __ldg(reinterpret_cast<const uint2*>(info + it.j0 + half)) : make_uint2(0u, 0u);
+      for (int j = it.j0 + half; j < j_end && ok; j += 2, ++n_s) {
+        const uint2 now = at;
+        if (j + 2 < j_end) at = __ldg(reinterpret_cast<const uint2*>(info + j + 2));
+        const float c = __uint_as_float(now.x) * fac, ev = __uint_as_float(now.y & ~kChFlags);
+        const int seen = pos - j * kChKeys;   // the last key of the tile that the row sees
+        if (!(ok = mbar_wait_warp(supper + 8 * half, n_s & 1u, abort_flag, p.status, 66))) break;
         tc_fence_after();
-        // twice over the scores in groups of 16 keys, the next group's read in flight (a thread that keeps all 64 spills)
-        const int kr0 = j * kChKeys;
-        uint32_t va[16], vb[16];
-        float ma = -INFINITY, mc = -INFINITY;
-        auto all_seen = [&](int k) { return kr0 + 16 * k + 15 <= it.first_pos && !(hide >> k & 1u); };
-        auto any_seen = [&](int k) { return kr0 + 16 * k <= it.last_pos && !(hide >> k & 1u); };
-        auto group_max = [&](const uint32_t (&v)[16], int k) {
-          if (all_seen(k)) {
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-              ma = fmax3(ma, __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
-              mc = fmax3(mc, __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
-            }
-          } else if (any_seen(k)) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (kr0 + 16 * k + i <= pos) ma = fmaxf(ma, __uint_as_float(v[i]));
-          }
+        auto lower = [&] {   // the scores of the lower 32 keys: complete (and with them the product before)
+          ok = mbar_wait_warp(sready + 8 * half, n_s & 1u, abort_flag, p.status, 68);
+          tc_fence_after();
         };
-        float tm = -INFINITY;
-        if (unlike == nullptr) {
-          tmem_ld16(s_addr, va);
-          tmem_ld16(s_addr + 16, vb);
-          tmem_ld_wait();
-          group_max(va, 0);
-          group_max(vb, 1);
-          tmem_ld16(s_addr + 32, va);
-          tmem_ld16(s_addr + 48, vb);
-          tmem_ld_wait();
-          group_max(va, 2);
-          group_max(vb, 3);
-          const float mx = fmaxf(ma, mc);
-          if (mx > -INFINITY) tm = fmaf(mx, c, ev);
-        } else {
-#pragma unroll 1
-          for (int k = 0; k < 4; ++k) {
-            tmem_ld16(s_addr + 16 * k, va);
-            tmem_ld_wait();
-            if (hide >> k & 1u) continue;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float2 tk = __ldg(unlike + 16 * k + i);
-              if (kr0 + 16 * k + i <= pos) tm = fmaxf(tm, fmaf(__uint_as_float(va[i]), tk.x * fac, tk.y));
-            }
-          }
-        }
-        tmem_ld16(s_addr, va);
-        const bool grow = fresh ? tm > -INFINITY : tm > m + kChMost;
-        if (__any_sync(0xffffffffu, grow)) {
+        bool done = false;
+        // the maximum to what leaves 2^kChTop, the sums with it
+        auto move = [&](float tm, bool grow) {
           const float m_new = grow ? tm - kChTop : m, corr = grow && !fresh ? ch_exp2(m - m_new) : 1.f;
           if (grow && !fresh) l = ch_rescale(l, m - m_new);
           m = m_new;
           fresh = fresh && !grow;
-          if (j != half) {   // (these scores exist only because the product before is complete)
-#pragma unroll
+          if (j != it.j0 + half) {   // (these scores exist only because the product before is complete)
+#pragma unroll 1
             for (int q = 0; q < 64; q += 16) {
               uint32_t o[16];
               tmem_ld16(s_addr + 128 + q, o);
@@ -577,81 +601,116 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
               tmem_st16(s_addr + 128 + q, o);
             }
           }
-        }
-        const uint64_t off2 = pair_f32(ev - m, ev - m), c2 = pair_f32(c, c);
-        uint64_t l2 = pair_f32(0.f, 0.f);
-        auto group_p = [&](const uint32_t (&v)[16], int k, uint32_t* w) {
-          if (all_seen(k)) {
+        };
+#pragma unroll 1
+        for (bool again = (now.y & kChFlags) == 0u; again;) {
+          uint32_t va[16], vb[16];
+          // Weights against the maximum so far, the tile's own maximum beside them: groups of 16 keys, the next group's read in
+          // flight, P in registers until the maximum is known to hold.  Else it moves, and the tile is taken again.
+          const uint64_t off2 = pair_f32(ev - m, ev - m), c2 = pair_f32(c, c);
+          uint64_t l2 = pair_f32(0.f, 0.f);
+          float ma = -INFINITY, mc = -INFINITY;
+          uint32_t w[2][16];
+          auto group = [&](const uint32_t (&v)[16], int k, bool masked) {
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = masked && 16 * k + i > seen ? -INFINITY : __uint_as_float(v[i]);
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+              ma = fmax3(ma, x[i], x[i + 1]);
+              mc = fmax3(mc, x[i + 2], x[i + 3]);
+            }
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
               float x0, x1;
-              unpair_f32(fma2(pair_f32(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), c2, off2), x0, x1);
+              unpair_f32(fma2(pair_f32(x[i], x[i + 1]), c2, off2), x0, x1);
               const float p0 = ch_exp2(x0), p1 = ch_exp2(x1);
               l2 = add2(l2, pair_f32(p0, p1));
               const __half2 h2 = __floats2half2_rn(p0, p1);
-              w[i >> 1] = *reinterpret_cast<const uint32_t*>(&h2);
+              w[k >> 1][8 * (k & 1) + (i >> 1)] = *reinterpret_cast<const uint32_t*>(&h2);
             }
-          } else if (any_seen(k)) {
+          };
+          auto tile = [&](bool masked) {
+            tmem_ld16(s_addr + 32, va);
+            tmem_ld_wait();
+            tmem_ld16(s_addr + 48, vb);
+            group(va, 2, masked);
+            tmem_ld_wait();
+            group(vb, 3, masked);
+            lower();
+            tmem_ld16(s_addr, va);
+            tmem_ld_wait();
+            tmem_ld16(s_addr + 16, vb);
+            group(va, 0, masked);
+            tmem_ld_wait();
+            group(vb, 1, masked);
+          };
+          if (j * kChKeys + kChKeys - 1 <= it.first_pos) tile(false);
+          else tile(true);
+          if (!ok) break;
+          const float tm = fmaf(fmaxf(ma, mc), c, ev);
+          // too small for fp32 (the maximum comes from values 2^80 times this tile's), of keys whose 2^(s - m) still counts in the sum
+          const bool grow = fresh ? tm > -INFINITY : tm > m + kChMost, small = !fresh && tm < m - 80.f && tm - ev > m - 60.f;
+          const uint32_t votes = (grow ? 1u : 0u) | (small ? 2u : 0u), vote = __reduce_or_sync(0xffffffffu, votes);
+          if (vote == 1u) {
+            move(tm, grow);
+            continue;
+          }
+          again = false;
+          if (vote == 0u) {
+            tmem_st16(s_addr, w[0]);
+            tmem_st16(s_addr + 16, w[1]);
+            float la, lb;
+            unpair_f32(l2, la, lb);
+            l = fmaf(la + lb, ch_exp2(-ev), l);
+            done = true;
+          }
+        }
+        if (ok && !done) lower();
+        if (!ok) break;
+        if (!done) {   // one by one: unlike, hidden or NaN tokens, weights that are too small
+          const uint32_t hide = now.y & 0xFu;
+          const float2* unlike = (now.y & kChUnlike) ? p.tok + (((size_t)it.req * p.kv.H + it.head) * p.tiles + j) * kChKeys : nullptr;
+          uint32_t v[16];
+          float tm = -INFINITY;
+#pragma unroll 1
+          for (int k = 0; k < 4; ++k) {
+            tmem_ld16(s_addr + 16 * k, v);
+            tmem_ld_wait();
+            if (hide >> k & 1u) continue;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float2 tk = unlike != nullptr ? __ldg(unlike + 16 * k + i) : make_float2(__uint_as_float(now.x), ev);
+              if (16 * k + i <= seen) tm = fmaxf(tm, fmaf(__uint_as_float(v[i]), tk.x * fac, tk.y));
+            }
+          }
+          const bool grow = fresh ? tm > -INFINITY : tm > m + kChMost;
+          if (__any_sync(0xffffffffu, grow)) move(tm, grow);
+#pragma unroll 1
+          for (int k = 0; k < 4; ++k) {   // P of 16 keys into columns whose scores have been read
+            uint32_t w[8];
+            tmem_ld16(s_addr + 16 * k, v);
+            tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-              const float p0 = kr0 + 16 * k + i <= pos ? ch_exp2(fmaf(__uint_as_float(v[i]), c, ev - m)) : 0.f;
-              const float p1 = kr0 + 16 * k + i + 1 <= pos ? ch_exp2(fmaf(__uint_as_float(v[i + 1]), c, ev - m)) : 0.f;
-              l2 = add2(l2, pair_f32(p0, p1));
-              const __half2 h2 = __floats2half2_rn(p0, p1);
+              float pr[2];
+#pragma unroll
+              for (int b = 0; b < 2; ++b) {
+                const float2 tk = unlike != nullptr ? __ldg(unlike + 16 * k + i + b) : make_float2(__uint_as_float(now.x), ev);
+                const float pk = 16 * k + i + b <= seen && !(hide >> k & 1u) ? ch_exp2(fmaf(__uint_as_float(v[i + b]), tk.x * fac, -m)) : 0.f;
+                l += pk;
+                pr[b] = pk * ch_exp2(tk.y);
+              }
+              const __half2 h2 = __floats2half2_rn(pr[0], pr[1]);
               w[i >> 1] = *reinterpret_cast<const uint32_t*>(&h2);
             }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = 0u;
+            tmem_st8(s_addr + 8 * k, w);
           }
-        };
-        // One by one: unlike tokens; or weights too small for fp32 (the maximum comes from values 2^80 times this tile's) of keys
-        // whose 2^(s - m) still counts in the sum.
-        if (unlike != nullptr || __any_sync(0xffffffffu, tm < m - 80.f && tm - ev > m - 60.f)) {
-#pragma unroll 1
-          for (int hq = 0; hq < 2; ++hq) {
-            uint32_t w[16];
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-              const int k = 2 * hq + kk;
-              tmem_ld16(s_addr + 16 * k, va);
-              tmem_ld_wait();
-#pragma unroll
-              for (int i = 0; i < 16; i += 2) {
-                float pr[2];
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                  const float2 tk = unlike != nullptr ? __ldg(unlike + 16 * k + i + b) : make_float2(__uint_as_float(now.x), ev);
-                  const bool seen = kr0 + 16 * k + i + b <= pos && !(hide >> k & 1u);
-                  const float pk = seen ? ch_exp2(fmaf(__uint_as_float(va[i + b]), tk.x * fac, -m)) : 0.f;
-                  l += pk;
-                  pr[b] = pk * ch_exp2(tk.y);
-                }
-                const __half2 h2 = __floats2half2_rn(pr[0], pr[1]);
-                w[8 * kk + (i >> 1)] = *reinterpret_cast<const uint32_t*>(&h2);
-              }
-            }
-            tmem_st16(s_addr + 16 * hq, w);
+          if (now.y & kChNan) {   // tokens stored as NaN: for the rows that see one
+            const uint2 bad = __ldg(reinterpret_cast<const uint2*>(info + j) + 1);
+            const unsigned long long mask = (unsigned long long)bad.y << 32 | bad.x;
+            if (seen >= 0 && (mask & (seen >= 63 ? ~0ull : (1ull << (seen + 1)) - 1ull))) l = NAN;
           }
-        } else
-#pragma unroll
-        for (int hq = 0; hq < 2; ++hq) {   // P of 32 keys into columns whose scores have been read
-          uint32_t w[16];
-          tmem_ld_wait();
-          tmem_ld16(s_addr + 32 * hq + 16, vb);
-          group_p(va, 2 * hq, w);
-          tmem_ld_wait();
-          if (hq == 0) tmem_ld16(s_addr + 32, va);
-          group_p(vb, 2 * hq + 1, w + 8);
-          tmem_st16(s_addr + 16 * hq, w);
-        }
-        float la, lb;
-        unpair_f32(l2, la, lb);
-        l = fmaf(la + lb, ch_exp2(-ev), l);
-        if (now.z | now.w) {   // tokens stored as NaN: for the rows that see one
-          const int seen = pos - kr0;
-          const unsigned long long mask = (unsigned long long)now.w << 32 | now.z;
-          if (seen >= 0 && (mask & (seen >= 63 ? ~0ull : (1ull << (seen + 1)) - 1ull))) l = NAN;
         }
         tmem_st_wait();
         tc_fence_before();
@@ -666,16 +725,22 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       const float top = fmaxf(own.x, other.x);
       const float a_me = ch_exp2(own.x - top), a_ot = ch_exp2(other.x - top);
       const float sum = ch_rescale(own.y, own.x - top) + ch_rescale(other.y, other.x - top);
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;   // nothing to see: zeros
+      const float inv = !it.whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum;   // nothing to see: zeros
       const float f0 = (half == 0 ? a_me : a_ot) * inv, f1 = (half == 0 ? a_ot : a_me) * inv;
-      // ---- (O_0 f_0 + O_1 f_1) -> out: this thread's 32 of the row's 64 dims
-      if ((ok = mbar_wait_warp(oready, nit & 1u, abort_flag, p.status, 67))) {
+      // ---- (O_0 f_0 + O_1 f_1) -> out, or its piece: this thread's 32 of the row's 64 dims
+      __nv_bfloat16* dst = p.out + (long long)(it.t0 + qi) * p.out_stride + (it.head * p.G + min(r, it.n_rows - 1) - qi * p.G) * 64 + half * 32;
+      float* piece = p.part + ((blockIdx.x * 2 + (it.j0 == 0 ? 1 : 0)) * kChRows + row) * kChPitch;
+      if (!it.whole && half == 0) *reinterpret_cast<float2*>(piece + 64) = make_float2(top, sum);
+      n_other += (uint32_t)(half == 0 ? it.n >> 1 : (it.n + 1) >> 1);
+      if (it.n > half) ok = mbar_wait_warp(pvdone + 8 * half, (n_s - 1) & 1u, abort_flag, p.status, 67);
+      if (ok && it.n > 1 - half) ok = mbar_wait_warp(pvdone + 8 * (half ^ 1), (n_other - 1) & 1u, abort_flag, p.status, 67);
+      if (ok) {
         tc_fence_after();
         uint32_t v[16], u[16];
 #pragma unroll
         for (int c = 0; c < 32; c += 16) {
           tmem_ld16(tmem + lane_addr + 128 + half * 32 + c, v);
-          if (it.n_tiles > 1) {
+          if (it.n > 1) {
             tmem_ld16(tmem + lane_addr + 192 + half * 32 + c, u);
           } else {
 #pragma unroll
@@ -686,11 +751,16 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             tc_fence_before();
             mbar_arrive(ofree);
           }
-          uint32_t o[8];
+          float x[16];
 #pragma unroll
-          for (int i = 0; i < 16; i += 2)
-            o[i >> 1] = pack_bf16(fmaf(__uint_as_float(u[i]), f1, __uint_as_float(v[i]) * f0), fmaf(__uint_as_float(u[i + 1]), f1, __uint_as_float(v[i + 1]) * f0));
-          if (live) {
+          for (int i = 0; i < 16; ++i) x[i] = fmaf(__uint_as_float(u[i]), f1, __uint_as_float(v[i]) * f0);
+          if (!it.whole) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(piece + half * 32 + c + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+          } else if (live) {
+            uint32_t o[8];
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) o[i >> 1] = pack_bf16(x[i], x[i + 1]);
             *reinterpret_cast<uint4*>(dst + c) = make_uint4(o[0], o[1], o[2], o[3]);
             *reinterpret_cast<uint4*>(dst + c + 8) = make_uint4(o[4], o[5], o[6], o[7]);
           }
@@ -713,7 +783,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
 }
 
 // ---- host
-struct ChunkSpace { size_t kd, vd, qd, fac, info, tok, total; };
+struct ChunkSpace { size_t kd, vd, qd, fac, info, tok, share, part, desc, total; };
 static ChunkSpace chunk_space(long long R, long long T, long long max_kv, long long n_heads, long long H) {
   ChunkSpace c;
   size_t off = 0;
@@ -725,6 +795,9 @@ static ChunkSpace chunk_space(long long R, long long T, long long max_kv, long l
   c.fac = take((size_t)T * n_heads * 4);
   c.info = take((size_t)R * H * tiles * 16);
   c.tok = take(rows * H * 8);
+  c.share = take(kChMaxWorkers * sizeof(int4));
+  c.desc = take(2 * kChMaxWorkers * sizeof(int4));
+  c.part = take((size_t)kChMaxWorkers * 2 * kChRows * kChPitch * sizeof(float));
   c.total = off;
   return c;
 }
@@ -733,7 +806,7 @@ size_t kv_chunk_bytes(int R, int T, int max_kv, int n_heads, int H) { return chu
 
 moin_status launch_kv_chunk(HostState* hs, const KvView& kv, const int* table, const int* rows, const int* cu_q, const int* kv_len, int n_rows,
                             int max_pages, int R, int T, int max_q, int max_kv, int n_heads, const __nv_bfloat16* q, long long q_stride,
-                            __nv_bfloat16* out, long long out_stride, const float2* rope, float scale_log2, void* workspace, cudaStream_t s) {
+                            __nv_bfloat16* out, long long out_stride, const float2* rope, float scale_log2, void* workspace, KvPieces* pieces, cudaStream_t s) {
   const ChunkSpace c = chunk_space(R, T, max_kv, n_heads, kv.H);
   char* w = (char*)workspace;
   ChunkParams p = {};
@@ -745,7 +818,12 @@ moin_status launch_kv_chunk(HostState* hs, const KvView& kv, const int* table, c
   p.q = q; p.q_stride = q_stride; p.out = out; p.out_stride = out_stride; p.rope = rope; p.scale_log2 = scale_log2;
   p.kd = (__half*)(w + c.kd); p.vd = (__half*)(w + c.vd); p.qd = (__half*)(w + c.qd); p.q_fac = (float*)(w + c.fac); p.info = (uint4*)(w + c.info); p.tok = (float2*)(w + c.tok);
   p.dense_blocks = R * kv.H * p.tiles;
-  p.by_request = R > 1 && R <= kChOrder && max_kv > 2 * (long long)max_q;
+  p.share = (int4*)(w + c.share); p.part = (float*)(w + c.part); p.desc = (int4*)(w + c.desc);
+  const long long items = (long long)p.n_blk * R * kv.H, most = items * ((p.tiles + 1) / 2 + kChItemCost) / kChLeast + 1;   // shares that there can be
+  long long workers = 2L * hs->n_sms < kChMaxWorkers ? 2L * hs->n_sms : kChMaxWorkers;
+  if (workers > most) workers = most;
+  p.workers = (int)workers;
+  *pieces = {p.part, p.desc, p.workers, items};
   p.status = hs->status;
   CUtensorMap mq, mk, mv;
   const uint64_t dense_rows = (uint64_t)R * p.tiles * kChKeys;
@@ -755,11 +833,9 @@ moin_status launch_kv_chunk(HostState* hs, const KvView& kv, const int* table, c
   if (st) return st;
   cudaError_t e = ensure_smem_optin(OPTIN_KV_CHUNK, kv_chunk_kernel, kChSmem);
   if (e != cudaSuccess) return record_cuda(e);
-  const long long q_blocks = T, items = (long long)p.n_blk * R * kv.H;
-  ProfScope prof(MOIN_K_KV_CHUNK, 2, s);
-  e = launch_pdl(kv_dense_kernel, (unsigned)(p.dense_blocks + q_blocks), 128, 0, s, p);
+  e = launch_pdl(kv_dense_kernel, 1u + (unsigned)p.dense_blocks + (unsigned)T, 128, 0, s, p);
   if (e == cudaSuccess)
-    e = launch_pdl(kv_chunk_kernel, (unsigned)(items < 2L * hs->n_sms ? items : 2L * hs->n_sms), kChThreads, kChSmem, s, mq, mk, mv, p);
+    e = launch_pdl(kv_chunk_kernel, (unsigned)workers, kChThreads, kChSmem, s, mq, mk, mv, p);
   return record_cuda(e);
 }
 
