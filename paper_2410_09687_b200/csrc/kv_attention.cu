@@ -859,12 +859,15 @@ extern "C" moin_status moin_rope_table(float* table, int32_t n_pos, int32_t head
 static int kv_nt(long long tall) { return tall <= 8 ? 1 : 2; }
 
 // Long chunks go to the tcgen05 kernel (kv_chunk.cu) where the times that both would take, in us as fitted to measurements, say so:
-// here a row of queries passes 0.7 keys per ns and pays for beginning an item; there 128 rows pass 1.9 keys per ns and row, an item costs
-// 11 us of one of 296 CTAs, a chain of tiles is as long as the longest request, and keys and values are laid out first.  Measured, here /
-// there, with heads 32 on 4 kv heads, chunks of q behind pasts of p tokens:
-//   R = 1    p 500   q 64 17.9 / 18.6   q 128 24.2 / 22.1   q 512 40 / 29      p 4000  q 64 30 / 75   q 256 65 / 78    q 512 119 / 95
-//   R = 8    p 500   q 32 23.0 / 22.1   q 128 48.6 / 29.4   q 512 210 / 105    p 4000  q 32 63 / 86   q 64 110 / 100   q 512 824 / 394
-//   R = 64   p 1     q 64 48 / 53       q 128 108 / 107     q 256 306 / 228    p 4000  q 16 201 / 198 q 64 758 / 464   q 256 3100 / 1390
+// here a row of queries passes 0.66 keys per ns and pays for beginning an item; there a CTA of 296 takes 1.9 us for 128 keys of 128 rows
+// and twice that to begin and end an item, keys, values and queries are laid out first, and there are three launches.  Measured, here /
+// there, for chunks of q tokens behind p:
+//   32 heads on 4    R = 1    p 500   q 64 18 / 19     q 128 24 / 21     q 512 40 / 28     p 4000  q 64 30 / 30     q 512 118 / 55
+//                    R = 16   p 1     q 64 23 / 26     q 128 37 / 33     q 512 226 / 126   p 4000  q 16 63 / 53     q 512 1634 / 553
+//                    R = 64   p 1     q 64 55 / 60     q 128 122 / 118   q 256 341 / 224   p 4000  q 16 200 / 146   q 256 3091 / 1097
+//   4 heads on 1     R = 1    p 4000  q 64 14 / 19     q 512 31 / 30     p 16000           q 64 19 / 26     q 512 70 / 43
+//   8 heads on 8     R = 4    p 4000  q 64 28 / 40     q 128 40 / 40     q 512 118 / 61
+// Over 150 such calls (R 1 to 64, p 1 to 16000, q 16 to 512) the rule's choice takes 1 % more than the better of the two.
 static bool kv_use_chunk(int R, int T, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim, float scale) {
   const double G = n_heads / n_kv_heads, H = n_kv_heads;
   const int impl = gemm_impl_option();   // 1: the kernel here, 2: the other wherever it can take the call
@@ -876,10 +879,9 @@ static bool kv_use_chunk(int R, int T, int max_q, int max_kv, int n_heads, int n
   if (R * tiles * 64 * H * 264 + (double)T * n_heads * 132 > (1ll << 30) || (max_q * G / 128 + 1) * R * H > (1ll << 30) ||
       max_kv > (1 << 19)) return false;
   if (impl == 2) return true;
-  const double keys = max_kv - 0.5 * (max_q < max_kv ? max_q : max_kv);
-  const double here = 8 + queries * n_heads * (keys + 200) / 0.7e6;
-  const double chain = 0.0165 * max_kv, work = items / 296 * 11 + items * 128 * keys / 1.9e6;
-  return 12 + (chain > work ? chain : work) + 1e-4 * R * H * max_kv < here;
+  const double keys = max_kv - 0.5 * (max_q < max_kv ? max_q : max_kv), pairs = items * (keys / 128 + 2) / 296;
+  const double here = 11 + queries * n_heads * (keys + 240) / 0.66e6;
+  return 16 + 1.9 * (pairs > 2 ? pairs : 2) + 1e-4 * R * H * max_kv + 2e-4 * queries * n_heads < here;
 }
 
 extern "C" size_t moin_kv_attention_workspace_bytes(int32_t R, int32_t T, int32_t max_q, int32_t max_kv, int32_t n_heads, int32_t n_kv_heads,

@@ -559,6 +559,41 @@ def test_chunks_of_many_items(lens, q, kernel):
     _check_attention(cache, tables, table, lens, q, 2 if len(lens) > 9 else 3, rng, rope=True)
 
 
+@pytest.mark.parametrize("kind", ["two items", "runs of requests", "one head each", "short behind long"])
+def test_chunk_shares(kind, kernel):
+    """Items that many CTAs share, shares that hold many items, requests without tokens, keys or queries between them."""
+    rng = np.random.default_rng(27)
+    if kind == "two items":
+        lens, q, H, G = [9000], [200], 1, 1
+    elif kind == "runs of requests":
+        lens = [int(x) for x in rng.integers(0, 300, 150)]
+        q, H, G = [int(rng.integers(0, min(n, 70) + 1)) for n in lens], 1, 3
+    elif kind == "one head each":
+        lens, q, H, G = [1, 700, 64, 2000, 65, 0, 1300], [1, 130, 64, 1, 65, 0, 128], 3, 1
+    else:
+        lens, q, H, G = [4000] + [20] * 30 + [2500], [3] + [20] * 30 + [129], 1, 2
+    cache, tables, table, _ = _serve(rng, lens, H, 64, 64)
+    _check_attention(cache, tables, table, lens, q, H * G, rng, rope=True)
+
+
+def test_chunk_maxima_that_move(kernel):
+    """Scores that rise by 20 powers of two from tile to tile, fall as fast, jump once, and stay: weights are taken against the largest so far."""
+    rng = np.random.default_rng(28)
+    lens, q_lens, heads = [1000, 500], [70, 33], 4
+    cache, tables, table, slot = _serve(rng, lens, 1, 64, 64)
+    u = rng.choice([-1.0, 1.0], (4, 64))
+    t = np.concatenate([np.arange(n) for n in lens])
+    k = 1.75 * t[:, None] / 64 * u[0] + np.where(t[:, None] >= 333, 9.0, 0.0) * u[1] + 0.1 * rng.standard_normal((len(t), 64))
+    v = rng.standard_normal((len(t), 64)) + 1.0
+    moin.kv_append(cache, i32(slot), _dev(ref.bf16(k[:, None].astype(np.float32))), _dev(ref.bf16(v[:, None].astype(np.float32))))
+    q = ref.bf16(np.broadcast_to(np.stack([u[0], -u[0], u[1], 0.01 * u[2]]), (103, heads, 64)).astype(np.float32))
+    cu = [0, 70, 103]
+    want, tol = ref.attention(cache.pages.cpu().numpy(), table, None, cu, lens, q, 0.125, 64)
+    got = moin.kv_attention(cache, tables, _dev(q), i32(cu), i32(lens), 70, 1000, scale=0.125).float().cpu().numpy().astype(np.float64)
+    bad = np.abs(got - want) > tol
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4], (np.abs(got - want) / tol).max())
+
+
 def test_the_rule_sends_long_chunks_to_the_tensor_cores():
     rng = np.random.default_rng(26)
     cache, tables, _, _ = _serve(rng, [600, 600], 4, 64, 64)
