@@ -456,7 +456,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   if (warp < 2) {
     // ------------------------------------------------------------------ loads and MMAs of a stream, one after the other: the whole
     // warp waits, one lane issues.  Tile i of the stream lies in slot i & 1; it is replaced when its product is complete.
-    const int h = warp;
+    const int h = __shfl_sync(0xffffffffu, warp, 0);   // (known to be the warp's: descriptors stay in uniform registers)
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
     const bool leader = elect_one();
     const uint32_t sk = sK + 2 * h * kChKV, sv = sV + 2 * h * kChKV, kf = kfull + 16 * h, vf = vfull + 16 * h;
     bool ok = true;
@@ -500,7 +501,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       tc_fence_after();
       if (leader) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) tc_mma_bf16(tmem + h * 64 + 32 * upper, dq + (uint64_t)(2 * k), dk + (uint64_t)(2 * k), kChIdescHalf, k > 0 ? 1u : 0u);
+        for (int k = 0; k < 4; ++k) tc_mma_bf16(tm + h * 64 + 32 * upper, dq + (uint64_t)(2 * k), dk + (uint64_t)(2 * k), kChIdescHalf, k > 0 ? 1u : 0u);
         tc_commit((upper ? supper : sready) + 8 * h);
         if (!upper && at.j + 2 >= at.it.n) tc_commit(qfree + 8 * (at.item & 1u));
       }
@@ -535,7 +536,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       if (leader) {
         const uint64_t dv = sdesc_k128(sv + s * kChKV);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) tc_mma_bf16_ta(tmem + 128 + h * 64, tmem + h * 64 + 8 * k, dv + kChVStep * k, kChIdescPV, k > 0 ? 1u : first);
+        for (int k = 0; k < 4; ++k) tc_mma_bf16_ta(tm + 128 + h * 64, tm + h * 64 + 8 * k, dv + kChVStep * k, kChIdescPV, k > 0 ? 1u : first);
         tc_commit(pvdone + 8 * h);
       }
       if (!same) {
