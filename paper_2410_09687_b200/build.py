@@ -71,7 +71,7 @@ def build_steps(force: bool = False) -> str:
            os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include")]
     tmp = STEPS + f".tmp{os.getpid()}"
     p = subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] +
-                       [f"-isystem{d}" for d in inc] + [src, "-o", tmp, "-L" + os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu",
+                       [f"-isystem{d}" for d in inc] + [src, "-o", tmp, "-L" + os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda",
                                                         "-ltorch_python"], capture_output=True, text=True)
     if p.returncode != 0:
         raise RuntimeError(f"g++ failed for {src}:\n{p.stdout}\n{p.stderr}")

@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -91,6 +92,9 @@ cudaStream_t stream_of(PyObject* o) {   // None: the current one
   return o == Py_None ? c10::cuda::getCurrentCUDAStream().stream() : reinterpret_cast<cudaStream_t>((intptr_t)integer(o));
 }
 
+// A new bf16 tensor beside `like` (on the current CUDA device: the caller has looked), without the dispatcher.
+at::Tensor fresh(at::IntArrayRef size, const at::Tensor& like) { return at::Tensor(at::detail::empty_cuda(size, at::kBFloat16, like.device(), std::nullopt)); }
+
 template <class F>
 PyObject* guarded(Py_ssize_t got, Py_ssize_t want, F&& body) {
   if (got != want) {
@@ -148,9 +152,9 @@ PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const auto* kv = reinterpret_cast<const moin_kv*>((intptr_t)integer(a[0]));
     const at::Tensor& slot = tensor(a[1]);
     const int32_t T = length(slot);
-    auto out = [&](PyObject* o) { return o == Py_None ? at::empty({T, kv->n_kv_heads, kv->head_dim}, slot.options().dtype(at::kBFloat16)) : tensor(o); };
-    const at::Tensor k = out(a[2]), v = out(a[3]);
     const int32_t* s = vec(a[1], T);
+    auto out = [&](PyObject* o) { return o == Py_None ? fresh({T, kv->n_kv_heads, kv->head_dim}, slot) : tensor(o); };
+    const at::Tensor k = out(a[2]), v = out(a[3]);
     const Rows kr = rows_of(k, T, kv->n_kv_heads, kv->head_dim), vr = rows_of(v, T, kv->n_kv_heads, kv->head_dim);
     const int32_t st = f_read(kv, s, kr.p, kr.stride, vr.p, vr.stride, T, stream_of(a[4]));
     return Py_BuildValue("(iNN)", (int)st, THPVariable_Wrap(k), THPVariable_Wrap(v));
@@ -171,7 +175,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (q.size(1) > INT32_MAX) refuse("too many heads");
     const int32_t heads = (int32_t)q.size(1);
     const Rows qr = rows_of(q, T, heads, kv->head_dim);
-    const at::Tensor out = a[10] == Py_None ? at::empty(q.sizes(), q.options()) : tensor(a[10]);
+    const at::Tensor out = a[10] == Py_None ? fresh(q.sizes(), q) : tensor(a[10]);
     const Rows outr = rows_of(out, T, heads, kv->head_dim);
     const Rope rope = rope_of(a[9], kv->head_dim);
     int32_t max_q = size32(a[5]);
