@@ -21,7 +21,7 @@
 // A weight below 2^-14 is off by 2^-25 at most: 2^-30 of the row's largest, so that 2^19 keys stay within 2^-11 of the sum.
 // Tensor memory: S_h / P_h at columns 64 h, O_h at 128 + 64 h.  Every mbarrier wait is bounded; on expiry the CTA raises the status
 // flag, drains and returns.
-// 4 requests of 512 new tokens behind 830 to 5900, 32 heads on 4: about 106 us for 52 GFLOP, bound by the instructions and exponentials of the
+// 4 requests of 512 new tokens behind 830 to 5900, 32 heads on 4: about 107 us for 52 GFLOP, bound by the instructions and exponentials of the
 // weights (a warp's tile 1.3 us, four warps on a scheduler: issue slots 49 % busy, exponentials 52 %, tensor cores 24 %) and by the chain.  One warp that issued both streams' MMAs took 900
 // cycles a round, and with the maximum found first, whole items per CTA and all scores behind the product it was 125 us.
 #include <cuda.h>
@@ -613,19 +613,18 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
           float ma = -INFINITY, mc = -INFINITY;
           uint32_t w[2][16];
           auto group = [&](const uint32_t (&v)[16], int k, bool masked) {
-            float x[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = masked && 16 * k + i > seen ? -INFINITY : __uint_as_float(v[i]);
+            auto out = [&](int i) { return masked && 16 * k + i > seen; };
+            auto x = [&](int i) { return out(i) ? -INFINITY : __uint_as_float(v[i]); };
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-              ma = fmax3(ma, x[i], x[i + 1]);
-              mc = fmax3(mc, x[i + 2], x[i + 3]);
+              ma = fmax3(ma, x(i), x(i + 1));
+              mc = fmax3(mc, x(i + 2), x(i + 3));
             }
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
               float x0, x1;
-              unpair_f32(fma2(pair_f32(x[i], x[i + 1]), c2, off2), x0, x1);
-              const float p0 = ch_exp2(x0), p1 = ch_exp2(x1);
+              unpair_f32(fma2(pair_f32(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), c2, off2), x0, x1);
+              const float p0 = out(i) ? 0.f : ch_exp2(x0), p1 = out(i + 1) ? 0.f : ch_exp2(x1);   // (c may be 0: not by scores of -inf)
               l2 = add2(l2, pair_f32(p0, p1));
               const __half2 h2 = __floats2half2_rn(p0, p1);
               w[k >> 1][8 * (k & 1) + (i >> 1)] = *reinterpret_cast<const uint32_t*>(&h2);

@@ -594,6 +594,14 @@ def test_chunk_maxima_that_move(kernel):
     assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4], (np.abs(got - want) / tol).max())
 
 
+def test_chunks_of_a_scale_that_vanishes(kernel):
+    """Scores of 1e-40, whose factors underflow: the means of the values seen."""
+    rng = np.random.default_rng(29)
+    lens = [200, 90]
+    cache, tables, table, _ = _serve(rng, lens, 2, 64, 16)
+    _check_attention(cache, tables, table, lens, [80, 90], 8, rng, scale=1e-40)
+
+
 def test_the_rule_sends_long_chunks_to_the_tensor_cores():
     rng = np.random.default_rng(26)
     cache, tables, _, _ = _serve(rng, [600, 600], 4, 64, 64)
