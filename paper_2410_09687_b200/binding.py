@@ -2,6 +2,7 @@
 tensors in place of raw pointers.  Argument marshalling only."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import List, Optional, Sequence
@@ -222,6 +223,12 @@ def _stream(stream: Optional[torch.cuda.Stream]) -> int:
         return stream.cuda_stream
     # the handle of torch.cuda.current_stream() without building the Stream object (0.3 us instead of 3.2 us a call)
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _on(stream):
+    """Tensors made inside belong to the stream that a call goes to: the allocator hands their memory out behind, and takes it back
+    for, work of that stream, not of the current one (which may still be using a block that it has freed)."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 def set_option(key: int, value: int) -> None:
@@ -654,7 +661,8 @@ class KvCache:
 
 class KvTables:
     """moin_kv_tables: block table, stack of free pages, lengths.  Without ``lens`` and ``n_free`` the tables start empty
-    (moin_kv_tables_reset, which also fills ``free_pages``)."""
+    (moin_kv_tables_reset on ``stream``, which also fills ``free_pages``: other work on a tensor that is handed over is the caller's to
+    order).  New tensors belong to ``stream``."""
 
     def __init__(self, block_table: torch.Tensor, free_pages: torch.Tensor, page_tokens: int, lens: Optional[torch.Tensor] = None,
                  n_free: Optional[torch.Tensor] = None, stream=None):
@@ -662,8 +670,9 @@ class KvTables:
         assert (lens is None) == (n_free is None)
         reset = lens is None
         if reset:
-            lens = torch.empty(block_table.shape[0], dtype=torch.int32, device=block_table.device)
-            n_free = torch.empty(1, dtype=torch.int32, device=block_table.device)
+            with _on(stream):
+                lens = torch.empty(block_table.shape[0], dtype=torch.int32, device=block_table.device)
+                n_free = torch.empty(1, dtype=torch.int32, device=block_table.device)
         assert lens.dtype == torch.int32 and lens.shape == (block_table.shape[0],) and n_free.dtype == torch.int32 and n_free.numel() == 1
         self.block_table, self.free_pages, self.lens, self.n_free = block_table, free_pages, lens, n_free
         self.n_rows, self.max_pages = block_table.shape
@@ -679,8 +688,9 @@ class KvTables:
 
     @classmethod
     def empty(cls, n_rows: int, max_pages: int, n_pages: int, page_tokens: int, device, stream=None) -> "KvTables":
-        i32 = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device=device)  # noqa: E731
-        return cls(i32(n_rows, max_pages), i32(n_pages), page_tokens, stream=stream)
+        with _on(stream):
+            return cls(torch.zeros(n_rows, max_pages, dtype=torch.int32, device=device), torch.empty(n_pages, dtype=torch.int32, device=device),
+                       page_tokens, stream=stream)
 
     def reset(self, stream=None) -> None:
         """moin_kv_tables_reset: every request forgotten, every page free."""
