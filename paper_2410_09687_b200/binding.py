@@ -734,7 +734,8 @@ def kv_update(tables: KvTables, want: torch.Tensor, batch: KvBatch, rows: Option
 
 def rope_table(n_pos: int, head_dim: int, base: float, device, stream=None) -> torch.Tensor:
     """moin_rope_table: [n_pos, head_dim / 2, 2] fp32 (cos, sin)."""
-    table = torch.empty(n_pos, head_dim // 2, 2, dtype=torch.float32, device=device)
+    with _on(stream):
+        table = torch.empty(n_pos, head_dim // 2, 2, dtype=torch.float32, device=device)
     _check(lib().moin_rope_table(_ptr(table), n_pos, head_dim, float(base), _stream(stream)), "moin_rope_table")
     return table
 
@@ -793,7 +794,8 @@ def decoder_forward_cached(model: DecoderModel, tokens: torch.Tensor, layers: Kv
     if logits_mode != LOGITS_NONE:
         shape = (T if logits_mode == LOGITS_ALL else R, cfg.vocab)
         if logits is None:
-            logits = torch.empty(*shape, dtype=torch.bfloat16, device=tokens.device)
+            with _on(stream):
+                logits = torch.empty(*shape, dtype=torch.bfloat16, device=tokens.device)
         elif logits.dtype != torch.bfloat16 or logits.shape != shape:
             raise MoinError(f"expected bf16 {shape}, got {tuple(logits.shape)} of {logits.dtype}")
     taps = _Taps(_ptr(hidden_in), _ptr(hidden_out), layer_begin, cfg.n_layers if layer_end is None else layer_end)

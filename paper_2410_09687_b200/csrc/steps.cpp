@@ -8,6 +8,7 @@
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -92,8 +93,13 @@ cudaStream_t stream_of(PyObject* o) {   // None: the current one
   return o == Py_None ? c10::cuda::getCurrentCUDAStream().stream() : reinterpret_cast<cudaStream_t>((intptr_t)integer(o));
 }
 
-// A new bf16 tensor beside `like` (on the current CUDA device: the caller has looked), without the dispatcher.
-at::Tensor fresh(at::IntArrayRef size, const at::Tensor& like) { return at::Tensor(at::detail::empty_cuda(size, at::kBFloat16, like.device(), std::nullopt)); }
+// A new bf16 tensor beside `like` (on the current CUDA device: the caller has looked) for a call on stream s, without the dispatcher.
+// Its memory belongs to s: of a block of the current stream, that one's pending work may be anywhere.
+at::Tensor fresh(at::IntArrayRef size, const at::Tensor& like, cudaStream_t s) {
+  c10::cuda::OptionalCUDAStreamGuard guard;
+  if (s != c10::cuda::getCurrentCUDAStream().stream()) guard.reset_stream(c10::cuda::getStreamFromExternal(s, like.get_device()));
+  return at::Tensor(at::detail::empty_cuda(size, at::kBFloat16, like.device(), std::nullopt));
+}
 
 template <class F>
 PyObject* guarded(Py_ssize_t got, Py_ssize_t want, F&& body) {
@@ -153,10 +159,11 @@ PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& slot = tensor(a[1]);
     const int32_t T = length(slot);
     const int32_t* s = vec(a[1], T);
-    auto out = [&](PyObject* o) { return o == Py_None ? fresh({T, kv->n_kv_heads, kv->head_dim}, slot) : tensor(o); };
+    const cudaStream_t stream = stream_of(a[4]);
+    auto out = [&](PyObject* o) { return o == Py_None ? fresh({T, kv->n_kv_heads, kv->head_dim}, slot, stream) : tensor(o); };
     const at::Tensor k = out(a[2]), v = out(a[3]);
     const Rows kr = rows_of(k, T, kv->n_kv_heads, kv->head_dim), vr = rows_of(v, T, kv->n_kv_heads, kv->head_dim);
-    const int32_t st = f_read(kv, s, kr.p, kr.stride, vr.p, vr.stride, T, stream_of(a[4]));
+    const int32_t st = f_read(kv, s, kr.p, kr.stride, vr.p, vr.stride, T, stream);
     return Py_BuildValue("(iNN)", (int)st, THPVariable_Wrap(k), THPVariable_Wrap(v));
   });
 }
@@ -175,7 +182,8 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (q.size(1) > INT32_MAX) refuse("too many heads");
     const int32_t heads = (int32_t)q.size(1);
     const Rows qr = rows_of(q, T, heads, kv->head_dim);
-    const at::Tensor out = a[10] == Py_None ? fresh(q.sizes(), q) : tensor(a[10]);
+    const cudaStream_t s = stream_of(a[11]);
+    const at::Tensor out = a[10] == Py_None ? fresh(q.sizes(), q, s) : tensor(a[10]);
     const Rows outr = rows_of(out, T, heads, kv->head_dim);
     const Rope rope = rope_of(a[9], kv->head_dim);
     int32_t max_q = size32(a[5]);
@@ -191,7 +199,6 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       scale = kv->head_dim == 64 ? 0.125 : 0.08838834764831845;
     }
     const int32_t *cu = vec(a[3], (int64_t)R + 1), *len = vec(a[4], R), *rows = vec(a[7], R);
-    const cudaStream_t s = stream_of(a[11]);
     const size_t bytes = f_ws(R, T, max_q, max_kv, heads, kv->n_kv_heads, kv->head_dim);
     void* ws = c10::cuda::CUDACachingAllocator::raw_alloc_with_stream(bytes, s);
     const int32_t st = f_attention(kv, tables, rows, cu, len, R, T, max_q, max_kv, qr.p, qr.stride, heads, (float)scale, rope.p, rope.n, outr.p,
