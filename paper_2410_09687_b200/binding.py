@@ -248,7 +248,8 @@ def device_status_reset(stream=None) -> None:
 
 def selftest_bounded_wait(limit_us: int, stream=None) -> dict:
     """moin_selftest_bounded_wait: runs the expiry path of the library's bounded device-side wait once."""
-    res = torch.full((3,), -1, dtype=torch.int32, device="cuda")
+    with _on(stream):
+        res = torch.full((3,), -1, dtype=torch.int32, device="cuda")
     _check(lib().moin_selftest_bounded_wait(int(limit_us), _ptr(res), _stream(stream)), "moin_selftest_bounded_wait")
     torch.cuda.synchronize()
     r = res.cpu().tolist()
@@ -278,7 +279,8 @@ class Router:
         self.centroids = centroids
         self.map = centroid_to_expert
         self.K, self.D = centroids.shape
-        self.inv_norm = torch.empty(self.K, dtype=torch.float32, device=centroids.device)
+        with _on(stream):
+            self.inv_norm = torch.empty(self.K, dtype=torch.float32, device=centroids.device)
         _check(lib().moin_router_prepare(_ptr(centroids), self.K, self.D, _ptr(self.inv_norm), _stream(stream)),
                "moin_router_prepare")
         self.c = _Router(_ptr(centroids), _ptr(self.inv_norm), _ptr(centroid_to_expert), self.K, self.D)
@@ -312,7 +314,8 @@ def route(router: Router, queries: torch.Tensor, out_expert: Optional[torch.Tens
     assert queries.dtype == torch.bfloat16 and queries.dim() == 2 and queries.shape[1] == router.D
     Q = queries.shape[0]
     if out_expert is None:
-        out_expert = torch.empty(Q, dtype=torch.int32, device=queries.device)
+        with _on(stream):
+            out_expert = torch.empty(Q, dtype=torch.int32, device=queries.device)
     n, s = router.workspace_bytes(Q), _stream(stream)
     ws = _scratch_alloc(n, s)
     try:
@@ -327,9 +330,10 @@ def route_top2(router: Router, queries: torch.Tensor, stream=None) -> dict:
     """moin_route_top2: best centroid, runner-up and the margin between their cosines."""
     assert queries.dtype == torch.bfloat16 and queries.dim() == 2 and queries.shape[1] == router.D
     Q, dev = queries.shape[0], queries.device
-    out = {"expert": torch.empty(Q, dtype=torch.int32, device=dev), "centroid": torch.empty(Q, dtype=torch.int32, device=dev),
-           "second": torch.empty(Q, dtype=torch.int32, device=dev), "best": torch.empty(Q, dtype=torch.float32, device=dev),
-           "margin": torch.empty(Q, dtype=torch.float32, device=dev)}
+    with _on(stream):
+        out = {"expert": torch.empty(Q, dtype=torch.int32, device=dev), "centroid": torch.empty(Q, dtype=torch.int32, device=dev),
+               "second": torch.empty(Q, dtype=torch.int32, device=dev), "best": torch.empty(Q, dtype=torch.float32, device=dev),
+               "margin": torch.empty(Q, dtype=torch.float32, device=dev)}
     n, s = lib().moin_route_top2_workspace_bytes(Q, router.K, router.D), _stream(stream)
     ws = _scratch_alloc(n, s)
     try:
@@ -418,7 +422,8 @@ def kmeans_update(plan: "Plan", x: torch.Tensor, centroids_old: torch.Tensor,
     assert x.dtype == torch.bfloat16 and centroids_old.dtype == torch.bfloat16 and x.dim() == 2
     assert centroids_old.shape == (plan.E, x.shape[1]) and plan.T == x.shape[0]
     if centroids_new is None:
-        centroids_new = torch.empty_like(centroids_old)
+        with _on(stream):
+            centroids_new = torch.empty_like(centroids_old)
     _check(lib().moin_kmeans_update(ctypes.byref(plan.c), _ptr(x), _ptr(centroids_old), _ptr(centroids_new),
                                     _ptr(inv_norm_new), x.shape[1], _stream(stream)), "moin_kmeans_update")
     return centroids_new
@@ -488,7 +493,8 @@ def plan_build(token_expert: torch.Tensor, E: int, mode: int = PLAN_AUTO, plan: 
     assert token_expert.dtype == torch.int32 and token_expert.dim() == 1
     T = token_expert.shape[0]
     if plan is None:
-        plan = Plan(T, E, token_expert.device, mode)
+        with _on(stream):
+            plan = Plan(T, E, token_expert.device, mode)
     else:
         assert plan.T == T and plan.E == E
         plan.c.mode = mode
@@ -510,7 +516,8 @@ def _workspace(device, nbytes: int) -> torch.Tensor:
 
 def lora_linear(plan: Optional[Plan], x: torch.Tensor, W: torch.Tensor, pool: Optional[Pool], scale: float,
                 y: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """moin_lora_linear.  Returns y (bf16 [T, d_out])."""
+    """moin_lora_linear.  Returns y (bf16 [T, d_out]).  Without ``workspace`` the calls on a device share one: order them on one
+    stream, or give each its own."""
     assert x.dtype == torch.bfloat16 and W.dtype == torch.bfloat16 and x.dim() == 2 and W.dim() == 2
     T, d_in = x.shape
     d_out = W.shape[0]
@@ -518,7 +525,8 @@ def lora_linear(plan: Optional[Plan], x: torch.Tensor, W: torch.Tensor, pool: Op
     if pool is not None:
         assert pool.d_in == d_in and pool.d_out == d_out
     if y is None:
-        y = torch.empty(T, d_out, dtype=torch.bfloat16, device=x.device)
+        with _on(stream):
+            y = torch.empty(T, d_out, dtype=torch.bfloat16, device=x.device)
     r = pool.r if pool is not None else 8
     n = lib().moin_lora_linear_workspace_bytes(T, d_in, d_out, r)
     ws = workspace if workspace is not None else _workspace(x.device, n)
@@ -550,7 +558,7 @@ class JobGroup:
 
 def lora_linear_group(plan: Plan, group: JobGroup, scale: float, workspace: Optional[torch.Tensor] = None,
                       stream=None) -> None:
-    """moin_lora_linear_group: every job's y = x W^T + scale (x A_e^T) B_e^T, merged launches."""
+    """moin_lora_linear_group: every job's y = x W^T + scale (x A_e^T) B_e^T, merged launches.  ``workspace``: as for lora_linear."""
     ws = workspace if workspace is not None else _workspace(group.device, group.workspace_bytes)
     _check(lib().moin_lora_linear_group(ctypes.byref(plan.c), group.c, group.n, float(scale), _ptr(ws), ws.numel(),
                                         _stream(stream)), "moin_lora_linear_group")
@@ -608,7 +616,8 @@ def dequant_fp8(codes: torch.Tensor, scale: torch.Tensor, out: Optional[torch.Te
     assert codes.dtype == torch.uint8 and scale.dtype == torch.float32 and codes.dim() == 2
     d_out, d_in = codes.shape
     if out is None:
-        out = torch.empty(d_out, d_in, dtype=torch.bfloat16, device=codes.device)
+        with _on(stream):
+            out = torch.empty(d_out, d_in, dtype=torch.bfloat16, device=codes.device)
     _check(lib().moin_dequant_fp8(_ptr(codes), _ptr(scale), d_out, d_in, _ptr(out), _stream(stream)), "moin_dequant_fp8")
     return out
 
@@ -619,12 +628,13 @@ def decoder_forward(model: DecoderModel, tokens: torch.Tensor, cu_seqlens: torch
                     hidden_out: Optional[torch.Tensor] = None, layer_begin: int = 0, layer_end: Optional[int] = None,
                     stream=None, token_expert: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """moin_decoder_forward, or moin_decoder_forward_per_token when ``token_expert`` ([T] int32) is given.
-    Returns logits (bf16) or None for LOGITS_NONE."""
+    Returns logits (bf16) or None for LOGITS_NONE.  The calls over one model share its scratch: order them on one stream."""
     R, T = cu_seqlens.shape[0] - 1, tokens.shape[0]
     cfg = model.cfg
     if logits is None and logits_mode != LOGITS_NONE:
         rows = T if logits_mode == LOGITS_ALL else R
-        logits = torch.empty(rows, cfg.vocab, dtype=torch.bfloat16, device=tokens.device)
+        with _on(stream):
+            logits = torch.empty(rows, cfg.vocab, dtype=torch.bfloat16, device=tokens.device)
     taps = _Taps(_ptr(hidden_in), _ptr(hidden_out), layer_begin, cfg.n_layers if layer_end is None else layer_end)
     ws = model.workspace(R, T)
     if token_expert is not None:
