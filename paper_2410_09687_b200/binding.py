@@ -704,6 +704,7 @@ class KvTables:
 
     def reset(self, stream=None) -> None:
         """moin_kv_tables_reset: every request forgotten, every page free."""
+        _here(self.device, "the tables are")
         _check(lib().moin_kv_tables_reset(ctypes.byref(self.c), _stream(stream)), "moin_kv_tables_reset")
 
 
@@ -727,6 +728,12 @@ def _same_device(*holders) -> int:
     return first
 
 
+def _here(device: int, what: str) -> None:
+    """The library launches on the current device: what lives on another one would be foreign addresses to it."""
+    if device != torch.cuda.current_device():
+        raise MoinError(f"{what} on device {device}, the current one is {torch.cuda.current_device()}")
+
+
 def _handle(stream) -> Optional[int]:
     return None if stream is None else stream.cuda_stream
 
@@ -746,6 +753,8 @@ def rope_table(n_pos: int, head_dim: int, base: float, device, stream=None) -> t
     """moin_rope_table: [n_pos, head_dim / 2, 2] fp32 (cos, sin)."""
     with _on(stream):
         table = torch.empty(n_pos, head_dim // 2, 2, dtype=torch.float32, device=device)
+    if table.is_cuda:   # (others: _ptr)
+        _here(table.get_device(), "the table would be")
     _check(lib().moin_rope_table(_ptr(table), n_pos, head_dim, float(base), _stream(stream)), "moin_rope_table")
     return table
 
@@ -815,6 +824,7 @@ def decoder_forward_cached(model: DecoderModel, tokens: torch.Tensor, layers: Kv
         if t is not None and (t.dtype != torch.int32 or t.shape != (n,)):
             raise MoinError(f"expected {n} int32 values, got {tuple(t.shape)} of {t.dtype}")
     where = _same_device(tables, batch, *layers.caches)
+    _here(model.device.index, "the model is")
     if where != torch.cuda.current_device() or any(t is not None and t.get_device() != where for t in (tokens, rows, req_expert, rope, logits, hidden_in, hidden_out, workspace)):
         raise MoinError("caches, tables and tensors must live on the current device")
     s = _stream(stream)
