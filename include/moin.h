@@ -561,7 +561,8 @@ moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables* tables, c
  *   batch      as filled by moin_kv_update for these tables and rows; refused requests get the logits of attention outputs of zero
  *   rope       table of moin_rope_table(rope_len, head_dim, model->rope_base), rope_len >= max_kv
  *   max_q, max_kv   host upper bounds as for moin_kv_attention
- *   logits     [batch->T, vocab] or [R, vocab], as logits_mode says (MOIN_LOGITS_LAST: zeros for a request without new tokens)
+ *   logits     [batch->T, vocab] or [R, vocab], as logits_mode says (MOIN_LOGITS_LAST: zeros for a request without new tokens,
+ *              also where none of them has any, batch->T == 0)
  * Reads nothing back; can be captured together with moin_kv_update.  workspace: 256-byte aligned,
  * moin_decoder_cached_workspace_bytes(...) bytes with the bounds that the call goes by.  Errors: as for moin_decoder_forward and moin_kv_attention, before anything
  * is launched. */

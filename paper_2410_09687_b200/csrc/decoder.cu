@@ -696,6 +696,14 @@ extern "C" moin_status moin_decoder_forward_cached(const moin_model* m, const in
                                                    void* workspace, size_t workspace_bytes, moin_stream stream) {
   if (!m || !caches || !tables || !batch) return MOIN_ERR_INVALID_ARG;
   if (batch->R < 0 || batch->T < 0) return MOIN_ERR_INVALID_ARG;
+  if (logits_mode == MOIN_LOGITS_LAST && batch->T == 0 && batch->R > 0) {   // no request has new tokens: no blocks, and zeros
+    if (!logits) return MOIN_ERR_INVALID_ARG;
+    if (m->vocab < 1) return MOIN_ERR_BAD_SHAPE;
+    HostState* hs;
+    const moin_status st = host_state(&hs);
+    if (st) return st == MOIN_ERR_NO_DEVICE ? MOIN_OK : st;   // (where there is no device there is no memory to clear either)
+    return record_cuda(cudaMemsetAsync(logits, 0, (size_t)batch->R * m->vocab * 2, (cudaStream_t)stream));
+  }
   if (batch->R == 0 || batch->T == 0) return MOIN_OK;
   if (!batch->cu_q || !batch->kv_len || !batch->slot || !batch->pos || !rope) return MOIN_ERR_INVALID_ARG;
   if (max_q < 1 || max_q > batch->T) max_q = batch->T;
