@@ -556,7 +556,8 @@ moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables* tables, c
  * them out) run through the blocks, their keys and values are stored in the layers' caches, and they attend to everything
  * cached of their request, themselves included.  The tokens of a request that runs through in one call or in many see the same
  * stored keys and values.  Everything else is moin_decoder_forward (adapters by req_expert, conventions, storage, taps).
- *   tokens     [batch->T] int32; rows of the batch behind cu_q[R] run as tokens of the base model and are stored nowhere
+ *   tokens     [batch->T] int32; rows of the batch behind cu_q[R] run as tokens of the base model with attention outputs of zero and are
+ *              stored nowhere (so do all rows where R == 0)
  *   caches     HOST array [n_layers], each of n_kv_heads heads of head_dim (64) in pages of tables->page_tokens
  *   batch      as filled by moin_kv_update for these tables and rows; refused requests get the logits of attention outputs of zero
  *   rope       table of moin_rope_table(rope_len, head_dim, model->rope_base), rope_len >= max_kv

@@ -7,15 +7,25 @@
 namespace moin {
 
 // token -> (position inside its request, its expert: the caller's per-token id if given, else the expert of its
-// request).  One CTA per request.
+// request).  One CTA per request.  On top of a cache (`att`, rows of att_row16 16-byte units) the batch may have room behind its last
+// request, rows of no request that run through the base model: one CTA more for their experts, and the others behind it
+// clear what the attention leaves as it was - these rows, and a request's behind the max_q-th - so that no row depends
+// on what the workspace held.  (Only once a call: no layer writes there.)
 __global__ void __launch_bounds__(256)
 token_meta_kernel(const int* __restrict__ cu, const int* __restrict__ req_expert,
                   const int* __restrict__ token_expert_in, int R, int T, int* __restrict__ pos,
-                  int* __restrict__ token_expert, int* __restrict__ last_row) {
+                  int* __restrict__ token_expert, int* __restrict__ last_row, uint4* __restrict__ att, int att_row16, int max_q) {
   pdl_begin();
   const int r = blockIdx.x;
-  if (r == R) {   // (only where the batch has room behind its last request: rows of no request, base model)
-    for (int t = min(max(cu[R], 0), T) + threadIdx.x; t < T; t += blockDim.x) token_expert[t] = -1;
+  auto clear = [&](int t) {
+    for (int i = threadIdx.x; i < att_row16; i += blockDim.x) att[(size_t)t * att_row16 + i] = make_uint4(0u, 0u, 0u, 0u);
+  };
+  if (r >= R) {
+    const int end = min(max(cu[R], 0), T);
+    if (r == R)
+      for (int t = end + threadIdx.x; t < T; t += blockDim.x) token_expert[t] = -1;
+    else
+      for (int t = end + r - R - 1; t < T; t += gridDim.x - R - 1) clear(t);
     return;
   }
   const int t0 = min(max(cu[r], 0), T), t1 = min(max(cu[r + 1], t0), T);
@@ -25,6 +35,8 @@ token_meta_kernel(const int* __restrict__ cu, const int* __restrict__ req_expert
     token_expert[t] = token_expert_in ? token_expert_in[t] : e;
   }
   if (threadIdx.x == 0) last_row[r] = (t1 > t0) ? t1 - 1 : -1;
+  if (att != nullptr)
+    for (int t = t0 + min(max_q, t1 - t0); t < t1; ++t) clear(t);
 }
 
 // W[j][i] = bf16(fp32(value(code[j][i]) * scale[j])): 8-bit float codes (4 exponent bits, bias 7, 3 mantissa bits,
@@ -473,12 +485,13 @@ static moin_status decoder_forward_impl(const moin_model* m, const int32_t* toke
                                         const moin_decoder_taps* taps, void* workspace, size_t workspace_bytes,
                                         moin_stream stream) {
   if (!m || R < 0 || T < 0) return MOIN_ERR_INVALID_ARG;
-  if (R == 0 || T == 0) return MOIN_OK;
+  if (T == 0 || (R == 0 && !kv)) return MOIN_OK;
   if (!cu_seqlens || !m->W || !m->attn_norm || !m->mlp_norm || !m->final_norm) return MOIN_ERR_INVALID_ARG;
   if (m->head_dim != 64 || m->n_kv_heads < 1 || (m->n_heads % m->n_kv_heads) != 0) return MOIN_ERR_BAD_SHAPE;
   if ((m->hidden % 64) != 0 || (m->ffn % 64) != 0 || (m->vocab % 8) != 0) return MOIN_ERR_BAD_SHAPE;
   if (logits_mode < MOIN_LOGITS_ALL || logits_mode > MOIN_LOGITS_NONE) return MOIN_ERR_INVALID_ARG;
-  if (logits_mode != MOIN_LOGITS_NONE && (!logits || !m->lm_head)) return MOIN_ERR_INVALID_ARG;
+  const bool no_logits = logits_mode == MOIN_LOGITS_NONE || (logits_mode == MOIN_LOGITS_LAST && R == 0);
+  if (!no_logits && (!logits || !m->lm_head)) return MOIN_ERR_INVALID_ARG;
   if (max_seqlen < 1 || max_seqlen > T) max_seqlen = T;
   const int lb = taps ? taps->layer_begin : 0, le = taps ? taps->layer_end : m->n_layers;
   if (lb < 0 || le > m->n_layers || lb > le) return MOIN_ERR_INVALID_ARG;
@@ -496,7 +509,9 @@ static moin_status decoder_forward_impl(const moin_model* m, const int32_t* toke
   const int qd = nh * 64, kvd = nkv * 64;
 
   { ProfScope prof(MOIN_K_GLUE, kv ? 1 : 2, s);
-  launch_pdl(token_meta_kernel, kv ? R + 1 : R, 256, 0, s, cu_seqlens, req_expert, token_expert_in, R, T, w.pos, w.token_expert, w.last_row);
+  const int clearing = T < 1056 ? (T + 7) / 8 : 132;
+  launch_pdl(token_meta_kernel, kv ? R + 1 + clearing : R, 256, 0, s, cu_seqlens, req_expert, token_expert_in, R, T, w.pos, w.token_expert, w.last_row,
+             kv ? (uint4*)w.att : nullptr, qd / 8, max_seqlen);
   if (!kv) launch_pdl(rope_table_kernel, (max_seqlen * 32 + 255) / 256, 256, 0, s, w.rope, max_seqlen, 32, (double)m->rope_base); }
   moin_plan plan;
   memset(&plan, 0, sizeof(plan));
@@ -639,7 +654,7 @@ static moin_status decoder_forward_impl(const moin_model* m, const int32_t* toke
       launch_pdl(add_rmsnorm_kernel, T, 256, 0, s, w.res, nullptr, (const __nv_bfloat16*)m->final_norm, w.xn, H, m->rms_eps, nullptr); }
     st = moin_lora_linear(nullptr, w.xn, m->lm_head, nullptr, 0.f, T, H, m->vocab, logits, w.lora, w.lora_bytes, stream);
     if (st) return st;
-  } else if (logits_mode == MOIN_LOGITS_LAST) {
+  } else if (!no_logits) {
     cudaError_t e = cudaMemsetAsync(w.xlast, 0, (size_t)R * H * 2, s);
     if (e != cudaSuccess) return record_cuda(e);
     { ProfScope prof(MOIN_K_GLUE, 1, s);
@@ -704,8 +719,8 @@ extern "C" moin_status moin_decoder_forward_cached(const moin_model* m, const in
     if (st) return st == MOIN_ERR_NO_DEVICE ? MOIN_OK : st;   // (where there is no device there is no memory to clear either)
     return record_cuda(cudaMemsetAsync(logits, 0, (size_t)batch->R * m->vocab * 2, (cudaStream_t)stream));
   }
-  if (batch->R == 0 || batch->T == 0) return MOIN_OK;
-  if (!batch->cu_q || !batch->kv_len || !batch->slot || !batch->pos || !rope) return MOIN_ERR_INVALID_ARG;
+  if (batch->T == 0) return MOIN_OK;
+  if (!batch->cu_q || (batch->R > 0 && !batch->kv_len) || !batch->slot || !batch->pos || !rope) return MOIN_ERR_INVALID_ARG;
   if (max_q < 1 || max_q > batch->T) max_q = batch->T;
   // everything the attention of a layer would refuse is refused before the first launch
   const long long row = (long long)tables->max_pages * tables->page_tokens;
