@@ -61,6 +61,7 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
+__device__ __forceinline__ uint64_t twice_f32(float v) { return pair_f32(v, v); }
 __device__ __forceinline__ float kv_exp2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -115,12 +116,19 @@ struct KvQuery {
   uint64_t fac[NT], sum[P][NT];
   int last[NT][2];          // last key the row sees
   int all;                  // keys below this are seen by every row
+  bool large;               // one of the warp's queries is
 };
+// A score is acc (sums of codes 2^-24 by queries near 2^9) times fac ks, and fac has 2^24 and the row's power in it: beyond 2^115 it
+// left fp32, and times signed sums gave NaN.  A warp with a query of 2^kKvLarge or more takes 2^24 into acc instead and holds
+// scores, factors and sums 2^-16 smaller until the score is complete: powers of two, so other rows' bits stay.  (Steps of their own:
+// the others pay nothing.)
+constexpr int kKvLarge = 16;
 
 template <int P, int NT>
 __device__ __forceinline__ void kv_load_query(const KvAttParams& p, const KvItem& it, int lane, KvQuery<P, NT>& q) {
   const int g = lane >> 2, t = lane & 3;
   const int n_rows = it.q_len * p.G, past = it.kv_len - it.q_len;
+  q.large = false;
   q.all = it.kv_len;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -165,26 +173,26 @@ __device__ __forceinline__ void kv_load_query(const KvAttParams& p, const KvItem
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
     // 2^(9 - exponent of the largest element); a row of zeros, subnormals or infinities stays as it is
     const int e = (int)(__float_as_uint(top) >> 23) - 127;
-    const float f = (e > -118 && e < 128) ? __uint_as_float((uint32_t)(9 - e + 127) << 23) : 1.f;
-    float sum[P];
+    const bool scaled = e > -118 && e < 128;
+    const float f = scaled ? __uint_as_float((uint32_t)(9 - e + 127) << 23) : 1.f;
+    const float inv = scaled ? __uint_as_float((uint32_t)(e - 9 + 127) << 23) : 1.f;
+    // to the lanes that hold these rows' scores: rows 2 t, 2 t + 1 of the n-tile
+    q.fac[n] = pair_f32(__shfl_sync(0xffffffffu, inv, 8 * t), __shfl_sync(0xffffffffu, inv, 8 * t + 4));
+    q.large = q.large || (scaled && e >= kKvLarge);
 #pragma unroll
     for (int pl = 0; pl < P; ++pl) {
-      sum[pl] = 0.f;
+      float sum = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        sum[pl] += (x[pl][4 * j] + x[pl][4 * j + 1]) + (x[pl][4 * j + 2] + x[pl][4 * j + 3]);
-        q.b[n][pl][j][0] = pack_f16(x[pl][4 * j] * f, x[pl][4 * j + 1] * f);
-        q.b[n][pl][j][1] = pack_f16(x[pl][4 * j + 2] * f * 0.0625f, x[pl][4 * j + 3] * f * 0.0625f);
+        const float y[4] = {x[pl][4 * j] * f, x[pl][4 * j + 1] * f, x[pl][4 * j + 2] * f, x[pl][4 * j + 3] * f};
+        sum += (y[0] + y[1]) + (y[2] + y[3]);
+        q.b[n][pl][j][0] = pack_f16(y[0], y[1]);
+        q.b[n][pl][j][1] = pack_f16(y[2] * 0.0625f, y[3] * 0.0625f);
       }
-      sum[pl] += __shfl_xor_sync(0xffffffffu, sum[pl], 1);
-      sum[pl] += __shfl_xor_sync(0xffffffffu, sum[pl], 2);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      q.sum[pl][n] = pair_f32(__shfl_sync(0xffffffffu, sum, 8 * t), __shfl_sync(0xffffffffu, sum, 8 * t + 4));
     }
-    // to the lanes that hold these rows' scores: rows 2 t, 2 t + 1 of the n-tile
-    const float fac = p.scale_log2 * 0x1p24f / f;
-    q.fac[n] = pair_f32(__shfl_sync(0xffffffffu, fac, 8 * t), __shfl_sync(0xffffffffu, fac, 8 * t + 4));
-#pragma unroll
-    for (int pl = 0; pl < P; ++pl)
-      q.sum[pl][n] = pair_f32(__shfl_sync(0xffffffffu, sum[pl], 8 * t) * p.scale_log2, __shfl_sync(0xffffffffu, sum[pl], 8 * t + 4) * p.scale_log2);
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int r = it.row0 + 8 * n + 2 * t + c;
@@ -195,6 +203,14 @@ __device__ __forceinline__ void kv_load_query(const KvAttParams& p, const KvItem
   }
   q.all = min(q.all, __shfl_xor_sync(0xffffffffu, q.all, 1));
   q.all = min(q.all, __shfl_xor_sync(0xffffffffu, q.all, 2));
+  q.large = __any_sync(0xffffffffu, q.large);
+  const uint64_t up = twice_f32(p.scale_log2 * (q.large ? 0x1p-16f : 0x1p24f)), less = twice_f32(q.large ? 0x1p-16f : 1.f);
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+#pragma unroll
+    for (int pl = 0; pl < P; ++pl) q.sum[pl][n] = mul2(mul2(q.sum[pl][n], mul2(q.fac[n], less)), twice_f32(p.scale_log2));
+    q.fac[n] = mul2(q.fac[n], up);
+  }
 }
 
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
@@ -203,11 +219,10 @@ __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ uint64_t twice_f32(float v) { return pair_f32(v, v); }
 
 // U tiles of 16 tokens from shared memory, the first at key0; bit u of `there`: tile u is part of the warp's work.  `whole`: every
-// row sees every token.
-template <bool whole, int P, int NT, int U>
+// row sees every token.  `large`: of a warp with large queries.
+template <bool whole, bool large, int P, int NT, int U>
 __device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, int key0, int kv_len, const KvQuery<P, NT>& q, int lane, KvState<P, NT>& st) {
   constexpr uint32_t kLo = 0x000F000Fu, kHi = 0x00F000F0u;
   const int g = lane >> 2;
@@ -243,8 +258,15 @@ __device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, in
       for (int h = 0; h < 2; ++h) {
         const uint64_t ks = twice_f32(kv_scale(pk[h])), kz = twice_f32(kv_zero(pk[h]));
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-          s[u][n][h] = fma2(pair_f32(acc[n][2 * h], acc[n][2 * h + 1]), mul2(q.fac[n], ks), fma2(q.sum[pl][n], kz, pl == 0 ? st.m[n] : s[u][n][h]));
+        for (int n = 0; n < NT; ++n) {
+          uint64_t codes = pair_f32(acc[n][2 * h], acc[n][2 * h + 1]), before = pl == 0 ? st.m[n] : s[u][n][h];
+          if (large) {
+            codes = mul2(codes, twice_f32(0x1p24f));
+            if (pl == 0) before = mul2(before, twice_f32(0x1p-16f));
+          }
+          s[u][n][h] = fma2(codes, mul2(q.fac[n], ks), fma2(q.sum[pl][n], kz, before));
+          if (large && pl == P - 1) s[u][n][h] = mul2(s[u][n][h], twice_f32(0x1p16f));
+        }
       }
     }
 #pragma unroll
@@ -609,8 +631,15 @@ kv_attention_kernel(const KvAttParams p) {
       cp_async_commit();
       const int key0 = (tile0 + U * i) * kKvTile;
       const uint32_t there = have & ((1u << U) - 1);
-      if (there == (1u << U) - 1 && key0 + U * kKvTile <= q.all) kv_step<true, P, NT, U>(ring + use_at, there, key0, it.kv_len, q, lane, st);
-      else kv_step<false, P, NT, U>(ring + use_at, there, key0, it.kv_len, q, lane, st);
+      const bool all = there == (1u << U) - 1 && key0 + U * kKvTile <= q.all;
+      if (!q.large) {
+        if (all) kv_step<true, false, P, NT, U>(ring + use_at, there, key0, it.kv_len, q, lane, st);
+        else kv_step<false, false, P, NT, U>(ring + use_at, there, key0, it.kv_len, q, lane, st);
+      } else if (all) {
+        kv_step<true, true, P, NT, U>(ring + use_at, there, key0, it.kv_len, q, lane, st);
+      } else {
+        kv_step<false, true, P, NT, U>(ring + use_at, there, key0, it.kv_len, q, lane, st);
+      }
       use_at += kStep;
       if (use_at == kKvStages * kStep) use_at = 0;
     }
