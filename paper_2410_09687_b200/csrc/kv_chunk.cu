@@ -44,6 +44,7 @@ constexpr int kChLeast = 4;                  // of a share, at least
 constexpr int kChPitch = 64 + 4;             // floats of a row of a piece: sums, maximum, sum of weights
 constexpr int kChTmemCols = 256;
 constexpr float kChTop = 5.f, kChMost = 15.f;   // log2 of the largest weight after a move of the maximum, and at all
+constexpr float kChHuge = 0x1p20f;              // scores (powers of two) from which a step of fp32 is 2^-4 and more
 
 constexpr uint32_t kChIdesc = (1u << 4) | ((uint32_t)(64 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);   // D fp32, A and B fp16, 128 x 64
 constexpr uint32_t kChIdescHalf = (1u << 4) | ((uint32_t)(32 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);   // D 128 x 32
@@ -585,6 +586,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
           tc_fence_after();
         };
         bool done = false;
+        float base = ev;   // what the scores times c are to be added to
         // the maximum to what leaves 2^kChTop, the sums with it
         auto move = [&](float tm, bool grow) {
           const float m_new = grow ? tm - kChTop : m, corr = grow && !fresh ? ch_exp2(m - m_new) : 1.f;
@@ -608,7 +610,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
           uint32_t va[16], vb[16];
           // Weights against the maximum so far, the tile's own maximum beside them: groups of 16 keys, the next group's read in
           // flight, P in registers until the maximum is known to hold.  Else it moves, and the tile is taken again.
-          const uint64_t off2 = pair_f32(ev - m, ev - m), c2 = pair_f32(c, c);
+          const uint64_t off2 = pair_f32(base - m, base - m), c2 = pair_f32(c, c);
           uint64_t l2 = pair_f32(0.f, 0.f);
           float ma = -INFINITY, mc = -INFINITY;
           uint32_t w[2][16];
@@ -648,12 +650,27 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
           if (j * kChKeys + kChKeys - 1 <= it.first_pos) tile(false);
           else tile(true);
           if (!ok) break;
-          const float tm = fmaf(fmaxf(ma, mc), c, ev);
+          const float tm = fmaf(fmaxf(ma, mc), c, base);
           // too small for fp32 (the maximum comes from values 2^80 times this tile's), of keys whose 2^(s - m) still counts in the sum
           const bool grow = fresh ? tm > -INFINITY : tm > m + kChMost, small = !fresh && tm < m - 80.f && tm - ev > m - 60.f;
-          const uint32_t votes = (grow ? 1u : 0u) | (small ? 2u : 0u), vote = __reduce_or_sync(0xffffffffu, votes);
-          if (vote == 1u) {
-            move(tm, grow);
+          // so large that a product not rounded, less a maximum that is, may be anything: the row's scores are first taken less the largest
+          const bool huge = base == ev && fabsf(tm) > kChHuge && fabsf(tm) < INFINITY;
+          const uint32_t votes = (grow ? 1u : 0u) | (small ? 2u : 0u) | (huge ? 4u : 0u), vote = __reduce_or_sync(0xffffffffu, votes);
+          if (vote != 0u && !(vote & 2u)) {
+            if (vote & 4u) {
+              const float less = huge ? fmaxf(ma, mc) : 0.f;
+              if (huge) base = tm;
+#pragma unroll 1
+              for (int q = 0; q < 64; q += 16) {
+                tmem_ld16(s_addr + q, va);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) va[i] = __float_as_uint(__uint_as_float(va[i]) - less);
+                tmem_st16(s_addr + q, va);
+              }
+              tmem_st_wait();
+            }
+            if (vote & 1u) move(tm, grow);
             continue;
           }
           again = false;
@@ -668,7 +685,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
         if (ok && !done) lower();
         if (!ok) break;
-        if (!done) {   // one by one: unlike, hidden or NaN tokens, weights that are too small
+        if (!done) {   // one by one: unlike, hidden or NaN tokens, weights that are too small, scores that are huge
           const uint32_t hide = now.y & 0xFu;
           const float2* unlike = (now.y & kChUnlike) ? p.tok + (((size_t)it.req * p.kv.H + it.head) * p.tiles + j) * kChKeys : nullptr;
           uint32_t v[16];
@@ -681,11 +698,14 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const float2 tk = unlike != nullptr ? __ldg(unlike + 16 * k + i) : make_float2(__uint_as_float(now.x), ev);
-              if (16 * k + i <= seen) tm = fmaxf(tm, fmaf(__uint_as_float(v[i]), tk.x * fac, tk.y));
+              if (16 * k + i <= seen) tm = fmaxf(tm, __fmaf_rn(__uint_as_float(v[i]), tk.x * fac, tk.y));
             }
           }
           const bool grow = fresh ? tm > -INFINITY : tm > m + kChMost;
           if (__any_sync(0xffffffffu, grow)) move(tm, grow);
+          // Beyond kChHuge a step of the score's fp32 is whole powers of two: a weight is taken from the score as it was rounded for the
+          // maximum, so that the largest has its 2^kChTop whatever the rounding did.
+          const bool huge = fabsf(tm) > kChHuge && fabsf(tm) < INFINITY;
 #pragma unroll 1
           for (int k = 0; k < 4; ++k) {   // P of 16 keys into columns whose scores have been read
             uint32_t w[8];
@@ -697,7 +717,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
 #pragma unroll
               for (int b = 0; b < 2; ++b) {
                 const float2 tk = unlike != nullptr ? __ldg(unlike + 16 * k + i + b) : make_float2(__uint_as_float(now.x), ev);
-                const float pk = 16 * k + i + b <= seen && !(hide >> k & 1u) ? ch_exp2(fmaf(__uint_as_float(v[i + b]), tk.x * fac, -m)) : 0.f;
+                const float f = tk.x * fac, x = huge ? __fmaf_rn(__uint_as_float(v[i + b]), f, tk.y) - m - tk.y : fmaf(__uint_as_float(v[i + b]), f, -m);
+                const float pk = 16 * k + i + b <= seen && !(hide >> k & 1u) ? ch_exp2(x) : 0.f;
                 l += pk;
                 pr[b] = pk * ch_exp2(tk.y);
               }
