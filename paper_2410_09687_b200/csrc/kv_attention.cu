@@ -11,7 +11,10 @@
 // brings them into the middle of fp16: exact.  The weights p sv are the only operand that is rounded, to fp16 (2^-12
 // relative); their sums p are not.  To keep them inside fp16 whatever the scales are, m follows the maximum of s_t +
 // log2(sv_t): a weight is at most 2^15, and precise to 2^-24 of the row's largest.  m lags (a row is rescaled when a
-// weight would exceed 2^15, to 2^10), so most tiles need no reduction over the warp.
+// weight would exceed 2^15, to 2^10), so most tiles need no reduction over the warp.  A wide head's second plane has values, and so
+// scales, of its own: its weights are p sv 2^d with a d per row, so that they too are at most 2^15 and precise to 2^-24 of that
+// plane's largest.  (With one maximum for both, 64 wide requests took 46.4 us instead of 48.2, but of a plane 2^-24 and
+// less of the other only sum p zv was left.)
 //
 // Sums over many tokens are made by fp32 additions that round, not in the accumulator of the MMA, which truncates: codes are
 // positive, so the sum grows with every token while what is left of it after sum p zv shrinks with their number (131072 tokens
@@ -32,6 +35,7 @@ constexpr int kKvStages = 3;         // steps of a warp in shared memory
 constexpr int kKvItemCost = 8;       // what beginning an item costs, in tiles
 constexpr float kKvTop = 10.f;       // log2 of the largest weight after a rescale
 constexpr float kKvMost = 15.f;      // log2 of the largest weight at all
+constexpr float kKvApart = 100.f;    // d at most: planes further apart lose from the smaller one
 
 // Who takes what: a CTA an item; warps equal shares of all items; or, of one request, each of gridDim.x CTAs its part of each item.
 enum { KV_WHOLE = 0, KV_SHARES = 1, KV_CUT = 2 };
@@ -106,6 +110,7 @@ template <int P, int NT>
 struct KvState {            // a warp's share of an item: 8 NT rows, 64 P channels; pairs are rows 2 t, 2 t + 1 of an n-tile
   uint64_t o[NT][P][4][2];  // [channel block of 16][g, g + 8]
   uint64_t m[NT], l[NT], z[P][NT];   // m: negated
+  uint64_t d[NT];           // (P = 2) log2 of what the second plane's weights are multiplied with
   uint32_t fresh;           // bit 2 n + c: the row has seen no key yet (its m is 0 and means nothing)
 };
 
@@ -228,7 +233,7 @@ __device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, in
   const int g = lane >> 2;
   uint64_t s[U][NT][2];    // [token g, g + 8]: scores in powers of two, less the row's m
   uint32_t pv[U][P][2];
-  float lg[U][2];
+  float lg[U][P][2];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
 #pragma unroll
@@ -270,11 +275,9 @@ __device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, in
       }
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float sv = kv_scale(pv[u][0][h]);
-      if (P == 2) sv = fmaxf(sv, kv_scale(pv[u][P - 1][h]));
-      lg[u][h] = fmaxf(kv_log2(sv), -64.f);
-    }
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int pl = 0; pl < P; ++pl) lg[u][pl][h] = fmaxf(kv_log2(kv_scale(pv[u][pl][h])), -64.f);
     if (!whole) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -289,49 +292,67 @@ __device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, in
         }
     }
   }
-  float top[NT][2];
+  float top[NT][P][2];     // log2 of the rows' largest weights here
   bool grow = st.fresh != 0;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float a0, b0, a1, b1;
-      unpair_f32(s[u][n][0], a0, b0);
-      unpair_f32(s[u][n][1], a1, b1);
-      a0 += lg[u][0]; b0 += lg[u][0]; a1 += lg[u][1]; b1 += lg[u][1];
-      top[n][0] = u == 0 ? fmaxf(a0, a1) : fmax3(top[n][0], a0, a1);
-      top[n][1] = u == 0 ? fmaxf(b0, b1) : fmax3(top[n][1], b0, b1);
+    for (int pl = 0; pl < P; ++pl) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float a0, b0, a1, b1;
+        unpair_f32(s[u][n][0], a0, b0);
+        unpair_f32(s[u][n][1], a1, b1);
+        a0 += lg[u][pl][0]; b0 += lg[u][pl][0]; a1 += lg[u][pl][1]; b1 += lg[u][pl][1];
+        top[n][pl][0] = u == 0 ? fmaxf(a0, a1) : fmax3(top[n][pl][0], a0, a1);
+        top[n][pl][1] = u == 0 ? fmaxf(b0, b1) : fmax3(top[n][pl][1], b0, b1);
+      }
+      if (pl == 1) {
+        float d0, d1;
+        unpair_f32(st.d[n], d0, d1);
+        top[n][pl][0] += d0;
+        top[n][pl][1] += d1;
+      }
+      grow = grow || fmaxf(top[n][pl][0], top[n][pl][1]) > kKvMost;
     }
-    grow = grow || fmaxf(top[n][0], top[n][1]) > kKvMost;
   }
   if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      float up[2], corr[2];   // the new m is so much larger
-      float l[2];
+      float up[P][2], corr[P][2];   // by so much smaller are a plane's weights to become, in log2; the factor of its sums
+      float l[2], d[2];
       unpair_f32(st.l[n], l[0], l[1]);
+      if (P == 2) unpair_f32(st.d[n], d[0], d[1]);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        float mx = top[n][c];
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
         const uint32_t bit = 1u << (2 * n + c);
         const bool fresh = st.fresh & bit;      // (its sums are 0, or NaN for good)
-        up[c] = 0.f;
-        corr[c] = 1.f;
-        if (mx > (fresh ? -INFINITY : kKvMost)) {
-          up[c] = mx - kKvTop;
-          st.fresh &= ~bit;
-          if (!fresh) {
-            corr[c] = kv_exp2(-up[c]);
-            l[c] = kv_rescale_sum(l[c], -up[c]);
-          }
+        bool seen = false;
+#pragma unroll
+        for (int pl = 0; pl < P; ++pl) {
+          float mx = top[n][pl][c];
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+          const bool more = mx > (fresh ? -INFINITY : kKvMost);
+          up[pl][c] = more ? mx - kKvTop : 0.f;
+          seen = seen || more;
         }
+        if (P == 2) {   // p becomes smaller by up[0], what it is multiplied with for the second plane takes the rest
+          const float apart = d[c] + up[0][c] - up[P - 1][c];
+          if (apart > kKvApart) up[P - 1][c] += apart - kKvApart;
+          if (apart < -kKvApart) up[0][c] += -kKvApart - apart;
+          d[c] = fminf(fmaxf(apart, -kKvApart), kKvApart);
+        }
+#pragma unroll
+        for (int pl = 0; pl < P; ++pl) corr[pl][c] = fresh ? 1.f : kv_exp2(-up[pl][c]);
+        if (!fresh) l[c] = kv_rescale_sum(l[c], -up[0][c]);
+        if (seen) st.fresh &= ~bit;
       }
-      const uint64_t less = pair_f32(-up[0], -up[1]), f = pair_f32(corr[0], corr[1]);
+      const uint64_t less = pair_f32(-up[0][0], -up[0][1]), f = pair_f32(corr[0][0], corr[0][1]);
       st.m[n] = add2(st.m[n], less);
       st.l[n] = pair_f32(l[0], l[1]);
+      if (P == 2) st.d[n] = pair_f32(d[0], d[1]);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         s[u][n][0] = add2(s[u][n][0], less);
@@ -342,10 +363,20 @@ __device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, in
         st.z[pl][n] = mul2(st.z[pl][n], f);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          st.o[n][pl][j][0] = mul2(st.o[n][pl][j][0], f);
-          st.o[n][pl][j][1] = mul2(st.o[n][pl][j][1], f);
+          const uint64_t fo = pair_f32(corr[pl][0], corr[pl][1]);
+          st.o[n][pl][j][0] = mul2(st.o[n][pl][j][0], fo);
+          st.o[n][pl][j][1] = mul2(st.o[n][pl][j][1], fo);
         }
       }
+    }
+  }
+  uint64_t apart[NT];
+  if (P == 2) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float x, y;
+      unpair_f32(st.d[n], x, y);
+      apart[n] = pair_f32(kv_exp2(x), kv_exp2(y));
     }
   }
   uint32_t b[U][NT][P][2];
@@ -367,15 +398,16 @@ __device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, in
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           float x, y;
+          const uint64_t w = mul2(pl == 1 ? mul2(pr[n], apart[n]) : pr[n], sv);
           if (whole) {
             st.z[pl][n] = fma2(pr[n], zv, st.z[pl][n]);
-            unpair_f32(mul2(pr[n], sv), x, y);
+            unpair_f32(w, x, y);
           } else {   // a value that a row must not see may be NaN
             const int key = key0 + u * kKvTile + g + 8 * h;
             const bool out0 = !(there >> u & 1u) || key > q.last[n][0], out1 = !(there >> u & 1u) || key > q.last[n][1];
             float zx, zy;
             unpair_f32(mul2(pr[n], zv), zx, zy);
-            unpair_f32(mul2(pr[n], sv), x, y);
+            unpair_f32(w, x, y);
             x = out0 ? 0.f : x;
             y = out1 ? 0.f : y;
             st.z[pl][n] = add2(st.z[pl][n], pair_f32(out0 ? 0.f : zx, out1 ? 0.f : zy));
@@ -614,7 +646,7 @@ kv_attention_kernel(const KvAttParams p) {
     st.fresh = (1u << (2 * NT)) - 1;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      st.m[n] = st.l[n] = 0;
+      st.m[n] = st.l[n] = st.d[n] = 0;
 #pragma unroll
       for (int pl = 0; pl < P; ++pl) {
         st.z[pl][n] = 0;
@@ -649,8 +681,9 @@ kv_attention_kernel(const KvAttParams p) {
     float* rows = reinterpret_cast<float*>(ring + (inside ? kRing : 0));
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      float l[2], m[2], z[P][2];
+      float l[2], m[2], d[2], z[P][2];
       unpair_f32(st.l[n], l[0], l[1]);
+      if (P == 2) unpair_f32(st.d[n], d[0], d[1]);
       unpair_f32(st.m[n], m[0], m[1]);
 #pragma unroll
       for (int pl = 0; pl < P; ++pl) unpair_f32(st.z[pl][n], z[pl][0], z[pl][1]);
@@ -665,15 +698,17 @@ kv_attention_kernel(const KvAttParams p) {
         }
         if (g == 0) *reinterpret_cast<float2*>(row + kCh) = make_float2((st.fresh >> (2 * n + c) & 1u) ? -FLT_MAX : -m[c], l[c]);
 #pragma unroll
-        for (int pl = 0; pl < P; ++pl)
+        for (int pl = 0; pl < P; ++pl) {
+          const float back = pl == 1 ? kv_exp2(-d[c]) : 1.f;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             float x[2], y[2];
             unpair_f32(st.o[n][pl][j][0], x[0], x[1]);
             unpair_f32(st.o[n][pl][j][1], y[0], y[1]);
-            row[64 * pl + 16 * j + g] = fmaf(x[c], 0x1p24f, z[pl][c]);
-            row[64 * pl + 16 * j + 8 + g] = fmaf(y[c] - x[c], 0x1p20f, z[pl][c]);
+            row[64 * pl + 16 * j + g] = fmaf(x[c], back * 0x1p24f, z[pl][c]);
+            row[64 * pl + 16 * j + 8 + g] = fmaf(y[c] - x[c], back * 0x1p20f, z[pl][c]);
           }
+        }
       }
     }
     __syncwarp();

@@ -1,8 +1,9 @@
-"""Cached attention where its numbers are large, small or many."""
+"""Cached attention where its numbers are large, small or many.  Reference and bounds: tests/kv_exact.py, tests/kv_ref.py."""
 import numpy as np
 import pytest
 import torch
 
+import kv_exact as exact
 import kv_ref as ref
 import paper_2410_09687_b200 as moin
 from test_gpu_kv import DEV, _dev, _serve, i32
@@ -57,3 +58,31 @@ def test_queries_near_the_largest_number(D, new, beside, power, unlike, kernel):
         small[big] = 0
         alone = moin.kv_attention(cache, tables, _dev(small), *args)
         assert torch.equal(got[torch.from_numpy(~big).to(DEV)], alone[torch.from_numpy(~big).to(DEV)])
+
+
+def _wide(rng, n, H, powers, page=32):
+    """A request of n tokens whose value planes are multiplied with 2^powers[t][plane]."""
+    cache, tables, table, slot = _serve(rng, [n], H, 128, page)
+    k = ref.bf16(rng.standard_normal((n, H, 128)).astype(np.float32))
+    v = rng.standard_normal((n, H, 2, 64)) * 2.0 ** powers[:, None, :, None]
+    moin.kv_append(cache, i32(slot), _dev(k), _dev(ref.bf16(v.reshape(n, H, 128).astype(np.float32))))
+    return cache, tables, torch.from_numpy(np.asarray(slot)).to(DEV)
+
+
+@pytest.mark.parametrize("new,G,n", [(1, 4, 700), (3, 4, 700), (20, 2, 300), (1, 8, 5000)])
+@pytest.mark.parametrize("kind", ["first small", "second small", "far apart", "by token", "rising"])
+def test_planes_of_a_wide_head_hold_their_own_precision(kind, new, G, n):
+    """Value planes 2^30 to 2^90 apart, from the start, token by token, or drifting: each plane is right within bounds of its own size."""
+    rng = np.random.default_rng(new + G + len(kind))
+    t = np.arange(n)
+    powers = {"first small": np.stack([np.full(n, -30.0), np.zeros(n)], -1), "second small": np.stack([np.zeros(n), np.full(n, -45.0)], -1),
+              "far apart": np.stack([np.full(n, 45.0), np.full(n, -45.0)], -1), "by token": rng.integers(-25, 26, (n, 2)).astype(float),
+              "rising": np.stack([40.0 - 80.0 * t / n, -40.0 + 80.0 * t / n], -1)}[kind]
+    H = 2
+    cache, tables, slot = _wide(rng, n, H, np.round(powers))
+    q = _dev(ref.bf16(rng.standard_normal((new, H * G, 128)).astype(np.float32)))
+    pos = torch.arange(n - new, n, device=DEV)
+    want, tol = exact.attention(cache, slot, q, pos, 128 ** -0.5, False)
+    for max_kv in (n, 0):
+        got = moin.kv_attention(cache, tables, q, i32([0, new]), i32([n]), new, max_kv).double()
+        assert got.isfinite().all() and ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).max()
