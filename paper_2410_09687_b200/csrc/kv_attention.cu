@@ -24,6 +24,8 @@
 // row] with tokens along a lane's registers: one movmatrix per 8 x 8 block turns them.
 #include <float.h>
 
+#include <type_traits>
+
 #include "kv.cuh"
 #include "ptx.cuh"
 
@@ -127,7 +129,10 @@ struct KvQuery {
 // left fp32, and times signed sums gave NaN.  A warp with a query of 2^kKvLarge or more takes 2^24 into acc instead and holds
 // scores, factors and sums 2^-16 smaller until the score is complete: powers of two, so other rows' bits stay.  (Steps of their own:
 // the others pay nothing.)
+// These steps also take over where a row's maximum passes kKvCoarse: fp32 has no room for log2(sv) beside it then, so m is the
+// largest score alone, and the first plane's weights are p sv 2^e, as the second plane's are p sv 2^d.
 constexpr int kKvLarge = 16;
+constexpr float kKvCoarse = 0x1p20f;
 
 template <int P, int NT>
 __device__ __forceinline__ void kv_load_query(const KvAttParams& p, const KvItem& it, int lane, KvQuery<P, NT>& q) {
@@ -226,9 +231,11 @@ template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // U tiles of 16 tokens from shared memory, the first at key0; bit u of `there`: tile u is part of the warp's work.  `whole`: every
-// row sees every token.  `large`: of a warp with large queries.
+// row sees every token.  `large`: of a warp with large queries or scores; without it false is returned, and nothing is done, where it
+// has to be made with it.
 template <bool whole, bool large, int P, int NT, int U>
-__device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, int key0, int kv_len, const KvQuery<P, NT>& q, int lane, KvState<P, NT>& st) {
+__device__ __forceinline__ bool kv_step(const uint8_t* tiles, uint32_t there, int key0, int kv_len, const KvQuery<P, NT>& q, int lane, KvState<P, NT>& st,
+                                        uint64_t (&e)[NT]) {
   constexpr uint32_t kLo = 0x000F000Fu, kHi = 0x00F000F0u;
   const int g = lane >> 2;
   uint64_t s[U][NT][2];    // [token g, g + 8]: scores in powers of two, less the row's m
@@ -307,9 +314,9 @@ __device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, in
         top[n][pl][0] = u == 0 ? fmaxf(a0, a1) : fmax3(top[n][pl][0], a0, a1);
         top[n][pl][1] = u == 0 ? fmaxf(b0, b1) : fmax3(top[n][pl][1], b0, b1);
       }
-      if (pl == 1) {
+      if (pl == 1 || large) {
         float d0, d1;
-        unpair_f32(st.d[n], d0, d1);
+        unpair_f32(pl == 1 ? st.d[n] : e[n], d0, d1);
         top[n][pl][0] += d0;
         top[n][pl][1] += d1;
       }
@@ -317,9 +324,20 @@ __device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, in
     }
   }
   if (__any_sync(0xffffffffu, grow)) {
+    if (!large) {
+      bool coarse = false;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float m[2];
+        unpair_f32(st.m[n], m[0], m[1]);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) coarse = coarse || (top[n][0][c] > -INFINITY && fabsf(top[n][0][c] - m[c]) > kKvCoarse);
+      }
+      if (__any_sync(0xffffffffu, coarse)) return false;
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      float up[P][2], corr[P][2];   // by so much smaller are a plane's weights to become, in log2; the factor of its sums
+      float up[P][2], corr[P][2], zc[2];   // by so much smaller are a plane's weights to become, in log2; the factor of its sums, of sums of p zv
       float l[2], d[2];
       unpair_f32(st.l[n], l[0], l[1]);
       if (P == 2) unpair_f32(st.d[n], d[0], d[1]);
@@ -346,10 +364,48 @@ __device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, in
         }
 #pragma unroll
         for (int pl = 0; pl < P; ++pl) corr[pl][c] = fresh ? 1.f : kv_exp2(-up[pl][c]);
+        if (large) {
+          float m[2], was[2][2];
+          unpair_f32(st.m[n], m[0], m[1]);
+          unpair_f32(e[n], was[0][0], was[0][1]);
+          if (P == 2) unpair_f32(st.d[n], was[1][0], was[1][1]);
+          float most = -INFINITY, t[P];   // the row's largest score so far, largest weights here against it
+          auto score = [&](int u, int h) {
+            float x[2];
+            unpair_f32(s[u][n][h], x[0], x[1]);
+            return x[c];
+          };
+#pragma unroll
+          for (int u = 0; u < U; ++u) most = fmax3(most, score(u, 0), score(u, 1));
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+          if (!fresh) most = fmaxf(most, 0.f);
+#pragma unroll
+          for (int pl = 0; pl < P; ++pl) {
+            t[pl] = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < U; ++u) t[pl] = fmax3(t[pl], score(u, 0) - most + lg[u][pl][0], score(u, 1) - most + lg[u][pl][1]);
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) t[pl] = fmaxf(t[pl], __shfl_xor_sync(0xffffffffu, t[pl], o));
+          }
+          const bool coarse = fabsf(most - m[c]) > kKvCoarse;
+          if (seen && (coarse || was[0][c] != 0.f)) {
+            up[0][c] = coarse ? most : most + (t[0] - kKvTop);
+            float now[P];
+#pragma unroll
+            for (int pl = 0; pl < P; ++pl) {
+              now[pl] = fminf(fmaxf((coarse ? kKvTop : t[0]) - t[pl], -kKvApart), kKvApart);
+              if (!fresh) corr[pl][c] = kv_exp2(now[pl] - was[pl][c] - up[0][c]);
+            }
+            e[n] = c == 0 ? pair_f32(now[0], was[0][1]) : pair_f32(was[0][0], now[0]);
+            if (P == 2) d[c] = now[P - 1];
+          }
+        }
+        zc[c] = !large ? corr[0][c] : fresh ? 1.f : kv_exp2(-up[0][c]);
         if (!fresh) l[c] = kv_rescale_sum(l[c], -up[0][c]);
         if (seen) st.fresh &= ~bit;
       }
-      const uint64_t less = pair_f32(-up[0][0], -up[0][1]), f = pair_f32(corr[0][0], corr[0][1]);
+      const uint64_t less = pair_f32(-up[0][0], -up[0][1]), f = pair_f32(zc[0], zc[1]);
       st.m[n] = add2(st.m[n], less);
       st.l[n] = pair_f32(l[0], l[1]);
       if (P == 2) st.d[n] = pair_f32(d[0], d[1]);
@@ -370,15 +426,15 @@ __device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, in
       }
     }
   }
-  uint64_t apart[NT];
-  if (P == 2) {
+  uint64_t apart[P][NT];
+#pragma unroll
+  for (int pl = large ? 0 : 1; pl < P; ++pl)
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       float x, y;
-      unpair_f32(st.d[n], x, y);
-      apart[n] = pair_f32(kv_exp2(x), kv_exp2(y));
+      unpair_f32(pl == 1 ? st.d[n] : e[n], x, y);
+      apart[pl][n] = pair_f32(kv_exp2(x), kv_exp2(y));
     }
-  }
   uint32_t b[U][NT][P][2];
 #pragma unroll
   for (int u = 0; u < U; ++u)
@@ -398,7 +454,7 @@ __device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, in
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           float x, y;
-          const uint64_t w = mul2(pl == 1 ? mul2(pr[n], apart[n]) : pr[n], sv);
+          const uint64_t w = mul2(pl == 1 || large ? mul2(pr[n], apart[pl][n]) : pr[n], sv);
           if (whole) {
             st.z[pl][n] = fma2(pr[n], zv, st.z[pl][n]);
             unpair_f32(w, x, y);
@@ -440,6 +496,7 @@ __device__ __forceinline__ void kv_step(const uint8_t* tiles, uint32_t there, in
       }
     }
   }
+  return true;
 }
 
 // What a request counts for an item: its tiles and the cost of beginning.  Items without tiles are there too: their rows are written.
@@ -654,26 +711,53 @@ kv_attention_kernel(const KvAttParams p) {
         for (int j = 0; j < 4; ++j) st.o[n][pl][j][0] = st.o[n][pl][j][1] = 0;
       }
     }
-#pragma unroll 1
-    for (int i = 0; i < n_steps; ++i) {
+    uint64_t e[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) e[n] = 0;
+    auto begin = [&](int i) {
       have >>= 4;
       cp_async_wait<kKvStages - 2>();
       __syncwarp();   // this step's tiles are there for every lane; the stage filled now was read a step ago
       if (i + kKvStages - 1 < n_steps) fill(i + kKvStages - 1);
       cp_async_commit();
+    };
+    auto step = [&](auto large, int i) -> bool {
       const int key0 = (tile0 + U * i) * kKvTile;
       const uint32_t there = have & ((1u << U) - 1);
-      const bool all = there == (1u << U) - 1 && key0 + U * kKvTile <= q.all;
-      if (!q.large) {
-        if (all) kv_step<true, false, P, NT, U>(ring + use_at, there, key0, it.kv_len, q, lane, st);
-        else kv_step<false, false, P, NT, U>(ring + use_at, there, key0, it.kv_len, q, lane, st);
-      } else if (all) {
-        kv_step<true, true, P, NT, U>(ring + use_at, there, key0, it.kv_len, q, lane, st);
+      if (there == (1u << U) - 1 && key0 + U * kKvTile <= q.all) {
+        if (!kv_step<true, decltype(large)::value, P, NT, U>(ring + use_at, there, key0, it.kv_len, q, lane, st, e)) return false;
       } else {
-        kv_step<false, true, P, NT, U>(ring + use_at, there, key0, it.kv_len, q, lane, st);
+        if (!kv_step<false, decltype(large)::value, P, NT, U>(ring + use_at, there, key0, it.kv_len, q, lane, st, e)) return false;
       }
       use_at += kStep;
       if (use_at == kKvStages * kStep) use_at = 0;
+      return true;
+    };
+    int i = 0;
+    bool begun = false;
+    if (!q.large) {
+#pragma unroll 1
+      for (; i < n_steps; ++i) {
+        begin(i);
+        if (!step(std::false_type(), i)) {
+          begun = true;
+          break;
+        }
+      }
+      if (begun) {   // (as kv_load_query leaves them for large queries)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          q.fac[n] = mul2(q.fac[n], twice_f32(0x1p-40f));
+#pragma unroll
+          for (int pl = 0; pl < P; ++pl) q.sum[pl][n] = mul2(q.sum[pl][n], twice_f32(0x1p-16f));
+        }
+      }
+    }
+#pragma unroll 1
+    for (; i < n_steps; ++i) {
+      if (!begun) begin(i);
+      begun = false;
+      step(std::true_type(), i);
     }
     // ---- the rows to shared memory: the ring is idle, a piece to be joined with the warp before has its own place
     __syncwarp();
@@ -681,9 +765,10 @@ kv_attention_kernel(const KvAttParams p) {
     float* rows = reinterpret_cast<float*>(ring + (inside ? kRing : 0));
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      float l[2], m[2], d[2], z[P][2];
+      float l[2], m[2], d[P][2], z[P][2];
       unpair_f32(st.l[n], l[0], l[1]);
-      if (P == 2) unpair_f32(st.d[n], d[0], d[1]);
+      unpair_f32(e[n], d[0][0], d[0][1]);
+      if (P == 2) unpair_f32(st.d[n], d[P - 1][0], d[P - 1][1]);
       unpair_f32(st.m[n], m[0], m[1]);
 #pragma unroll
       for (int pl = 0; pl < P; ++pl) unpair_f32(st.z[pl][n], z[pl][0], z[pl][1]);
@@ -699,7 +784,7 @@ kv_attention_kernel(const KvAttParams p) {
         if (g == 0) *reinterpret_cast<float2*>(row + kCh) = make_float2((st.fresh >> (2 * n + c) & 1u) ? -FLT_MAX : -m[c], l[c]);
 #pragma unroll
         for (int pl = 0; pl < P; ++pl) {
-          const float back = pl == 1 ? kv_exp2(-d[c]) : 1.f;
+          const float back = kv_exp2(-d[pl][c]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             float x[2], y[2];

@@ -18,15 +18,13 @@ def kernel(request):
     moin.set_option(moin.OPT_GEMM_IMPL, 0)
 
 
-@pytest.mark.parametrize("unlike", [False, True])
+@pytest.mark.parametrize("unlike", [0, -30, 20, 60])
 @pytest.mark.parametrize("D,new,beside", [(64, 1, False), (64, 5, False), (64, 70, True), (128, 1, False), (128, 9, True)])
 @pytest.mark.parametrize("power", [20, 24, 27, 30, 60, 100, 116, 120])
 def test_queries_near_the_largest_number(D, new, beside, power, unlike, kernel):
     """Queries of 2^20 to 2^120 against keys a_t u: the token with the largest a_t takes all weight, so the result is its value (half a
     bf16 step, and half an fp16 step of what its weight multiplies, or of weight and value where both are in fp16).  Ordinary
-    queries beside them give the same bits as alone, but where tokens of unlike sizes (every seventh value 2^30 smaller) are taken one by one."""
-    if unlike and (kernel == "rows" or D == 128):
-        pytest.skip("values of unlike sizes: the kernel of long chunks")
+    queries beside them give the same bits as alone, but where tokens of unlike sizes (every seventh value 2^unlike times the others) are taken one by one."""
     rng = np.random.default_rng(power + D)
     n, H, G, page = 200, 2, 4, 16
     cache, tables, table, slot = _serve(rng, [n], H, D, page)
@@ -36,7 +34,7 @@ def test_queries_near_the_largest_number(D, new, beside, power, unlike, kernel):
     k = ref.bf16((a[:, None, None] * u).astype(np.float32)) * np.ones((1, H, 1), np.float32)
     v = ref.bf16(rng.standard_normal((n, H, D)).astype(np.float32))
     if unlike:
-        v[::7] *= np.float32(2.0 ** -30)
+        v[::7] *= np.float32(2.0 ** unlike)
     moin.kv_append(cache, i32(slot), _dev(k), _dev(v))
     sign = np.where(np.arange(new * H * G).reshape(new, H * G) % 3 == 0, -1.0, 1.0)
     q = ref.bf16((2.0 ** power * sign[..., None] * u).astype(np.float32))
@@ -86,3 +84,34 @@ def test_planes_of_a_wide_head_hold_their_own_precision(kind, new, G, n):
     for max_kv in (n, 0):
         got = moin.kv_attention(cache, tables, q, i32([0, new]), i32([n]), new, max_kv).double()
         assert got.isfinite().all() and ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).max()
+
+
+@pytest.mark.parametrize("D,H,G,new,n", [(64, 2, 8, 1, 700), (64, 1, 4, 9, 300), (128, 2, 4, 1, 500), (128, 1, 2, 20, 200), (64, 1, 8, 1, 40000)])
+@pytest.mark.parametrize("size", [4, 30, 90])
+def test_scores_that_jump_by_more_than_fp32_can_add(D, H, G, new, n, size, kernel):
+    """Keys of 2^size, of either sign, between ordinary ones: scores rise and fall by 2^size from tile to tile, values' sizes too.  The
+    largest keys take all weight, to the last ones of them that a query sees; queries of the other sign see the smallest."""
+    if kernel == "tcgen05" and size > 4:
+        size -= 20
+    rng = np.random.default_rng(size + n + D)
+    cache, tables, _, slot = _serve(rng, [n], H, D, 32)
+    u = rng.choice([-1.0, 1.0], D)
+    a = rng.uniform(-1, 1, n)
+    big = rng.permutation(n - new)[:9]
+    a[big[:4]], a[big[4:8]] = 2.0 ** size * np.array([1, 1.5, 0.5, 1.25]), -2.0 ** size * np.array([1, 1.5, 0.5, 1.25])
+    k = ref.bf16((a[:, None, None] * u).astype(np.float32)) * np.ones((1, H, 1), np.float32)
+    v = ref.bf16((rng.standard_normal((n, H, D)) * 2.0 ** rng.integers(-12, 13, (n, 1, 1))).astype(np.float32))
+    moin.kv_append(cache, i32(slot), _dev(k), _dev(v))
+    sign = np.where(np.arange(new * H * G).reshape(new, H * G) % 2 == 0, 64.0, -64.0)
+    q = ref.bf16((sign[..., None] * u).astype(np.float32))
+    got = moin.kv_attention(cache, tables, _dev(q), i32([0, new]), i32([n]), new, n).double().cpu().numpy()
+    if size == 4:   # ordinary scores: against the formula
+        want, tol = exact.attention(cache, torch.from_numpy(np.asarray(slot)).to(DEV), _dev(q), torch.arange(n - new, n, device=DEV), D ** -0.5, kernel == "tcgen05" and D == 64)
+        assert (np.abs(got - want.cpu().numpy()) <= tol.cpu().numpy()).all()
+        return
+    at = np.where(sign > 0, big[1], big[5])
+    c, s, z = ref.load(cache.pages.cpu().numpy(), np.asarray(slot), 1)
+    val, part = (z[..., None] + s[..., None] * c).reshape(n, H, D), (s[..., None] * c).reshape(n, H, D)
+    head = (np.arange(H * G) // G)[None]
+    want = val[at, head]
+    assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * (np.abs(want) + part[at, head]) + 2.0 ** -30 * np.abs(val[at, head]).max(-1, keepdims=True)).all()
