@@ -44,6 +44,11 @@ constexpr int kChLeast = 4;                  // of a share, at least
 constexpr int kChPitch = 64 + 4;             // floats of a row of a piece: sums, maximum, sum of weights
 constexpr int kChTmemCols = 256;
 constexpr float kChTop = 5.f, kChMost = 15.f;   // log2 of the largest weight after a move of the maximum, and at all
+// The tensor core's accumulator truncates: over a chain of n keys a sum loses about n 2^-28 of itself, always the same way (measured:
+// behind 2^19 keys, 2^18 a stream, 2^-9.9 of every value, where rounding to bf16 is 2^-9.3 in the mean square).  Behind kChFlush tiles
+// of a stream the sum goes into memory, by fp32 additions, and a new one begins.
+constexpr int kChFlush = 512;                   // a power of two
+constexpr int kChKeep = 17;                     // float4 of a row there: sums, the maximum that they are taken against
 constexpr float kChHuge = 0x1p20f;              // scores (powers of two) from which a step of fp32 is 2^-4 and more
 
 constexpr uint32_t kChIdesc = (1u << 4) | ((uint32_t)(64 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);   // D fp32, A and B fp16, 128 x 64
@@ -69,6 +74,7 @@ struct ChunkParams {
   int dense_blocks, workers;
   int4* share;              // [worker]: (row block of a request, head, what of that item is passed) where its share begins, its size
   float* part;              // [worker][2][128][kChPitch]: pieces of items, in slot 1 of one that begins here without ending, else in slot 0
+  float4* keep;             // [worker][stream][kChKeep][128]: sums of the tiles before (kChFlush)
   int4* desc;               // [worker][2]: the item that it begins without ending it, as kv_join_kernel takes it
   DeviceStatus* status;
 };
@@ -520,7 +526,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     }
     while (ok && at.have) {
       const uint32_t s = i & 1u, ph = (i >> 1) & 1u;
-      const uint32_t first = at.j == h ? 0u : 1u, item = at.item;
+      const uint32_t first = at.j == h ? 0u : 1u, more = (at.j >> 1) & (kChFlush - 1) ? 1u : 0u, item = at.item;
       // The next tile's scores: the upper 32 keys' columns are free since P is there, the lower ones' hold P.  Those of another item
       // come behind the product, for which its queries may wait.
       const bool same = at.j + 2 < at.it.n;
@@ -537,7 +543,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       if (leader) {
         const uint64_t dv = sdesc_k128(sv + s * kChKV);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) tc_mma_bf16_ta(tm + 128 + h * 64, tm + h * 64 + 8 * k, dv + kChVStep * k, kChIdescPV, k > 0 ? 1u : first);
+        for (int k = 0; k < 4; ++k) tc_mma_bf16_ta(tm + 128 + h * 64, tm + h * 64 + 8 * k, dv + kChVStep * k, kChIdescPV, k > 0 ? 1u : more);
         tc_commit(pvdone + 8 * h);
       }
       if (!same) {
@@ -573,169 +579,205 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       float m = 0.f, l = 0.f;   // maximum (powers of two), sum of 2^(s - m)
       bool fresh = true;        // no key seen yet: m means nothing
       const int j_end = it.j0 + it.n;
-      uint2 at = half < it.n ? __ldg(reinterpret_cast<const uint2*>(info + it.j0 + half)) : make_uint2(0u, 0u);
-      for (int j = it.j0 + half; j < j_end && ok; j += 2, ++n_s) {
-        const uint2 now = at;
-        if (j + 2 < j_end) at = __ldg(reinterpret_cast<const uint2*>(info + j + 2));
-        const float c = __uint_as_float(now.x) * fac, ev = __uint_as_float(now.y & ~kChFlags);
-        const int seen = pos - j * kChKeys;   // the last key of the tile that the row sees
-        if (!(ok = mbar_wait_warp(supper + 8 * half, n_s & 1u, abort_flag, p.status, 66))) break;
-        tc_fence_after();
-        auto lower = [&] {   // the scores of the lower 32 keys: complete (and with them the product before)
-          ok = mbar_wait_warp(sready + 8 * half, n_s & 1u, abort_flag, p.status, 68);
-          tc_fence_after();
-        };
-        bool done = false;
-        float base = ev;   // what the scores times c are to be added to
-        // the maximum to what leaves 2^kChTop, the sums with it
-        auto move = [&](float tm, bool grow) {
-          const float m_new = grow ? tm - kChTop : m, corr = grow && !fresh ? ch_exp2(m - m_new) : 1.f;
-          if (grow && !fresh) l = ch_rescale(l, m - m_new);
-          m = m_new;
-          fresh = fresh && !grow;
-          if (j != it.j0 + half) {   // (these scores exist only because the product before is complete)
+      // The sums so far to memory, added to what is there already, all against the present maximum.
+      auto flush = [&](bool begun) {
+        float4* keep = p.keep + (size_t)(blockIdx.x * 2 + half) * kChKeep * kChRows + row;
+        const float corr = begun ? ch_exp2(keep[16 * kChRows].x - m) : 0.f;
 #pragma unroll 1
-            for (int q = 0; q < 64; q += 16) {
-              uint32_t o[16];
-              tmem_ld16(s_addr + 128 + q, o);
-              tmem_ld_wait();
+        for (int q = 0; q < 16; q += 4) {
+          uint32_t o[16];
+          tmem_ld16(s_addr + 128 + 4 * q, o);
+          tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
-              tmem_st16(s_addr + 128 + q, o);
+          for (int i = 0; i < 4; ++i) {
+            float4 v = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
+            float4* at = keep + (q + i) * kChRows;
+            if (begun) {
+              const float4 b = *at;
+              v = make_float4(fmaf(b.x, corr, v.x), fmaf(b.y, corr, v.y), fmaf(b.z, corr, v.z), fmaf(b.w, corr, v.w));
             }
+            *at = v;
           }
-        };
-#pragma unroll 1
-        for (bool again = (now.y & kChFlags) == 0u; again;) {
-          uint32_t va[16], vb[16];
-          // Weights against the maximum so far, the tile's own maximum beside them: groups of 16 keys, the next group's read in
-          // flight, P in registers until the maximum is known to hold.  Else it moves, and the tile is taken again.
-          const uint64_t off2 = pair_f32(base - m, base - m), c2 = pair_f32(c, c);
-          uint64_t l2 = pair_f32(0.f, 0.f);
-          float ma = -INFINITY, mc = -INFINITY;
-          uint32_t w[2][16];
-          auto group = [&](const uint32_t (&v)[16], int k, bool masked) {
-            auto out = [&](int i) { return masked && 16 * k + i > seen; };
-            auto x = [&](int i) { return out(i) ? -INFINITY : __uint_as_float(v[i]); };
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-              ma = fmax3(ma, x(i), x(i + 1));
-              mc = fmax3(mc, x(i + 2), x(i + 3));
-            }
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-              float x0, x1;
-              unpair_f32(fma2(pair_f32(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), c2, off2), x0, x1);
-              const float p0 = out(i) ? 0.f : ch_exp2(x0), p1 = out(i + 1) ? 0.f : ch_exp2(x1);   // (c may be 0: not by scores of -inf)
-              l2 = add2(l2, pair_f32(p0, p1));
-              const __half2 h2 = __floats2half2_rn(p0, p1);
-              w[k >> 1][8 * (k & 1) + (i >> 1)] = *reinterpret_cast<const uint32_t*>(&h2);
-            }
+        }
+        keep[16 * kChRows].x = fresh ? -FLT_MAX : m;
+      };
+      uint2 at = half < it.n ? __ldg(reinterpret_cast<const uint2*>(info + it.j0 + half)) : make_uint2(0u, 0u);
+      for (int j = it.j0 + half, stop = min(j_end, j + 2 * kChFlush);; stop = min(j_end, j + 2 * kChFlush)) {
+        for (; j < stop && ok; j += 2, ++n_s) {
+          const uint2 now = at;
+          if (j + 2 < j_end) at = __ldg(reinterpret_cast<const uint2*>(info + j + 2));
+          const float c = __uint_as_float(now.x) * fac, ev = __uint_as_float(now.y & ~kChFlags);
+          const int seen = pos - j * kChKeys;   // the last key of the tile that the row sees
+          if (!(ok = mbar_wait_warp(supper + 8 * half, n_s & 1u, abort_flag, p.status, 66))) break;
+          tc_fence_after();
+          auto lower = [&] {   // the scores of the lower 32 keys: complete (and with them the product before)
+            ok = mbar_wait_warp(sready + 8 * half, n_s & 1u, abort_flag, p.status, 68);
+            tc_fence_after();
           };
-          auto tile = [&](bool masked) {
-            tmem_ld16(s_addr + 32, va);
-            tmem_ld_wait();
-            tmem_ld16(s_addr + 48, vb);
-            group(va, 2, masked);
-            tmem_ld_wait();
-            group(vb, 3, masked);
-            lower();
-            tmem_ld16(s_addr, va);
-            tmem_ld_wait();
-            tmem_ld16(s_addr + 16, vb);
-            group(va, 0, masked);
-            tmem_ld_wait();
-            group(vb, 1, masked);
-          };
-          if (j * kChKeys + kChKeys - 1 <= it.first_pos) tile(false);
-          else tile(true);
-          if (!ok) break;
-          const float tm = fmaf(fmaxf(ma, mc), c, base);
-          // too small for fp32 (the maximum comes from values 2^80 times this tile's), of keys whose 2^(s - m) still counts in the sum
-          const bool grow = fresh ? tm > -INFINITY : tm > m + kChMost, small = !fresh && tm < m - 80.f && tm - ev > m - 60.f;
-          // so large that a product not rounded, less a maximum that is, may be anything: the row's scores are first taken less the largest
-          const bool huge = base == ev && fabsf(tm) > kChHuge && fabsf(tm) < INFINITY;
-          const uint32_t votes = (grow ? 1u : 0u) | (small ? 2u : 0u) | (huge ? 4u : 0u), vote = __reduce_or_sync(0xffffffffu, votes);
-          if (vote != 0u && !(vote & 2u)) {
-            if (vote & 4u) {
-              const float less = huge ? fmaxf(ma, mc) : 0.f;
-              if (huge) base = tm;
+          bool done = false;
+          float base = ev;   // what the scores times c are to be added to
+          // the maximum to what leaves 2^kChTop, the sums with it
+          auto move = [&](float tm, bool grow) {
+            const float m_new = grow ? tm - kChTop : m, corr = grow && !fresh ? ch_exp2(m - m_new) : 1.f;
+            if (grow && !fresh) l = ch_rescale(l, m - m_new);
+            m = m_new;
+            fresh = fresh && !grow;
+            if (j != it.j0 + half) {   // (these scores exist only because the product before is complete)
 #pragma unroll 1
               for (int q = 0; q < 64; q += 16) {
-                tmem_ld16(s_addr + q, va);
+                uint32_t o[16];
+                tmem_ld16(s_addr + 128 + q, o);
                 tmem_ld_wait();
 #pragma unroll
-                for (int i = 0; i < 16; ++i) va[i] = __float_as_uint(__uint_as_float(va[i]) - less);
-                tmem_st16(s_addr + q, va);
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
+                tmem_st16(s_addr + 128 + q, o);
               }
-              tmem_st_wait();
             }
-            if (vote & 1u) move(tm, grow);
-            continue;
+          };
+#pragma unroll 1
+          for (bool again = (now.y & kChFlags) == 0u; again;) {
+            uint32_t va[16], vb[16];
+            // Weights against the maximum so far, the tile's own maximum beside them: groups of 16 keys, the next group's read in
+            // flight, P in registers until the maximum is known to hold.  Else it moves, and the tile is taken again.
+            const uint64_t off2 = pair_f32(base - m, base - m), c2 = pair_f32(c, c);
+            uint64_t l2 = pair_f32(0.f, 0.f);
+            float ma = -INFINITY, mc = -INFINITY;
+            uint32_t w[2][16];
+            auto group = [&](const uint32_t (&v)[16], int k, bool masked) {
+              auto out = [&](int i) { return masked && 16 * k + i > seen; };
+              auto x = [&](int i) { return out(i) ? -INFINITY : __uint_as_float(v[i]); };
+#pragma unroll
+              for (int i = 0; i < 16; i += 4) {
+                ma = fmax3(ma, x(i), x(i + 1));
+                mc = fmax3(mc, x(i + 2), x(i + 3));
+              }
+#pragma unroll
+              for (int i = 0; i < 16; i += 2) {
+                float x0, x1;
+                unpair_f32(fma2(pair_f32(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), c2, off2), x0, x1);
+                const float p0 = out(i) ? 0.f : ch_exp2(x0), p1 = out(i + 1) ? 0.f : ch_exp2(x1);   // (c may be 0: not by scores of -inf)
+                l2 = add2(l2, pair_f32(p0, p1));
+                const __half2 h2 = __floats2half2_rn(p0, p1);
+                w[k >> 1][8 * (k & 1) + (i >> 1)] = *reinterpret_cast<const uint32_t*>(&h2);
+              }
+            };
+            auto tile = [&](bool masked) {
+              tmem_ld16(s_addr + 32, va);
+              tmem_ld_wait();
+              tmem_ld16(s_addr + 48, vb);
+              group(va, 2, masked);
+              tmem_ld_wait();
+              group(vb, 3, masked);
+              lower();
+              tmem_ld16(s_addr, va);
+              tmem_ld_wait();
+              tmem_ld16(s_addr + 16, vb);
+              group(va, 0, masked);
+              tmem_ld_wait();
+              group(vb, 1, masked);
+            };
+            if (j * kChKeys + kChKeys - 1 <= it.first_pos) tile(false);
+            else tile(true);
+            if (!ok) break;
+            const float tm = fmaf(fmaxf(ma, mc), c, base);
+            // too small for fp32 (the maximum comes from values 2^80 times this tile's), of keys whose 2^(s - m) still counts in the sum
+            const bool grow = fresh ? tm > -INFINITY : tm > m + kChMost, small = !fresh && tm < m - 80.f && tm - ev > m - 60.f;
+            // so large that a product not rounded, less a maximum that is, may be anything: the row's scores are first taken less the largest
+            const bool huge = base == ev && fabsf(tm) > kChHuge && fabsf(tm) < INFINITY;
+            const uint32_t votes = (grow ? 1u : 0u) | (small ? 2u : 0u) | (huge ? 4u : 0u), vote = __reduce_or_sync(0xffffffffu, votes);
+            if (vote != 0u && !(vote & 2u)) {
+              if (vote & 4u) {
+                const float less = huge ? fmaxf(ma, mc) : 0.f;
+                if (huge) base = tm;
+#pragma unroll 1
+                for (int q = 0; q < 64; q += 16) {
+                  tmem_ld16(s_addr + q, va);
+                  tmem_ld_wait();
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) va[i] = __float_as_uint(__uint_as_float(va[i]) - less);
+                  tmem_st16(s_addr + q, va);
+                }
+                tmem_st_wait();
+              }
+              if (vote & 1u) move(tm, grow);
+              continue;
+            }
+            again = false;
+            if (vote == 0u) {
+              tmem_st16(s_addr, w[0]);
+              tmem_st16(s_addr + 16, w[1]);
+              float la, lb;
+              unpair_f32(l2, la, lb);
+              l = fmaf(la + lb, ch_exp2(-ev), l);
+              done = true;
+            }
           }
-          again = false;
-          if (vote == 0u) {
-            tmem_st16(s_addr, w[0]);
-            tmem_st16(s_addr + 16, w[1]);
-            float la, lb;
-            unpair_f32(l2, la, lb);
-            l = fmaf(la + lb, ch_exp2(-ev), l);
-            done = true;
+          if (ok && !done) lower();
+          if (!ok) break;
+          if (!done) {   // one by one: unlike, hidden or NaN tokens, weights that are too small, scores that are huge
+            const uint32_t hide = now.y & 0xFu;
+            const float2* unlike = (now.y & kChUnlike) ? p.tok + (((size_t)it.req * p.kv.H + it.head) * p.tiles + j) * kChKeys : nullptr;
+            uint32_t v[16];
+            float tm = -INFINITY;
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {
+              tmem_ld16(s_addr + 16 * k, v);
+              tmem_ld_wait();
+              if (hide >> k & 1u) continue;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const float2 tk = unlike != nullptr ? __ldg(unlike + 16 * k + i) : make_float2(__uint_as_float(now.x), ev);
+                if (16 * k + i <= seen) tm = fmaxf(tm, __fmaf_rn(__uint_as_float(v[i]), tk.x * fac, tk.y));
+              }
+            }
+            const bool grow = fresh ? tm > -INFINITY : tm > m + kChMost;
+            if (__any_sync(0xffffffffu, grow)) move(tm, grow);
+            // Beyond kChHuge a step of the score's fp32 is whole powers of two: a weight is taken from the score as it was rounded for the
+            // maximum, so that the largest has its 2^kChTop whatever the rounding did.
+            const bool huge = fabsf(tm) > kChHuge && fabsf(tm) < INFINITY;
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {   // P of 16 keys into columns whose scores have been read
+              uint32_t w[8];
+              tmem_ld16(s_addr + 16 * k, v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; i += 2) {
+                float pr[2];
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                  const float2 tk = unlike != nullptr ? __ldg(unlike + 16 * k + i + b) : make_float2(__uint_as_float(now.x), ev);
+                  const float f = tk.x * fac, x = huge ? __fmaf_rn(__uint_as_float(v[i + b]), f, tk.y) - m - tk.y : fmaf(__uint_as_float(v[i + b]), f, -m);
+                  const float pk = 16 * k + i + b <= seen && !(hide >> k & 1u) ? ch_exp2(x) : 0.f;
+                  l += pk;
+                  pr[b] = pk * ch_exp2(tk.y);
+                }
+                const __half2 h2 = __floats2half2_rn(pr[0], pr[1]);
+                w[i >> 1] = *reinterpret_cast<const uint32_t*>(&h2);
+              }
+              tmem_st8(s_addr + 8 * k, w);
+            }
+            if (now.y & kChNan) {   // tokens stored as NaN: for the rows that see one
+              const uint2 bad = __ldg(reinterpret_cast<const uint2*>(info + j) + 1);
+              const unsigned long long mask = (unsigned long long)bad.y << 32 | bad.x;
+              if (seen >= 0 && (mask & (seen >= 63 ? ~0ull : (1ull << (seen + 1)) - 1ull))) l = NAN;
+            }
           }
+          tmem_st_wait();
+          tc_fence_before();
+          mbar_arrive(pready + 8 * half);
         }
-        if (ok && !done) lower();
+        if (!ok || j >= j_end) break;
+        // the next tile's product begins a new sum; its scores exist only because the product before is complete
+        ok = mbar_wait_warp(sready + 8 * half, n_s & 1u, abort_flag, p.status, 68);
+        tc_fence_after();
         if (!ok) break;
-        if (!done) {   // one by one: unlike, hidden or NaN tokens, weights that are too small, scores that are huge
-          const uint32_t hide = now.y & 0xFu;
-          const float2* unlike = (now.y & kChUnlike) ? p.tok + (((size_t)it.req * p.kv.H + it.head) * p.tiles + j) * kChKeys : nullptr;
-          uint32_t v[16];
-          float tm = -INFINITY;
-#pragma unroll 1
-          for (int k = 0; k < 4; ++k) {
-            tmem_ld16(s_addr + 16 * k, v);
-            tmem_ld_wait();
-            if (hide >> k & 1u) continue;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float2 tk = unlike != nullptr ? __ldg(unlike + 16 * k + i) : make_float2(__uint_as_float(now.x), ev);
-              if (16 * k + i <= seen) tm = fmaxf(tm, __fmaf_rn(__uint_as_float(v[i]), tk.x * fac, tk.y));
-            }
-          }
-          const bool grow = fresh ? tm > -INFINITY : tm > m + kChMost;
-          if (__any_sync(0xffffffffu, grow)) move(tm, grow);
-          // Beyond kChHuge a step of the score's fp32 is whole powers of two: a weight is taken from the score as it was rounded for the
-          // maximum, so that the largest has its 2^kChTop whatever the rounding did.
-          const bool huge = fabsf(tm) > kChHuge && fabsf(tm) < INFINITY;
-#pragma unroll 1
-          for (int k = 0; k < 4; ++k) {   // P of 16 keys into columns whose scores have been read
-            uint32_t w[8];
-            tmem_ld16(s_addr + 16 * k, v);
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-              float pr[2];
-#pragma unroll
-              for (int b = 0; b < 2; ++b) {
-                const float2 tk = unlike != nullptr ? __ldg(unlike + 16 * k + i + b) : make_float2(__uint_as_float(now.x), ev);
-                const float f = tk.x * fac, x = huge ? __fmaf_rn(__uint_as_float(v[i + b]), f, tk.y) - m - tk.y : fmaf(__uint_as_float(v[i + b]), f, -m);
-                const float pk = 16 * k + i + b <= seen && !(hide >> k & 1u) ? ch_exp2(x) : 0.f;
-                l += pk;
-                pr[b] = pk * ch_exp2(tk.y);
-              }
-              const __half2 h2 = __floats2half2_rn(pr[0], pr[1]);
-              w[i >> 1] = *reinterpret_cast<const uint32_t*>(&h2);
-            }
-            tmem_st8(s_addr + 8 * k, w);
-          }
-          if (now.y & kChNan) {   // tokens stored as NaN: for the rows that see one
-            const uint2 bad = __ldg(reinterpret_cast<const uint2*>(info + j) + 1);
-            const unsigned long long mask = (unsigned long long)bad.y << 32 | bad.x;
-            if (seen >= 0 && (mask & (seen >= 63 ? ~0ull : (1ull << (seen + 1)) - 1ull))) l = NAN;
-          }
-        }
-        tmem_st_wait();
-        tc_fence_before();
-        mbar_arrive(pready + 8 * half);
+        flush(((j - it.j0) >> 1) > kChFlush);
+      }
+      const bool kept[2] = {(it.n + 1) >> 1 > kChFlush, it.n >> 1 > kChFlush};   // streams with sums in memory: there they are completed
+      if (kept[half] && ok) {
+        ok = mbar_wait_warp(pvdone + 8 * half, (n_s - 1) & 1u, abort_flag, p.status, 67);
+        tc_fence_after();
+        if (ok) flush(true);
       }
       float2* mine = xml + (nit & 1u) * 256;
       mine[half * 128 + row] = make_float2(fresh ? -FLT_MAX : m, l);
@@ -768,6 +810,17 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             for (int i = 0; i < 16; ++i) u[i] = 0u;   // (nothing was ever accumulated there)
           }
           tmem_ld_wait();
+          auto from_memory = [&](int stream, uint32_t (&o)[16]) {
+            const float4* keep = p.keep + (size_t)(blockIdx.x * 2 + stream) * kChKeep * kChRows + (half * 8 + c / 4) * kChRows + row;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float4 b = keep[i * kChRows];
+              o[4 * i] = __float_as_uint(b.x); o[4 * i + 1] = __float_as_uint(b.y);
+              o[4 * i + 2] = __float_as_uint(b.z); o[4 * i + 3] = __float_as_uint(b.w);
+            }
+          };
+          if (kept[0]) from_memory(0, v);
+          if (kept[1]) from_memory(1, u);
           if (c == 16) {                          // O is in registers: the accumulators may be written again
             tc_fence_before();
             mbar_arrive(ofree);
@@ -804,7 +857,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
 }
 
 // ---- host
-struct ChunkSpace { size_t kd, vd, qd, fac, info, tok, share, part, desc, total; };
+struct ChunkSpace { size_t kd, vd, qd, fac, info, tok, share, part, desc, keep, total; };
 static ChunkSpace chunk_space(long long R, long long T, long long max_kv, long long n_heads, long long H) {
   ChunkSpace c;
   size_t off = 0;
@@ -819,6 +872,7 @@ static ChunkSpace chunk_space(long long R, long long T, long long max_kv, long l
   c.share = take(kChMaxWorkers * sizeof(int4));
   c.desc = take(2 * kChMaxWorkers * sizeof(int4));
   c.part = take((size_t)kChMaxWorkers * 2 * kChRows * kChPitch * sizeof(float));
+  c.keep = take(tiles > 2 * kChFlush ? (size_t)kChMaxWorkers * 2 * kChKeep * kChRows * sizeof(float4) : 0);
   c.total = off;
   return c;
 }
@@ -839,7 +893,7 @@ moin_status launch_kv_chunk(HostState* hs, const KvView& kv, const int* table, c
   p.q = q; p.q_stride = q_stride; p.out = out; p.out_stride = out_stride; p.rope = rope; p.scale_log2 = scale_log2;
   p.kd = (__half*)(w + c.kd); p.vd = (__half*)(w + c.vd); p.qd = (__half*)(w + c.qd); p.q_fac = (float*)(w + c.fac); p.info = (uint4*)(w + c.info); p.tok = (float2*)(w + c.tok);
   p.dense_blocks = R * kv.H * p.tiles;
-  p.share = (int4*)(w + c.share); p.part = (float*)(w + c.part); p.desc = (int4*)(w + c.desc);
+  p.share = (int4*)(w + c.share); p.part = (float*)(w + c.part); p.keep = (float4*)(w + c.keep); p.desc = (int4*)(w + c.desc);
   const long long items = (long long)p.n_blk * R * kv.H, most = items * ((p.tiles + 1) / 2 + kChItemCost) / kChLeast + 1;   // shares that there can be
   long long workers = 2L * hs->n_sms < kChMaxWorkers ? 2L * hs->n_sms : kChMaxWorkers;
   if (workers > most) workers = most;

@@ -115,3 +115,57 @@ def test_scores_that_jump_by_more_than_fp32_can_add(D, H, G, new, n, size, kerne
     head = (np.arange(H * G) // G)[None]
     want = val[at, head]
     assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * (np.abs(want) + part[at, head]) + 2.0 ** -30 * np.abs(val[at, head]).max(-1, keepdims=True)).all()
+
+
+def _long(n, H, seed, values, keys=None, page=128):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    pages = -(-n // page)
+    cache = moin.KvCache.empty(pages, page, H, 64, DEV)
+    slot = torch.arange(n, dtype=torch.int32, device=DEV)
+    k = torch.randn(n, H, 64, generator=gen, device=DEV)
+    moin.kv_append(cache, slot, (k if keys is None else 0.1 * k + keys).to(torch.bfloat16), values(gen).to(torch.bfloat16))
+    tables = moin.KvTables(torch.arange(pages, dtype=torch.int32, device=DEV).view(1, -1), torch.zeros(pages, dtype=torch.int32, device=DEV), page)
+    return cache, tables, slot, gen
+
+
+@pytest.mark.parametrize("n", [65536, 131072, 524288])
+def test_long_chunks_hold_their_precision(n):
+    """A chunk behind 2^16 to 2^19 tokens, 512 items (more than there are CTAs, so that shares hold whole ones), a flat softmax over
+    values with means of their own: sums as long as they get.  Beside the bound: a sum that loses a little the same way at every step
+    shows in the mean of the errors along the result, roundings to bf16 do not (they are taken off; what is left of them is 2^-9.3 over the
+    root of 6144 results, some of them alike).  2^-12 is a sixteenth of what one rounding may be off by."""
+    H, G, m = 4, 8, 2048
+    cache, tables, slot, gen = _long(n, H, n, lambda gen: 0.2 * torch.randn(n, H, 64, generator=gen, device=DEV) + (4 + 4 * torch.rand(1, H, 64, generator=gen, device=DEV)) *
+                                     torch.where(torch.rand(1, H, 64, generator=gen, device=DEV) < 0.5, -1.0, 1.0))
+    q = (0.2 * torch.randn(m, H * G, 64, generator=gen, device=DEV)).to(torch.bfloat16)
+    pick = torch.tensor([0, 1000, m - 1], device=DEV)
+    moin.set_option(moin.OPT_GEMM_IMPL, 2)
+    try:
+        got = moin.kv_attention(cache, tables, q, i32([0, m]), i32([n]), m, n)[pick].double()
+    finally:
+        moin.set_option(moin.OPT_GEMM_IMPL, 0)
+    want, tol = exact.attention(cache, slot.long(), q[pick], n - m + pick, 0.125, True)
+    assert ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).max()
+    drift = ((got - want.to(torch.bfloat16).double()) / want).mean()
+    assert drift.abs() <= 2.0 ** -12, drift
+
+
+@pytest.mark.parametrize("new", [1200, 2400, 5])
+@pytest.mark.parametrize("kind", ["rising", "falling", "late"])
+def test_long_chunks_whose_maxima_move(kind, new):
+    """Scores that rise or fall by 12 over 140 037 tokens, or are all alike but for the last tokens: sums that went to memory meet another
+    maximum.  150 items (shares begin inside them), 300, and two."""
+    n, H, G = 140037, 2, 8
+    t = torch.arange(n, device=DEV)[:, None, None] / n
+    u = torch.where(torch.arange(64, device=DEV) % 3 == 0, -1.0, 1.0)
+    a = {"rising": 1.5 * t - 0.75, "falling": 0.75 - 1.5 * t, "late": torch.where(t > 0.97, 1.2, -0.3)}[kind]
+    cache, tables, slot, gen = _long(n, H, 7, lambda gen: torch.randn(n, H, 64, generator=gen, device=DEV) + 1, a * u)
+    q = (u + 0.05 * torch.randn(new, H * G, 64, generator=gen, device=DEV)).to(torch.bfloat16)
+    pick = torch.tensor([0, new // 2, new - 1], device=DEV)
+    moin.set_option(moin.OPT_GEMM_IMPL, 2)
+    try:
+        got = moin.kv_attention(cache, tables, q, i32([0, new]), i32([n]), new, n)[pick].double()
+    finally:
+        moin.set_option(moin.OPT_GEMM_IMPL, 0)
+    want, tol = exact.attention(cache, slot.long(), q[pick], n - new + pick, 0.125, True)
+    assert ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).max()
