@@ -540,10 +540,16 @@ moin_status moin_rope_table(float* table, int32_t n_pos, int32_t head_dim, float
  *   rows     [R] rows of the tables, NULL: row i
  *   max_q, max_kv   host upper bounds of a request's queries and cached tokens (outside 1..T / 1..max_pages * page_tokens: those)
  * A query that sees nothing (kv_len 0, a position before the first) gets zeros; so do the queries (at most max_q of them) of a request
- * whose row or kv_len is out of range or whose queries are more than max_q.  A page id outside [0, n_pages) hides its tokens.  Rows of out behind cu_q[R] stay as they were.  fp32 scores, softmax and
- * sums; the un-normalised weights times the value's scale enter the second product rounded to fp16, relative to the row's largest.
+ * whose row or kv_len is out of range or whose queries are more than max_q.  A page id outside [0, n_pages) hides its tokens.  Rows of out
+ * behind cu_q[R] stay as they were.
+ * Precision: scores, softmax and sums are fp32; the un-normalised weights times the value's scale enter the second product rounded to
+ * fp16 (2^-11 of each at most; those below 2^-24 of the largest of their row and 64 channels lose bits).  Queries may be of any finite size.  Long
+ * chunks that go to the tensor cores (heads of 64, by size; MOIN_OPT_GEMM_IMPL = 1 keeps them from it) have the keys and values that
+ * the codes stand for rounded to fp16 as well, 2^-11 of each at most: a score is off by up to scale 2^-11 sum |q||k|, other calls
+ * take the codes as they are.
  * Scratch: workspace, moin_kv_attention_workspace_bytes(...) bytes with the bounds that the call goes by (up to about 1 GiB where long
- * chunks attend to long requests: keys and values are then laid out in 16 bits for the tensor cores), 16-byte aligned, of this call alone while it runs.
+ * chunks attend to long requests: keys and values are then laid out in fp16 for the tensor cores), 16-byte aligned, of this call alone
+ * while it runs.
  * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED, WORKSPACE.  R == 0 or T == 0 is a no-op. */
 size_t moin_kv_attention_workspace_bytes(int32_t R, int32_t T, int32_t max_q, int32_t max_kv, int32_t n_heads, int32_t n_kv_heads,
                                          int32_t head_dim);

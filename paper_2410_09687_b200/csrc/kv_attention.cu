@@ -8,11 +8,11 @@
 // fp16 by one AND: c 2^-24, a subnormal that tensor cores multiply exactly.  The upper nibble of a byte gives 16 c 2^-24: its query
 // channels are divided by 16.  The values' upper nibbles stay beside the lower ones, c + 16 c', and the sums over c, which the same lane
 // holds, are taken off at the end.  Queries are bf16 times a power of two per row that
-// brings them into the middle of fp16: exact.  The weights p sv are the only operand that is rounded, to fp16 (2^-12
+// brings them into the middle of fp16: exact.  The weights p sv are the only operand that is rounded, to fp16 (2^-11
 // relative); their sums p are not.  To keep them inside fp16 whatever the scales are, m follows the maximum of s_t +
-// log2(sv_t): a weight is at most 2^15, and precise to 2^-24 of the row's largest.  m lags (a row is rescaled when a
+// log2(sv_t): a weight is at most 2^15, and precise to 2^-35 of the row's largest (2^-25 at 2^10).  m lags (a row is rescaled when a
 // weight would exceed 2^15, to 2^10), so most tiles need no reduction over the warp.  A wide head's second plane has values, and so
-// scales, of its own: its weights are p sv 2^d with a d per row, so that they too are at most 2^15 and precise to 2^-24 of that
+// scales, of its own: its weights are p sv 2^d with a d per row, so that they too are at most 2^15 and precise to 2^-35 of that
 // plane's largest.  (With one maximum for both, 64 wide requests took 46.4 us instead of 48.2, but of a plane 2^-24 and
 // less of the other only sum p zv was left.)
 //

@@ -2,7 +2,7 @@
 // MMAs, made for a few rows, are bound by their instructions.
 //
 // kv_dense_kernel lays the requests' keys and values out as fp16 [request, position, kv head, 64] in the workspace, each tile of 64
-// tokens times a power of two that brings its largest value to 2^13 .. 2^14 (a value is off by 2^-12 of itself, or by 2^-39 of the
+// tokens times a power of two that brings its largest value to 2^13 .. 2^14 (a value is off by 2^-11 of itself, or by 2^-38 of the
 // tile's largest) - or, in a tile whose tokens are unlike (their largest values differ by more than 2^12), each token times its own,
 // so that no token's precision depends on another, which a row may not even see -, and the queries as fp16 rows (rotated; times a power of two per row: exact) in the order the tiles take
 // them, [kv head, token, head of the group]: a tile of 128 rows is one box whatever the group is.  What is stored as NaN is laid

@@ -169,3 +169,26 @@ def test_long_chunks_whose_maxima_move(kind, new):
         moin.set_option(moin.OPT_GEMM_IMPL, 0)
     want, tol = exact.attention(cache, slot.long(), q[pick], n - new + pick, 0.125, True)
     assert ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).max()
+
+
+@pytest.mark.parametrize("q_scale", [1.0, 8.0, 40.0])
+@pytest.mark.parametrize("heads,H", [(16, 2), (4, 4)])
+def test_chunks_within_the_bound_of_their_own_formats(heads, H, q_scale):
+    """The tensor-core kernel for chunks takes keys and values in fp16: its scores are off by scale 2^-11 sum |q||k| at most, which the
+    bound of tests/kv_exact.py has (that of tests/kv_ref.py is for codes as they are); for scores up to several hundred."""
+    rng = np.random.default_rng(heads)
+    lens, new = [513, 300], [200, 70]
+    cache, tables, table, slot = _serve(rng, lens, H, 64, 32)
+    q = _dev(ref.bf16((q_scale * rng.standard_normal((270, heads, 64))).astype(np.float32)))
+    moin.set_option(moin.OPT_GEMM_IMPL, 2)
+    try:
+        got = moin.kv_attention(cache, tables, q, i32([0, 200, 270]), i32(lens), 200, 513).double()
+    finally:
+        moin.set_option(moin.OPT_GEMM_IMPL, 0)
+    slot = torch.from_numpy(np.asarray(slot)).to(DEV)
+    for a, b, s, n in ((0, 200, slot[:513], 513), (200, 270, slot[513:], 300)):
+        want, tol = exact.attention(cache, s, q[a:b], torch.arange(n - (b - a), n, device=DEV), 0.125, True)
+        assert ((got[a:b] - want).abs() <= tol).all(), ((got[a:b] - want).abs() / tol).max()
+        # the roundings are independent: over 64 products their sum is off by the root of 64 rather than by 64 of them, and the results
+        # in the mean square by a sixteenth of the bound and a rounding of their own
+        assert (got[a:b] - want).norm() <= (tol / 16 + 2.0 ** -9 * want.abs()).norm()
