@@ -471,7 +471,7 @@ typedef struct {
   void* pages;          /* device, moin_kv_bytes(...) bytes, 16-byte aligned */
   int32_t n_pages;
   int32_t page_tokens;  /* 16, 32, 64 or 128 */
-  int32_t n_kv_heads;
+  int32_t n_kv_heads;   /* at most 16384 */
   int32_t head_dim;     /* 64 or 128; n_pages * page_tokens < 2^31 */
 } moin_kv;
 size_t moin_kv_bytes(int32_t n_pages, int32_t page_tokens, int32_t n_kv_heads, int32_t head_dim);
@@ -549,8 +549,9 @@ moin_status moin_rope_table(float* table, int32_t n_pos, int32_t head_dim, float
  * take the codes as they are.
  * Scratch: workspace, moin_kv_attention_workspace_bytes(...) bytes with the bounds that the call goes by (up to about 1 GiB where long
  * chunks attend to long requests: keys and values are then laid out in fp16 for the tensor cores), 16-byte aligned, of this call alone
- * while it runs.
- * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED, WORKSPACE.  R == 0 or T == 0 is a no-op. */
+ * while it runs.  The size depends on MOIN_OPT_GEMM_IMPL: it is that of a call under the option's present value.
+ * Errors: INVALID_ARG, BAD_SHAPE (R > 65535 and max_q * (n_heads / n_kv_heads)^2 >= 2^32 among others), MISALIGNED, WORKSPACE.  R == 0 or
+ * T == 0 is a no-op. */
 size_t moin_kv_attention_workspace_bytes(int32_t R, int32_t T, int32_t max_q, int32_t max_kv, int32_t n_heads, int32_t n_kv_heads,
                                          int32_t head_dim);
 moin_status moin_kv_attention(const moin_kv* kv, const moin_kv_tables* tables, const int32_t* rows, const int32_t* cu_q,
