@@ -271,6 +271,7 @@ struct HostState {
   int device = -1;
   int n_sms = 0;
   int gemm_impl = 0;               // MOIN_OPT_GEMM_IMPL (process-wide option, copied in on every call)
+  int kv_per_sm[4] = {};           // CTAs of the cache attention kernels that fit an SM; 0: not asked yet
   size_t smem_optin[kOptinSlots] = {};   // dynamic shared memory already opted in, per kernel (see ensure_smem_optin)
 };
 moin_status host_state(HostState** out);      // lazily initialised for the current device

@@ -936,7 +936,7 @@ static moin_status kv_att_launch(HostState* hs, int optin, KvAttParams& p, cudaS
   cudaError_t e = ensure_smem_optin(optin, kv_attention_kernel<P, NT, U>, smem);
   if (e != cudaSuccess) return record_cuda(e);
   const long long blocks = ((long long)p.max_q * p.G + 8 * NT - 1) / (8 * NT), items = blocks * p.kv.H * p.R;
-  static int per_sm = 0;   // (the same on every device this library runs on)
+  int& per_sm = hs->kv_per_sm[optin - OPTIN_KV_ATTENTION];
   if (per_sm == 0) {
     int n = 0;
     if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kv_attention_kernel<P, NT, U>, 32 * kKvAttWarps, smem)) != cudaSuccess) return record_cuda(e);
