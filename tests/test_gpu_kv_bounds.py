@@ -192,3 +192,35 @@ def test_chunks_within_the_bound_of_their_own_formats(heads, H, q_scale):
         # the roundings are independent: over 64 products their sum is off by the root of 64 rather than by 64 of them, and the results
         # in the mean square by a sixteenth of the bound and a rounding of their own
         assert (got[a:b] - want).norm() <= (tol / 16 + 2.0 ** -9 * want.abs()).norm()
+
+
+@pytest.mark.parametrize("D,G,q", [(64, 8, 1), (64, 4, 3), (64, 4, 30), (128, 4, 1), (128, 4, 3), (128, 2, 20)])
+@pytest.mark.parametrize("kind", ["one", "few", "many short", "more than there are CTAs"])
+def test_attention_under_loose_bounds(kind, D, G, q):
+    """Short requests that were declared as long as their rows, and rows that hold much more: most shares are empty, and requests
+    without queries or tokens stand between the others."""
+    rng = np.random.default_rng(D + G + q + len(kind))
+    lens = {"one": [37], "few": [31, 0, 5, 60, 17], "many short": [int(x) for x in rng.integers(0, 60, 40)],
+            "more than there are CTAs": [int(x) for x in rng.integers(0, 40, 300)]}[kind]
+    H = 4 if kind == "more than there are CTAs" else 2
+    if kind == "more than there are CTAs" and q > 1:
+        lens = lens[:110]
+    new = [0 if i % 5 == 3 else min(q, n) if n else i % 2 for i, n in enumerate(lens)]
+    cache, tables, table, _ = _serve(rng, lens, H, D, 32)
+    wide = np.full((len(lens), 300), -1, np.int64)      # rows of 9600 tokens
+    wide[:, :table.shape[1]] = table
+    tables = moin.KvTables(i32(wide), torch.zeros(cache.n_pages, dtype=torch.int32, device=DEV), 32)
+    cu = np.concatenate([[0], np.cumsum(new)])
+    T = int(cu[-1])
+    x = ref.bf16(rng.standard_normal((T + 2, H * G, D)).astype(np.float32))
+    want, tol = ref.attention(cache.pages.cpu().numpy(), wide, None, cu, lens, x, D ** -0.5, 32)
+    moin.set_option(moin.OPT_GEMM_IMPL, 1)
+    try:
+        for max_q in (0, max(q, 1)):
+            out = torch.full((T + 2, H * G, D), 9.0, dtype=torch.bfloat16, device=DEV)
+            moin.kv_attention(cache, tables, _dev(x), i32(cu), i32(lens), max_q, 0, out=out)
+            got = out.double().cpu().numpy()
+            assert (got[T:] == 9).all()
+            assert (np.abs(got[:T] - want[:T]) <= tol[:T]).all(), np.nanmax(np.abs(got[:T] - want[:T]))
+    finally:
+        moin.set_option(moin.OPT_GEMM_IMPL, 0)
