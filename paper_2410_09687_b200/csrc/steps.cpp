@@ -93,12 +93,13 @@ cudaStream_t stream_of(PyObject* o) {   // None: the current one
   return o == Py_None ? c10::cuda::getCurrentCUDAStream().stream() : reinterpret_cast<cudaStream_t>((intptr_t)integer(o));
 }
 
-// A new bf16 tensor beside `like` (on the current CUDA device: the caller has looked) for a call on stream s, without the dispatcher.
-// Its memory belongs to s: of a block of the current stream, that one's pending work may be anywhere.
-at::Tensor fresh(at::IntArrayRef size, const at::Tensor& like, cudaStream_t s) {
-  c10::cuda::OptionalCUDAStreamGuard guard;
-  if (s != c10::cuda::getCurrentCUDAStream().stream()) guard.reset_stream(c10::cuda::getStreamFromExternal(s, like.get_device()));
-  return at::Tensor(at::detail::empty_cuda(size, at::kBFloat16, like.device(), std::nullopt));
+// A new bf16 tensor beside `like` (on the current CUDA device: the caller has looked) for a call on `stream`, without the dispatcher.
+// Its memory belongs to that stream: of a block of the current one, pending work may be anywhere.
+at::Tensor fresh(at::IntArrayRef size, const at::Tensor& like, PyObject* stream) {
+  auto make = [&] { return at::Tensor(at::detail::empty_cuda(size, at::kBFloat16, like.device(), std::nullopt)); };
+  if (stream == Py_None) return make();
+  const c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(stream_of(stream), like.get_device()));
+  return make();
 }
 
 template <class F>
@@ -159,11 +160,10 @@ PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& slot = tensor(a[1]);
     const int32_t T = length(slot);
     const int32_t* s = vec(a[1], T);
-    const cudaStream_t stream = stream_of(a[4]);
-    auto out = [&](PyObject* o) { return o == Py_None ? fresh({T, kv->n_kv_heads, kv->head_dim}, slot, stream) : tensor(o); };
+    auto out = [&](PyObject* o) { return o == Py_None ? fresh({T, kv->n_kv_heads, kv->head_dim}, slot, a[4]) : tensor(o); };
     const at::Tensor k = out(a[2]), v = out(a[3]);
     const Rows kr = rows_of(k, T, kv->n_kv_heads, kv->head_dim), vr = rows_of(v, T, kv->n_kv_heads, kv->head_dim);
-    const int32_t st = f_read(kv, s, kr.p, kr.stride, vr.p, vr.stride, T, stream);
+    const int32_t st = f_read(kv, s, kr.p, kr.stride, vr.p, vr.stride, T, stream_of(a[4]));
     return Py_BuildValue("(iNN)", (int)st, THPVariable_Wrap(k), THPVariable_Wrap(v));
   });
 }
@@ -182,8 +182,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (q.size(1) > INT32_MAX) refuse("too many heads");
     const int32_t heads = (int32_t)q.size(1);
     const Rows qr = rows_of(q, T, heads, kv->head_dim);
-    const cudaStream_t s = stream_of(a[11]);
-    const at::Tensor out = a[10] == Py_None ? fresh(q.sizes(), q, s) : tensor(a[10]);
+    const at::Tensor out = a[10] == Py_None ? fresh(q.sizes(), q, a[11]) : tensor(a[10]);
     const Rows outr = rows_of(out, T, heads, kv->head_dim);
     const Rope rope = rope_of(a[9], kv->head_dim);
     int32_t max_q = size32(a[5]);
@@ -199,6 +198,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       scale = kv->head_dim == 64 ? 0.125 : 0.08838834764831845;
     }
     const int32_t *cu = vec(a[3], (int64_t)R + 1), *len = vec(a[4], R), *rows = vec(a[7], R);
+    const cudaStream_t s = stream_of(a[11]);
     const size_t bytes = f_ws(R, T, max_q, max_kv, heads, kv->n_kv_heads, kv->head_dim);
     void* ws = c10::cuda::CUDACachingAllocator::raw_alloc_with_stream(bytes, s);
     const int32_t st = f_attention(kv, tables, rows, cu, len, R, T, max_q, max_kv, qr.p, qr.stride, heads, (float)scale, rope.p, rope.n, outr.p,
