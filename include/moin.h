@@ -543,10 +543,11 @@ moin_status moin_rope_table(float* table, int32_t n_pos, int32_t head_dim, float
  * whose row or kv_len is out of range or whose queries are more than max_q.  A page id outside [0, n_pages) hides its tokens.  Rows of out
  * behind cu_q[R] stay as they were.
  * Precision: scores, softmax and sums are fp32; the un-normalised weights times the value's scale enter the second product rounded to
- * fp16 (2^-11 of each at most; those below 2^-24 of the largest of their row and 64 channels lose bits).  Queries may be of any finite size.  Long
- * chunks that go to the tensor cores (heads of 64, by size; MOIN_OPT_GEMM_IMPL = 1 keeps them from it) have the keys and values that
- * the codes stand for rounded to fp16 as well, 2^-11 of each at most: a score is off by up to scale 2^-11 sum |q||k|, other calls
- * take the codes as they are.
+ * fp16 (2^-11 of each at most; those below 2^-24 of the largest of their row and 64 channels lose bits, and more of them where the
+ * halves of a wide head are over 2^100 apart).  Queries may be of any size whose scores fp32 holds.  Long chunks that go to the tensor
+ * cores (heads of 64, by size; MOIN_OPT_GEMM_IMPL = 1 keeps them from it) have the keys and values that the codes stand for rounded to
+ * fp16 as well, by at most 2^-11 of each, 2^-26 of its token's largest or 2^-89: a score is off by up to scale 2^-11 sum |q||k|.  Other
+ * calls take the codes as they are.
  * Scratch: workspace, moin_kv_attention_workspace_bytes(...) bytes with the bounds that the call goes by (up to about 1 GiB where long
  * chunks attend to long requests: keys and values are then laid out in fp16 for the tensor cores), 16-byte aligned, of this call alone
  * while it runs.  The size depends on MOIN_OPT_GEMM_IMPL: it is that of a call under the option's present value.

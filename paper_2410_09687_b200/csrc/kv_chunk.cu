@@ -21,8 +21,8 @@
 // A weight below 2^-14 is off by 2^-25 at most: 2^-30 of the row's largest, so that 2^19 keys stay within 2^-11 of the sum.
 // Tensor memory: S_h / P_h at columns 64 h, O_h at 128 + 64 h.  Every mbarrier wait is bounded; on expiry the CTA raises the status
 // flag, drains and returns.
-// 4 requests of 512 new tokens behind 830 to 5900, 32 heads on 4: about 107 us for 52 GFLOP, bound by the instructions and exponentials of the
-// weights (a warp's tile 1.3 us, four warps on a scheduler: issue slots 49 % busy, exponentials 52 %, tensor cores 24 %) and by the chain.  One warp that issued both streams' MMAs took 900
+// 4 requests of 512 new tokens behind 830 to 5900, 32 heads on 4: about 109 us for 52 GFLOP, bound by the instructions and exponentials of the
+// weights (a warp's tile 1.3 us, four warps on a scheduler: issue slots 48 % busy, exponentials 52 %, tensor cores 23 %) and by the chain.  One warp that issued both streams' MMAs took 900
 // cycles a round, and with the maximum found first, whole items per CTA and all scores behind the product it was 125 us.
 #include <cuda.h>
 #include <float.h>

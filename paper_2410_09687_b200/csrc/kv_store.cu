@@ -119,10 +119,11 @@ __device__ __forceinline__ void kv_rotate_words(uint32_t& a, uint32_t& b, const 
 // A warp stores the keys or the values of a group, of one head and NP planes of it: its lanes load two token rows (g and g + 8 of
 // the tile, 16 channels a plane each), quantise them and hold the tile's words.  Whole tiles are written by 16-byte stores, others
 // byte by byte, a token's own bytes only.
-// Bound by the instructions of rotation and quantisation (about 550 a warp, tile and plane) and the chain slot, position, (cos, sin),
-// store for prompts, by the chain alone for single tokens.  A wide head's planes in one warp (NP = 2): a key's partner plane is not
-// loaded and rotated twice; 21 thousand tokens of 8 heads of 128 take 52 us, with a warp per plane 71 (112 MB: 2.2 TB/s); for few
-// tokens a warp per plane is 0.9 us faster.  Seven CTAs an SM: 2 us less than the six that 80 registers leave.
+// Bound by the chain slot, position, (cos, sin), row, quantised words, store, with few warps to hide it: for prompts issue slots are
+// 54 % busy (about 550 instructions a warp, tile and plane) at 35 % of the warps that an SM holds, for single tokens there is nothing
+// but the chain.  A wide head's planes in one warp (NP = 2): a key's partner plane is not loaded and rotated twice; 21 thousand tokens of
+// 8 heads of 128 take 46 us (110 MB: 2.4 TB/s); when this form took 52, a warp per plane took 71, and for few tokens was 0.9 us
+// faster.  Seven CTAs an SM: 2 us less than the six that 80 registers leave.
 template <int D, int NP>
 __global__ void __launch_bounds__(32 * kKvStoreWarps, 7)
 kv_append_kernel(const KvStoreParams p) {
