@@ -681,7 +681,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             if (!ok) break;
             const float tm = fmaf(fmaxf(ma, mc), c, base);
             // too small for fp32 (the maximum comes from values 2^80 times this tile's), of keys whose 2^(s - m) still counts in the sum
-            const bool grow = fresh ? tm > -INFINITY : tm > m + kChMost, small = !fresh && tm < m - 80.f && tm - ev > m - 60.f;
+            // (differences, which are exact: of large maxima a sum with 15 rounds to 16, and 2^16 is beyond fp16)
+            const bool grow = fresh ? tm > -INFINITY : tm - m > kChMost, small = !fresh && tm < m - 80.f && tm - ev > m - 60.f;
             // so large that a product not rounded, less a maximum that is, may be anything: the row's scores are first taken less the largest
             const bool huge = base == ev && fabsf(tm) > kChHuge && fabsf(tm) < INFINITY;
             const uint32_t votes = (grow ? 1u : 0u) | (small ? 2u : 0u) | (huge ? 4u : 0u), vote = __reduce_or_sync(0xffffffffu, votes);
@@ -730,7 +731,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
                 if (16 * k + i <= seen) tm = fmaxf(tm, __fmaf_rn(__uint_as_float(v[i]), tk.x * fac, tk.y));
               }
             }
-            const bool grow = fresh ? tm > -INFINITY : tm > m + kChMost;
+            const bool grow = fresh ? tm > -INFINITY : tm - m > kChMost;
             if (__any_sync(0xffffffffu, grow)) move(tm, grow);
             // Beyond kChHuge a step of the score's fp32 is whole powers of two: a weight is taken from the score as it was rounded for the
             // maximum, so that the largest has its 2^kChTop whatever the rounding did.

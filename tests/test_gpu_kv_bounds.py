@@ -224,3 +224,25 @@ def test_attention_under_loose_bounds(kind, D, G, q):
             assert (np.abs(got[:T] - want[:T]) <= tol[:T]).all(), np.nanmax(np.abs(got[:T] - want[:T]))
     finally:
         moin.set_option(moin.OPT_GEMM_IMPL, 0)
+
+
+@pytest.mark.parametrize("D,H,G,new,n", [(64, 2, 8, 1, 700), (64, 1, 4, 70, 300), (128, 2, 4, 1, 500), (128, 1, 2, 20, 200), (64, 1, 8, 1, 40000)])
+@pytest.mark.parametrize("size", [10, 16, 24, 40])
+def test_scores_that_are_all_far_below_zero(D, H, G, new, n, size, kernel):
+    """Every score is between -2^size and -2^(size + 1) times 64 or so; the least negative key, seen by all, takes all weight: the next one is
+    2^-5 of its size further, hundreds and more in the exponent."""
+    rng = np.random.default_rng(size + n)
+    cache, tables, _, slot = _serve(rng, [n], H, D, 32)
+    u = rng.choice([-1.0, 1.0], D)
+    a = -rng.uniform(1.0625, 2, n)
+    best = int(rng.integers(0, n - new + 1))
+    a[best] = -1
+    k = ref.bf16((2.0 ** size * a[:, None, None] * u).astype(np.float32)) * np.ones((1, H, 1), np.float32)
+    v = ref.bf16((rng.standard_normal((n, H, D)) * 2.0 ** rng.integers(-12, 13, (n, 1, 1))).astype(np.float32))
+    moin.kv_append(cache, i32(slot), _dev(k), _dev(v))
+    q = ref.bf16(np.broadcast_to(64 * u, (new, H * G, D)).astype(np.float32))
+    got = moin.kv_attention(cache, tables, _dev(q), i32([0, new]), i32([n]), new, n).double().cpu().numpy()
+    c, s, z = ref.load(cache.pages.cpu().numpy(), np.asarray(slot)[best:best + 1], 1)
+    head = np.arange(H * G) // G
+    val, part = ((z[..., None] + s[..., None] * c).reshape(H, D)[head], (s[..., None] * c).reshape(H, D)[head])
+    assert (np.abs(got - val) <= 2.0 ** -8 * np.abs(val) + 2.0 ** -10 * (np.abs(val) + part) + 2.0 ** -30 * np.abs(val).max(-1, keepdims=True)).all()
