@@ -779,8 +779,8 @@ def kv_read(cache: KvCache, slot: torch.Tensor, k: Optional[torch.Tensor] = None
 def kv_attention(cache: KvCache, tables: KvTables, q: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor, max_q: int = 0,
                  max_kv: int = 0, rows: Optional[torch.Tensor] = None, scale: Optional[float] = None,
                  rope: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """moin_kv_attention: q [T, n_heads, head_dim] over the cached tokens of each token's request.  Returns out, like q; rows of a new
-    ``out`` behind the last request are undefined.  scale: 1 / sqrt(head_dim) unless given.  The scratch comes from the caching
+    """moin_kv_attention: q [T, n_heads, head_dim] over the cached tokens of each token's request.  Returns out, like q (which it may not
+    overlap); rows of a new ``out`` behind the last request are undefined.  scale: 1 / sqrt(head_dim) unless given.  The scratch comes from the caching
     allocator and is this call's alone: calls, streams and captured graphs may overlap."""
     st, out = (_steps or _load_steps()).attention(cache.addr, tables.addr, q, cu_q, kv_len, max_q, max_kv, rows, scale, rope, out, _handle(stream),
                                                    _same_device(cache, tables))

@@ -80,6 +80,14 @@ Rows rows_of(const at::Tensor& t, int64_t T, int64_t heads, int64_t dim) {
   if (t.stride(-1) != 1 || (t.dim() == 3 && heads > 1 && t.stride(1) != dim)) refuse("the heads of a token must lie side by side");
   return {t.data_ptr(), T > 1 ? t.stride(0) : heads * dim};
 }
+// Do rows of `width` elements share memory?  (Queries and results may be parts of the rows of one tensor.)
+bool share(const Rows& a, const Rows& b, int64_t T, int64_t width) {
+  const int64_t off = (static_cast<char*>(b.p) - static_cast<char*>(a.p)) / 2;   // elements; both are 16-bit, 16-byte aligned (or refused)
+  if (T == 0 || off >= (T - 1) * a.stride + width || -off >= (T - 1) * b.stride + width) return false;
+  if (a.stride != b.stride) return true;
+  const int64_t in = ((off % a.stride) + a.stride) % a.stride;
+  return in < width || a.stride - in < width;
+}
 // [positions, dim / 2, 2] fp32
 struct Rope { const float* p; int32_t n; };
 Rope rope_of(PyObject* o, int64_t dim) {
@@ -184,6 +192,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Rows qr = rows_of(q, T, heads, kv->head_dim);
     const at::Tensor out = a[10] == Py_None ? fresh(q.sizes(), q, a[11]) : tensor(a[10]);
     const Rows outr = rows_of(out, T, heads, kv->head_dim);
+    if (a[10] != Py_None && share(qr, outr, T, (int64_t)heads * kv->head_dim)) refuse("out may not overlap q: other parts of the call still read it");
     const Rope rope = rope_of(a[9], kv->head_dim);
     int32_t max_q = size32(a[5]);
     if (max_q < 1 || max_q > T) max_q = T;
