@@ -130,9 +130,11 @@ struct KvQuery {
 // scores, factors and sums 2^-16 smaller until the score is complete: powers of two, so other rows' bits stay.  (Steps of their own:
 // the others pay nothing.)
 // These steps also take over where a row's maximum passes kKvCoarse: fp32 has no room for log2(sv) beside it then, so m is the
-// largest score alone, and the first plane's weights are p sv 2^e, as the second plane's are p sv 2^d.
+// largest score alone, and the first plane's weights are p sv 2^e, as the second plane's are p sv 2^d.  And where a row's scores rise
+// by more than kKvGone: what it has is nothing beside 2^kKvGone, and the new scores, taken less the old maximum, may have lost
+// theirs to its size, so the row begins anew with them.
 constexpr int kKvLarge = 16;
-constexpr float kKvCoarse = 0x1p20f;
+constexpr float kKvCoarse = 0x1p20f, kKvGone = 512.f;
 
 template <int P, int NT>
 __device__ __forceinline__ void kv_load_query(const KvAttParams& p, const KvItem& it, int lane, KvQuery<P, NT>& q) {
@@ -232,7 +234,7 @@ __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_gr
 
 // U tiles of 16 tokens from shared memory, the first at key0; bit u of `there`: tile u is part of the warp's work.  `whole`: every
 // row sees every token.  `large`: of a warp with large queries or scores; without it false is returned, and nothing is done, where it
-// has to be made with it.
+// has to be made with it, and with it where it has to be made again.
 template <bool whole, bool large, int P, int NT, int U>
 __device__ __forceinline__ bool kv_step(const uint8_t* tiles, uint32_t there, int key0, int kv_len, const KvQuery<P, NT>& q, int lane, KvState<P, NT>& st,
                                         uint64_t (&e)[NT]) {
@@ -331,9 +333,58 @@ __device__ __forceinline__ bool kv_step(const uint8_t* tiles, uint32_t there, in
         float m[2];
         unpair_f32(st.m[n], m[0], m[1]);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) coarse = coarse || (top[n][0][c] > -INFINITY && fabsf(top[n][0][c] - m[c]) > kKvCoarse);
+        for (int c = 0; c < 2; ++c) {
+          const float t = top[n][0][c];
+          coarse = coarse || (t > -INFINITY && fabsf(t - m[c]) > kKvCoarse) || (t > kKvGone && !(st.fresh >> (2 * n + c) & 1u));
+        }
       }
       if (__any_sync(0xffffffffu, coarse)) return false;
+    } else {
+      bool anew = false;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float most[2] = {-INFINITY, -INFINITY}, m[2], d[2], was[2], keep[2];
+        unpair_f32(st.m[n], m[0], m[1]);
+        unpair_f32(e[n], was[0], was[1]);
+        if (P == 2) unpair_f32(st.d[n], d[0], d[1]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float x, y;
+            unpair_f32(s[u][n][h], x, y);
+            most[0] = fmaxf(most[0], x);
+            most[1] = fmaxf(most[1], y);
+          }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) most[c] = fmaxf(most[c], __shfl_xor_sync(0xffffffffu, most[c], o));
+          const uint32_t bit = 1u << (2 * n + c);
+          const bool gone = most[c] > kKvGone && !(st.fresh & bit);
+          anew = anew || gone;
+          if (gone) {
+            st.fresh |= bit;
+            m[c] = d[c] = was[c] = 0.f;
+          }
+          keep[c] = gone ? 0.f : 1.f;   // (times the sums: a NaN stays)
+        }
+        const uint64_t f = pair_f32(keep[0], keep[1]);
+        st.m[n] = pair_f32(m[0], m[1]);
+        e[n] = pair_f32(was[0], was[1]);
+        if (P == 2) st.d[n] = pair_f32(d[0], d[1]);
+        st.l[n] = mul2(st.l[n], f);
+#pragma unroll
+        for (int pl = 0; pl < P; ++pl) {
+          st.z[pl][n] = mul2(st.z[pl][n], f);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            st.o[n][pl][j][0] = mul2(st.o[n][pl][j][0], f);
+            st.o[n][pl][j][1] = mul2(st.o[n][pl][j][1], f);
+          }
+        }
+      }
+      if (__any_sync(0xffffffffu, anew)) return false;
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -754,10 +805,10 @@ kv_attention_kernel(const KvAttParams p) {
       }
     }
 #pragma unroll 1
-    for (; i < n_steps; ++i) {
+    while (i < n_steps) {
       if (!begun) begin(i);
-      begun = false;
-      step(std::true_type(), i);
+      begun = !step(std::true_type(), i);   // (again at most once: a row that has begun anew does not)
+      i += begun ? 0 : 1;
     }
     // ---- the rows to shared memory: the ring is idle, a piece to be joined with the warp before has its own place
     __syncwarp();

@@ -246,3 +246,23 @@ def test_scores_that_are_all_far_below_zero(D, H, G, new, n, size, kernel):
     head = np.arange(H * G) // G
     val, part = ((z[..., None] + s[..., None] * c).reshape(H, D)[head], (s[..., None] * c).reshape(H, D)[head])
     assert (np.abs(got - val) <= 2.0 ** -8 * np.abs(val) + 2.0 ** -10 * (np.abs(val) + part) + 2.0 ** -30 * np.abs(val).max(-1, keepdims=True)).all()
+
+
+@pytest.mark.parametrize("D,H,G,new,n", [(64, 2, 8, 1, 700), (64, 1, 4, 70, 400), (128, 2, 4, 1, 500), (128, 1, 2, 20, 300), (64, 1, 8, 1, 40000), (128, 1, 7, 48, 6000)])
+@pytest.mark.parametrize("size", [18, 24, 40, 80])
+@pytest.mark.parametrize("values", [-40, 0, 47])
+def test_scores_that_come_back_from_far_below_zero(D, H, G, new, n, size, values, kernel):
+    """Keys of -2^size and less, then ordinary ones: the first leave no weight, the rest is the formula over the others; values of any
+    size, planes of a wide head of their own."""
+    rng = np.random.default_rng(size + n + values)
+    cache, tables, _, slot = _serve(rng, [n], H, D, 32)
+    u, half = rng.choice([-1.0, 1.0], D), n // 2
+    a = np.concatenate([-2.0 ** size * rng.uniform(1, 2, half), np.zeros(n - half)])
+    k = a[:, None, None] * u + np.where(np.arange(n) < half, 0, 1)[:, None, None] * rng.standard_normal((n, H, D))
+    v = rng.standard_normal((n, H, D // 64, 64)) * 2.0 ** (values + 12 * rng.uniform(-1, 1, (n, 1, D // 64, 1)))
+    moin.kv_append(cache, i32(slot), _dev(ref.bf16(k.astype(np.float32))), _dev(ref.bf16(v.reshape(n, H, D).astype(np.float32))))
+    q = _dev(ref.bf16((4 * u + rng.standard_normal((new, H * G, D))).astype(np.float32)))
+    got = moin.kv_attention(cache, tables, q, i32([0, new]), i32([n]), new, n).double()
+    slot = torch.from_numpy(np.asarray(slot)).to(DEV)[half:]
+    want, tol = exact.attention(cache, slot, q, torch.arange(n - new, n, device=DEV) - half, D ** -0.5, kernel == "tcgen05" and D == 64)
+    assert got.isfinite().all() and ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).max()
