@@ -13,7 +13,7 @@
 // log2(sv_t): a weight is at most 2^15, and precise to 2^-35 of the row's largest (2^-25 at 2^10).  m lags (a row is rescaled when a
 // weight would exceed 2^15, to 2^10), so most tiles need no reduction over the warp.  A wide head's second plane has values, and so
 // scales, of its own: its weights are p sv 2^d with a d per row, so that they too are at most 2^15 and precise to 2^-35 of that
-// plane's largest.  (With one maximum for both, 64 wide requests took 46.4 us instead of 48.2, but of a plane 2^-24 and
+// plane's largest.  (With one maximum for both, 64 wide requests, now 49.2 us, took 1.8 less, but of a plane 2^-24 and
 // less of the other only sum p zv was left.)
 //
 // Sums over many tokens are made by fp32 additions that round, not in the accumulator of the MMA, which truncates: codes are
